@@ -26,7 +26,7 @@
  *  - Calls on different streams that write the same buffers race; calls are
  *    otherwise re-entrant.
  *  - All sequences of a batch share one past length, except in
- *    infllm_step_varlen.
+ *    infllm_step_varlen, infllm_prompt_attend and infllm_prefix_attend.
  */
 #ifndef INFLLM_H
 #define INFLLM_H
@@ -338,6 +338,102 @@ infllm_status infllm_step_varlen(const infllm_params* p, const infllm_memory* m,
                                  int32_t n_q, const int64_t* past_lens, const int32_t* units_built, float* scores,
                                  int32_t* idx, void* out, int64_t out_head_stride, float* lse, void* workspace,
                                  size_t workspace_bytes, void* stream);
+
+/* ---- batches that share a document ------------------------------------------
+ * What a program that serves many requests over long documents uses beside the
+ * step: packed prompts, the continuations of one document, and copies of whole
+ * sequences between memories.  All of them take positions as already applied
+ * (E_UNSUPPORTED with params.rope_inv_freq, except infllm_copy_sequences).
+ * Values that are not finite stay with the rows that see them: a NaN or infinity
+ * in a key, a value or behind a sequence's end changes no row that does not
+ * attend it; a NaN among a row's scores makes its output and lse NaN. */
+
+/* Causal attention of whole prompts, packed: n_seqs sequences of seq_lens[i] >= 0
+ * tokens (a HOST array, read during the call) lie one after another, `total`
+ * tokens in all.  For token i of a sequence and query head h (kv head g = h / G):
+ * one softmax of sm_scale * q_i . k_t over the tokens t <= i of the same sequence.
+ * This is the step's attention for prompts that fit the window (nothing evicted),
+ * for all of them in one launch (256 sequences that are not empty; more take one
+ * launch for every 256).  Of the params only the heads, head_dim, dtype and
+ * sm_scale matter.
+ *  q, k, v, out: dtype rows of head_dim elements; the row of token t and head h
+ *     starts at t * token_stride + h * head_stride elements (k and v share their
+ *     strides; strides are multiples of 16 bytes and not negative; the output's
+ *     rows must not overlap).  So [head][token][D], [token][head][D] and views of a
+ *     fused projection [token][(Hq + 2 Hkv) * D] all do.
+ *  lse: optional [Hq][total] float32 natural log-sum-exp of the logits.
+ *  workspace: infllm_prompt_workspace_bytes(p, n_seqs, seq_lens) bytes, which may
+ *     be 0 (then NULL is allowed).
+ * Rows past `total` are neither read nor written.  E_UNSUPPORTED where total * G
+ * exceeds 2^31 - 1, or for bf16 a sequence's keys span more than 4 GiB. */
+size_t infllm_prompt_workspace_bytes(const infllm_params* p, int32_t n_seqs, const int32_t* seq_lens);
+infllm_status infllm_prompt_attend(const infllm_params* p, int32_t n_seqs, const int32_t* seq_lens, const void* q,
+                                   int64_t q_token_stride, int64_t q_head_stride, const void* k, const void* v,
+                                   int64_t kv_token_stride, int64_t kv_head_stride, void* out,
+                                   int64_t out_token_stride, int64_t out_head_stride, float* lse, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that infllm_prefix_score and infllm_prefix_attend need for
+ * `batch` continuations of n_q current tokens each, a document of prefix_len
+ * tokens and own stores of own_capacity tokens (up to params.topk looked-up
+ * units).  Depends only on these arguments; 0 where they are invalid. */
+size_t infllm_prefix_workspace_bytes(const infllm_params* p, int32_t batch, int32_t n_q, int64_t prefix_len,
+                                     int64_t own_capacity);
+
+/* Unit relevance of a shared document: as infllm_score_units, for `batch`
+ * continuations of the one sequence in `prefix` (prefix->batch must be 1; a slot
+ * of a larger memory is a view with its pointers moved), whose key sums are read
+ * once for all.  q: [batch][Hq] heads of n_q x D dtype rows; scores:
+ * [batch][Hkv][n_units] float32, which infllm_select_topk takes with
+ * rows = batch * Hkv.  Uses only unit_ksum and max_units of the memory. */
+infllm_status infllm_prefix_score(const infllm_params* p, const infllm_memory* prefix, int32_t batch, const void* q,
+                                  int64_t q_head_stride, int32_t n_q, int32_t n_units, float* scores, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/* Attention of own->batch continuations (at most 64) of one document.  The document
+ * is the first prefix_len tokens of `prefix` (prefix->batch must be 1), with the
+ * partition of infllm_partition at prefix_len; continuation b has own_lens[b] >= 0
+ * tokens of its own (a HOST array) in slot b of `own`, followed by its n_q current
+ * tokens X.  For query i of continuation b, head h (kv head g): one softmax of
+ * sm_scale * q . k over I, the units idx[b][g][0 .. min(n_idx, n_units)) of the
+ * document (entries that are negative or >= n_units are skipped), L, the own tokens,
+ * and X up to i.  The keys of I and L are read once for all continuations.  The
+ * partition stays that of the document: with n_local >= prefix_len the whole
+ * document is attended (n_idx = 0), and tokens of a continuation are not evicted
+ * (one that grows past the window is moved to a memory of its own with
+ * infllm_copy_sequences).  Of the memories only batch, capacity, k and v are used.
+ *  k, v: the current tokens' keys and values, [batch][Hkv] heads of n_q x D rows
+ *     with kv_head_stride, written to positions own_lens[b] .. + n_q of `own`
+ *     before the attention; both NULL when they are there already.
+ *  idx: [batch][Hkv][n_idx] int32 (NULL allowed when nothing is looked up);
+ *     n_idx <= params.topk for the workspace of infllm_prefix_workspace_bytes.
+ *  out, lse: as in infllm_chunk_attend ([batch][Hq], n_q rows each).
+ * The two stores must not overlap where X is written.  E_RANGE if prefix_len or an
+ * own_lens[b] + n_q exceeds its capacity.  For bf16 a [capacity][D] slice of either
+ * store spans at most 4 GiB (else E_UNSUPPORTED). */
+infllm_status infllm_prefix_attend(const infllm_params* p, const infllm_memory* prefix, int64_t prefix_len,
+                                   const infllm_memory* own, const int64_t* own_lens, const void* q,
+                                   int64_t q_head_stride, const void* k, const void* v, int64_t kv_head_stride,
+                                   int32_t n_q, const int32_t* idx, int32_t n_idx, void* out, int64_t out_head_stride,
+                                   float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Copies of whole sequences: slot src_seq[i] of `src` to slot dst_seq[i] of `dst`,
+ * i < n (at most 64), all in one launch.  Forks a sequence (several copies of one
+ * slot, whose bytes are read once), moves it to a memory of another size, or closes
+ * up a batch in place (dst and src the same memory).  lens[i] positions of K and V
+ * (and k_rot with the positional remap) are copied, the representatives and key
+ * sums of units_built[i] units (<= n_units(lens[i]), as the caller passes units_built
+ * to the next infllm_step), and the query rings' slots of the last
+ * min(lens[i], src ring, dst ring) positions, so that the copy is continued like its
+ * source (a ring smaller than the source's must still be one the next append accepts).
+ * Everything else of the destination is left as it was.  The arrays are HOST arrays.
+ * With INFLLM_REPR_MEAN there are no rings and no representatives.
+ * E_RANGE: a slot outside its memory, a length beyond a capacity, units beyond a
+ * max_units.  E_SHAPE: two copies to one slot, or a destination whose K overlaps a
+ * slot that the call reads. */
+infllm_status infllm_copy_sequences(const infllm_params* p, const infllm_memory* dst, const infllm_memory* src, int32_t n,
+                                    const int32_t* dst_seq, const int32_t* src_seq, const int64_t* lens,
+                                    const int32_t* units_built, void* stream);
 
 /* Static description of a status code. */
 const char* infllm_status_string(infllm_status s);

@@ -4,6 +4,7 @@
 //    softmax; the float32 accuracy path.  It reads keys through the same
 //    virtual key axis as the other kernels.
 #include <algorithm>
+#include <type_traits>
 
 #include "launch.h"
 
@@ -11,6 +12,8 @@ namespace infllm {
 
 hipError_t launch_attend_mfma(const AttendArgs& a, hipStream_t s);
 hipError_t launch_attend_decode(const AttendArgs& a, hipStream_t s);
+hipError_t launch_prompt_mfma(const PromptArgs& a, hipStream_t s);
+hipError_t launch_prefix_mfma(const PrefixArgs& a, hipStream_t s);
 
 namespace {
 
@@ -51,8 +54,13 @@ constexpr int kF32Sel = 2048;  // lookup entries kept in LDS
 // With the positional remap (ROPE) a wave holds both forms of its query rows; a tile
 // of memory keys takes the one at distance l_L, a tile of local keys the other, and
 // the tile that holds both kinds takes both and picks per key.
-template <int D, int NW, bool ROPE>
-__global__ void __launch_bounds__(64 * NW, 1) attend_f32_kernel(AttendArgs a) {
+// Args: a step's arguments, packed prompts' (the keys of a row tile are one run of
+// strided rows) or the prefix attention's (one of its regions), without the remap.
+template <int D, int NW, bool ROPE, typename Args = AttendArgs>
+__global__ void __launch_bounds__(64 * NW, 1) attend_f32_kernel(Args a) {
+  constexpr bool kStep = std::is_same_v<Args, AttendArgs>;
+  constexpr bool kPrompt = std::is_same_v<Args, PromptArgs>;
+  constexpr bool kPrefix = std::is_same_v<Args, PrefixArgs>;
   constexpr int KT = kF32Keys, RW = 32 * NW;
   constexpr int QL = D / 2;             // query dims per lane
   constexpr int DBLK = D / 32;          // 32-wide output blocks
@@ -66,23 +74,57 @@ __global__ void __launch_bounds__(64 * NW, 1) attend_f32_kernel(AttendArgs a) {
   __shared__ int32_t sidx[kF32Sel];
 
   const int G = a.n_q_heads / a.n_kv_heads;
-  const int R = G * a.geom.n_q;
-  const int n_row_tiles = (R + RW - 1) / RW;
-  const int L = (int)gridDim.x - 1 - xcd_logical_block(blockIdx.x, gridDim.x);
-  const int rt = L % n_row_tiles;
-  const int tmp = L / n_row_tiles;
-  const int part = tmp % a.parts;
-  const int bg = tmp / a.parts;
-  const int b = bg / a.n_kv_heads, g = bg - b * a.n_kv_heads;
-  // this sequence's step (its own past length in a variable-length batch)
-  const SeqStep sq = seq_step(a, b);
+  int R, rt, part, bg, b, g, parts = 1;
+  SeqStep sq;
+  int64_t seq_start = 0;  // first token of a packed prompt
+  PrefixWork pw = {};
+  if constexpr (kStep) {
+    R = G * a.geom.n_q;
+    const int n_row_tiles = (R + RW - 1) / RW;
+    const int L = (int)gridDim.x - 1 - xcd_logical_block(blockIdx.x, gridDim.x);
+    rt = L % n_row_tiles;
+    const int tmp = L / n_row_tiles;
+    part = tmp % a.parts;
+    bg = tmp / a.parts;
+    b = bg / a.n_kv_heads;
+    g = bg - b * a.n_kv_heads;
+    // this sequence's step (its own past length in a variable-length batch)
+    sq = seq_step(a, b);
+    parts = a.parts;
+  } else if constexpr (kPrompt) {
+    const int t = div_by(blockIdx.x, a.d_kv);
+    static_assert(RW == 32 || RW == 64 || RW == 128, "row tiles of a power of two");
+    const PromptTile pt = prompt_tile(a, t, NW == 4 ? 7 : NW == 2 ? 6 : 5);
+    g = bg = (int)blockIdx.x - t * (int)a.d_kv.d;
+    b = part = 0;
+    rt = pt.tile;
+    R = G * pt.len;
+    seq_start = pt.start;
+    sq.geom = StepGeom{};
+    sq.geom.block_size = 8;
+    sq.geom.n_q = sq.geom.n_virtual = pt.len;
+    sq.mem_len = sq.parts_mem = 0;
+  } else {
+    pw = prefix_work(a, blockIdx.x);
+    g = pw.g;
+    b = pw.b;
+    bg = b * a.n_kv_heads + g;
+    part = pw.part;
+    rt = pw.tile;
+    parts = pw.region == 0 ? a.parts_s : pw.region == 1 ? a.parts_u : a.parts_o;
+    R = G * a.n_q * (pw.region == 0 ? a.batch : 1);
+    sq.geom = prefix_geom(a, pw);
+    sq.mem_len = sq.parts_mem = 0;
+  }
   const StepGeom& geo = sq.geom;
   const int mem_len = sq.mem_len;
 
   // the tiles the row tile's queries see, split evenly over the parts
   const int v_x0 = geo.n_virtual - geo.n_q;
-  const int n_tiles = (v_x0 + (min(R, (rt + 1) * RW) - 1) / G) / KT + 1;
-  const int t_begin = (int)((int64_t)n_tiles * part / a.parts), t_end = (int)((int64_t)n_tiles * (part + 1) / a.parts);
+  // (every row sees every key of the prefix attention's first two regions)
+  const bool no_causal = kPrefix && pw.region != 2;
+  const int n_tiles = no_causal ? (geo.n_virtual + KT - 1) / KT : (v_x0 + (min(R, (rt + 1) * RW) - 1) / G) / KT + 1;
+  const int t_begin = (int)((int64_t)n_tiles * part / parts), t_end = (int)((int64_t)n_tiles * (part + 1) / parts);
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -92,18 +134,45 @@ __global__ void __launch_bounds__(64 * NW, 1) attend_f32_kernel(AttendArgs a) {
   const bool active = rt * RW + wave * 32 < R;  // whether the wave has rows at all
   const int qi = row_ok ? row / G : 0;
   const int qh = g * G + (row_ok ? row - qi * G : 0);
-  const int vlim = v_x0 + qi;  // last visible key
-  const int32_t* idx_row = a.idx + (int64_t)bg * geo.idx_stride;
-  const float* kbase = (const float*)a.k_store + (int64_t)bg * a.capacity * D;
-  const float* vbase = (const float*)a.v_store + (int64_t)bg * a.capacity * D;
-  const float* krot = ROPE ? (const float*)a.k_rot + (int64_t)bg * a.capacity * D : nullptr;
+  const int vlim = no_causal ? geo.n_virtual - 1 : v_x0 + qi;  // last visible key
+  const int32_t* idx_row = nullptr;
+  const float *kbase, *vbase, *krot = nullptr;
+  int64_t key_step = D;  // elements from one key's row to the next
+  if constexpr (kStep) {
+    idx_row = a.idx + (int64_t)bg * geo.idx_stride;
+    kbase = (const float*)a.k_store + (int64_t)bg * a.capacity * D;
+    vbase = (const float*)a.v_store + (int64_t)bg * a.capacity * D;
+    if (ROPE) krot = (const float*)a.k_rot + (int64_t)bg * a.capacity * D;
+  } else if constexpr (kPrompt) {
+    const int64_t at = seq_start * a.kv_tok + g * a.kv_head;
+    kbase = (const float*)a.k + at;
+    vbase = (const float*)a.v + at;
+    key_step = a.kv_tok;
+  } else {
+    idx_row = a.idx + (int64_t)bg * geo.idx_stride;
+    const int64_t at = (pw.region == 2 ? bg * a.own_capacity : g * a.prefix_capacity) * D;
+    kbase = (const float*)(pw.region == 2 ? a.own_k : a.prefix_k) + at;
+    vbase = (const float*)(pw.region == 2 ? a.own_v : a.prefix_v) + at;
+  }
+  // The sequence and position of the lane's query (in the shared region of the prefix
+  // attention qi counts the queries of all continuations).
+  int qb = b, qj = qi;
+  if constexpr (kPrefix) {
+    if (pw.region == 0) {
+      qb = div_by(qi, a.d_q);
+      qj = qi - qb * a.n_q;
+    }
+  }
 
-  for (int u = tid; u < min(geo.n_sel, kF32Sel); u += 64 * NW) sidx[u] = idx_row[u];
+  if constexpr (!kPrompt)
+    for (int u = tid; u < min(geo.n_sel, kF32Sel); u += 64 * NW) sidx[u] = idx_row[u];
 
   // Query pieces: qv as given; under the remap qv is the query at its own position
   // (L and X) and qm the query turned by R(l_L) (I and the units, keys unrotated).
   float qv[QL], qm[ROPE ? QL : 1];
-  const float* qp = (const float*)a.q + (int64_t)(b * a.n_q_heads + qh) * a.q_head_stride + (int64_t)qi * D;
+  const float* qp = (const float*)a.q;
+  if constexpr (kPrompt) qp += (seq_start + qi) * a.q_tok + qh * a.q_head;
+  else qp += (int64_t)(qb * a.n_q_heads + qh) * a.q_head_stride + (int64_t)qj * D;
 #pragma unroll
   for (int i = 0; i < QL / 4; ++i) {
     const f32x4 x = row_ok ? *(const f32x4*)(qp + 8 * i + 4 * gsel) : f32x4{0.f, 0.f, 0.f, 0.f};
@@ -156,7 +225,7 @@ __global__ void __launch_bounds__(64 * NW, 1) attend_f32_kernel(AttendArgs a) {
     for (int j = 0; j < NI; ++j) {
       const int r = (NI * wave + j) * RPI + lane / GPR;
       const int gran = (lane % GPR) ^ (r & 15);
-      const int64_t off = spos[slot][r] * D + 4 * gran;
+      const int64_t off = spos[slot][r] * key_step + 4 * gran;
       const float* kp = ROPE && t * KT + r >= mem_len ? krot : kbase;
       lds_load_lane(lds_k + buf + j * 1024, kp + off);
       lds_load_lane(lds_v + buf + j * 1024, vbase + off);
@@ -308,12 +377,34 @@ __global__ void __launch_bounds__(64 * NW, 1) attend_f32_kernel(AttendArgs a) {
   const auto lw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
   const float l_tot = __uint_as_float(lw[0]) + __uint_as_float(lw[1]);
   if (!row_ok) return;
-  const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-  const float lse_v = l_tot > 0.f ? m + logf(l_tot) : -__builtin_inff();
-  const int64_t grow = (int64_t)(b * a.n_q_heads + qh) * geo.n_q + qi;
-  const int64_t rows_total = (int64_t)a.batch * a.n_q_heads * geo.n_q;
-  float* op = a.parts == 1 ? (float*)a.out + (int64_t)(b * a.n_q_heads + qh) * a.out_head_stride + (int64_t)qi * D
-                           : (float*)a.part_o + ((int64_t)part * rows_total + grow) * D;
+  float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+  float lse_v = l_tot > 0.f ? m + logf(l_tot) : -__builtin_inff();
+  int64_t grow = 0, rows_total = 0;
+  float* op;
+  int n_parts = 1;
+  if constexpr (kStep) {
+    grow = (int64_t)(b * a.n_q_heads + qh) * geo.n_q + qi;
+    rows_total = (int64_t)a.batch * a.n_q_heads * geo.n_q;
+    n_parts = a.parts;
+    op = n_parts == 1 ? (float*)a.out + (int64_t)(b * a.n_q_heads + qh) * a.out_head_stride + (int64_t)qi * D
+                      : (float*)a.part_o + ((int64_t)part * rows_total + grow) * D;
+  } else if constexpr (kPrompt) {
+    grow = qh * a.lse_stride + seq_start + qi;
+    op = (float*)a.out + (seq_start + qi) * a.out_tok + qh * a.out_head;
+  } else {
+    grow = (int64_t)(qb * a.n_q_heads + qh) * a.n_q + qj;
+    rows_total = (int64_t)a.batch * a.n_q_heads * a.n_q;
+    n_parts = a.parts;
+    part += prefix_first_part(a, pw.region);
+    op = n_parts == 1 ? (float*)a.out + (int64_t)(qb * a.n_q_heads + qh) * a.out_head_stride + (int64_t)qj * D
+                      : (float*)a.part_o + ((int64_t)part * rows_total + grow) * D;
+  }
+  if constexpr (!kStep) {
+    if (l_tot != l_tot) {  // a NaN among the row's scores is the row's, through the merge as well
+      inv = l_tot;
+      lse_v = n_parts == 1 ? l_tot : __builtin_inff();
+    }
+  }
   typedef float orow_t __attribute__((ext_vector_type(DBLK)));
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
@@ -323,8 +414,10 @@ __global__ void __launch_bounds__(64 * NW, 1) attend_f32_kernel(AttendArgs a) {
     *(orow_t*)(op + DBLK * (8 * (j >> 2) + 4 * gsel + (j & 3))) = w;
   }
   if (gsel == 0) {
-    if (a.parts > 1) a.part_lse[(int64_t)part * rows_total + grow] = lse_v;
-    else if (a.lse != nullptr) a.lse[grow] = lse_v;
+    if constexpr (!kPrompt) {
+      if (n_parts > 1) a.part_lse[(int64_t)part * rows_total + grow] = lse_v;
+    }
+    if (n_parts == 1 && a.lse != nullptr) a.lse[grow] = lse_v;
   }
 }
 
@@ -343,6 +436,15 @@ void launch_f32_d(const AttendArgs& a, hipStream_t s) {
   if (nw == 4) launch_f32<D, 4>(a, blocks, s);
   else if (nw == 2) launch_f32<D, 2>(a, blocks, s);
   else launch_f32<D, 1>(a, blocks, s);
+}
+
+template <int D, int NW>
+void launch_prompt_f32(const PromptArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((attend_f32_kernel<D, NW, false, PromptArgs>), dim3(a.n_tiles * a.n_kv_heads), dim3(64 * NW), 0, s, a);
+}
+template <int D, int NW>
+void launch_prefix_f32(const PrefixArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((attend_f32_kernel<D, NW, false, PrefixArgs>), dim3(prefix_workgroups(a)), dim3(64 * NW), 0, s, a);
 }
 
 bool decode_eligible(bool bf16, int n_q, int G, int n_sel) {
@@ -465,6 +567,29 @@ int attend_select_max(const AttendArgs& a) {
   if (a.geom.n_q == 0 || !decode_eligible(a.bf16, a.geom.n_q, G, a.geom.n_sel)) return -1;
   // (of a row of at most n_sel units every unit is looked up, and nothing is selected)
   return a.geom.n_sel <= kWaveSelMaxK ? kDecodeSelMax : a.geom.n_sel;
+}
+
+hipError_t launch_prompt(const PromptArgs& a, hipStream_t s) {
+  if (a.n_tiles == 0) return hipSuccess;
+  if (a.bf16) return launch_prompt_mfma(a, s);
+  const bool wide = a.head_dim == 128;
+  switch (a.row_waves) {
+    case 4: wide ? launch_prompt_f32<128, 4>(a, s) : launch_prompt_f32<64, 4>(a, s); break;
+    case 2: wide ? launch_prompt_f32<128, 2>(a, s) : launch_prompt_f32<64, 2>(a, s); break;
+    default: wide ? launch_prompt_f32<128, 1>(a, s) : launch_prompt_f32<64, 1>(a, s); break;
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_prefix(const PrefixArgs& a, hipStream_t s) {
+  if (a.bf16) return launch_prefix_mfma(a, s);
+  const bool wide = a.head_dim == 128;
+  switch (a.row_waves) {
+    case 4: wide ? launch_prefix_f32<128, 4>(a, s) : launch_prefix_f32<64, 4>(a, s); break;
+    case 2: wide ? launch_prefix_f32<128, 2>(a, s) : launch_prefix_f32<64, 2>(a, s); break;
+    default: wide ? launch_prefix_f32<128, 1>(a, s) : launch_prefix_f32<64, 1>(a, s); break;
+  }
+  return hipGetLastError();
 }
 
 hipError_t launch_attend(const AttendArgs& a, hipStream_t s) {

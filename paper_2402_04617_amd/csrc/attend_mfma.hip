@@ -19,6 +19,8 @@
 //                  A = V^T fragments read from the key-major V tile with the LDS
 //                  transpose read (ds_read_b64_tr_b16), in the key order the
 //                  accumulator layout gives P^T.
+#include <type_traits>
+
 #include "launch.h"
 #include "topk_select.h"
 
@@ -117,8 +119,14 @@ __device__ __forceinline__ void publish_barrier() {
 // the tile's sum of P = exp2(S*c2 - m) and the running max m it was formed
 // against, from which the attention mass of each unit follows once the final
 // lse is known (mass_parts_kernel).
-template <int D, int SEL, bool MASS>
-__global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a) {
+// Args: a step's arguments, or those of another job that the same tile loop does:
+// packed prompts (PromptArgs: a row tile of one sequence, its keys one run of strided
+// rows) or one region of the prefix attention (PrefixArgs).
+template <int D, int SEL, bool MASS, typename Args = AttendArgs>
+__global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
+  constexpr bool kStep = std::is_same_v<Args, AttendArgs>;
+  constexpr bool kPrompt = std::is_same_v<Args, PromptArgs>;
+  constexpr bool kPrefix = std::is_same_v<Args, PrefixArgs>;
   constexpr int CH = D / 8;                   // 16-byte granules per row
   constexpr int KSTEPS = D / 16;              // MFMA k-steps over the head dim
   constexpr int DBLK = D / 32;                // 32-wide output blocks
@@ -135,27 +143,62 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
   // and that read waits for every load in flight.
   // Every argument the prologue reads, requested at once: read where they are used,
   // their cold cache lines were waited for one after another.
-  asm volatile("" ::"s"(a.batch), "s"(a.capacity), "s"(a.q_head_stride), "s"(a.q), "s"(a.k_store), "s"(a.v_store),
-               "s"(a.parts), "s"(a.row_waves), "s"(a.n_q_heads), "s"(a.n_kv_heads));
-  asm volatile("" ::"s"(a.geom.n_init), "s"(a.geom.n_units), "s"(a.geom.n_sel), "s"(a.geom.block_size),
-               "s"(a.geom.unit_base), "s"(a.geom.idx_stride), "s"(a.geom.local_begin), "s"(a.geom.past_len),
-               "s"(a.geom.n_q), "s"(a.geom.n_virtual));
-  asm volatile("" ::"s"(a.mem_len), "s"(a.parts_mem), "s"(a.rope.on), "s"(a.var.on), "s"(a.d_row_tiles.mul),
-               "s"(a.d_parts.mul), "s"(a.d_kv.mul), "s"(a.d_group.mul), "s"(a.d_block.mul), "s"(a.sel_scores),
-               "s"(a.sel_stride));
+  if constexpr (kStep) {
+    asm volatile("" ::"s"(a.batch), "s"(a.capacity), "s"(a.q_head_stride), "s"(a.q), "s"(a.k_store), "s"(a.v_store),
+                 "s"(a.parts), "s"(a.row_waves), "s"(a.n_q_heads), "s"(a.n_kv_heads));
+    asm volatile("" ::"s"(a.geom.n_init), "s"(a.geom.n_units), "s"(a.geom.n_sel), "s"(a.geom.block_size),
+                 "s"(a.geom.unit_base), "s"(a.geom.idx_stride), "s"(a.geom.local_begin), "s"(a.geom.past_len),
+                 "s"(a.geom.n_q), "s"(a.geom.n_virtual));
+    asm volatile("" ::"s"(a.mem_len), "s"(a.parts_mem), "s"(a.rope.on), "s"(a.var.on), "s"(a.d_row_tiles.mul),
+                 "s"(a.d_parts.mul), "s"(a.d_kv.mul), "s"(a.d_group.mul), "s"(a.d_block.mul), "s"(a.sel_scores),
+                 "s"(a.sel_stride));
+  }
   const int G = (int)a.d_group.d;
-  const int R = G * a.geom.n_q;
-  const int n_row_tiles = (int)a.d_row_tiles.d;
+  int R, rt, bg, part, b, g;
+  SeqStep sq;
+  int64_t seq_start = 0;  // first token of a packed prompt
+  PrefixWork pw = {};
+  if constexpr (kStep) {
+    R = G * a.geom.n_q;
+    const int n_row_tiles = (int)a.d_row_tiles.d;
+    // XCD-aware order, reversed so that the workgroups dispatched first are those
+    // with the most work: the last key part (it holds the causal diagonal of X) and
+    // the last row tiles (their queries see the most of X)
+    const int L = (int)gridDim.x - 1 - xcd_logical_block(blockIdx.x, gridDim.x);
+    const int tmp = div_by(L, a.d_row_tiles);
+    rt = L - tmp * n_row_tiles;
+    bg = div_by(tmp, a.d_parts);
+    part = tmp - bg * a.parts;
+    b = div_by(bg, a.d_kv);
+    g = bg - b * a.n_kv_heads;
+    // this sequence's step (its own past length in a variable-length batch)
+    sq = seq_step(a, b);
+  } else if constexpr (kPrompt) {
+    // the kv heads side by side (8 of them: one per XCD, whose L2 then holds its keys),
+    // the row tiles by falling work
+    const int t = div_by(blockIdx.x, a.d_kv);
+    const PromptTile pt = prompt_tile(a, t, a.row_waves == NWAVE ? 8 : 7);
+    g = bg = (int)blockIdx.x - t * (int)a.d_kv.d;
+    b = part = 0;
+    rt = pt.tile;
+    R = G * pt.len;
+    seq_start = pt.start;
+    sq.geom = StepGeom{};
+    sq.geom.block_size = 8;
+    sq.geom.n_q = sq.geom.n_virtual = pt.len;
+    sq.mem_len = sq.parts_mem = 0;
+  } else {
+    pw = prefix_work(a, blockIdx.x);
+    g = pw.g;
+    b = pw.b;
+    bg = b * (int)a.d_kv.d + g;
+    part = pw.part;
+    rt = pw.tile;
+    R = G * a.n_q * (pw.region == 0 ? a.batch : 1);
+    sq.geom = prefix_geom(a, pw);
+    sq.mem_len = sq.parts_mem = 0;
+  }
   const int rows_wg = 32 * a.row_waves;
-  // XCD-aware order, reversed so that the workgroups dispatched first are those
-  // with the most work: the last key part (it holds the causal diagonal of X) and
-  // the last row tiles (their queries see the most of X)
-  const int L = (int)gridDim.x - 1 - xcd_logical_block(blockIdx.x, gridDim.x);
-  const int tmp = div_by(L, a.d_row_tiles), rt = L - tmp * n_row_tiles;
-  const int bg = div_by(tmp, a.d_parts), part = tmp - bg * a.parts;
-  const int b = div_by(bg, a.d_kv), g = bg - b * a.n_kv_heads;
-  // this sequence's step (its own past length in a variable-length batch)
-  const SeqStep sq = seq_step(a, b);
   const StepGeom& geo = sq.geom;
   const int mem_len = sq.mem_len, parts_mem = sq.parts_mem;
 
@@ -166,17 +209,26 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
   // rotated keys, queries at their own positions); a tile holding keys of both
   // kinds is taken by both sides, each masking the other's keys.
   const int n_tiles = (geo.n_virtual + KB - 1) / KB;
-  const bool remap = a.rope.on != 0;
-  const bool mem_part = part < parts_mem;
-  int rt0 = 0, rt1 = n_tiles, rpart = part, rparts = a.parts;
-  if (mem_part) {
-    rt1 = (mem_len + KB - 1) / KB;
-    rparts = parts_mem;
-  } else if (parts_mem > 0) {
-    rt0 = mem_len / KB;
-    rpart = part - parts_mem;
-    rparts = a.parts - parts_mem;
+  bool remap = false, mem_part = false;
+  int rt0 = 0, rt1 = n_tiles, rpart = part, rparts = 1;
+  if constexpr (kStep) {
+    remap = a.rope.on != 0;
+    mem_part = part < parts_mem;
+    rparts = a.parts;
+    if (mem_part) {
+      rt1 = (mem_len + KB - 1) / KB;
+      rparts = parts_mem;
+    } else if (parts_mem > 0) {
+      rt0 = mem_len / KB;
+      rpart = part - parts_mem;
+      rparts = a.parts - parts_mem;
+    }
+  } else if constexpr (kPrefix) {
+    rparts = pw.region == 0 ? a.parts_s : pw.region == 1 ? a.parts_u : a.parts_o;
   }
+  // whether every row sees every key of the part's region
+  const bool no_causal = kPrefix ? pw.region != 2 : mem_part;
+  const int region_keys = kPrefix ? geo.n_virtual : mem_len;
   // The parts split the tiles this row tile's queries see by cost rather than by
   // count, so that they end together: a masked tile (the causal diagonal) costs
   // kMaskCost plain tiles, and with the selection inside (SEL) the parts that
@@ -186,7 +238,7 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
   const int v_x0 = geo.n_virtual - geo.n_q;  // first current-token key
   const int qi_min = div_by(min(R - 1, rt * rows_wg), a.d_group);
   const int qi_max = div_by(min(R, (rt + 1) * rows_wg) - 1, a.d_group);
-  const int vis_end = mem_part ? mem_len : v_x0 + qi_min + 1;  // every row of the tile sees the keys below
+  const int vis_end = no_causal ? region_keys : v_x0 + qi_min + 1;  // every row of the tile sees the keys below
   rt1 = min(rt1, (v_x0 + qi_max) / KB + 1);                    // later tiles are fully causal-masked
   const int a_m = min(max(vis_end / KB, rt0), rt1);            // first masked tile
   int s_end = rt0;                                             // end of the tiles charged the selection
@@ -227,12 +279,36 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
   const int qi = row_ok ? div_by(row, a.d_group) : 0;
   // last virtual key this row may see: causal within X (which also excludes the
   // ragged end), or for a memory part of the remap the last memory key
-  const int vlim = mem_part ? mem_len - 1 : v_x0 + qi;
+  const int vlim = no_causal ? region_keys - 1 : v_x0 + qi;
   const int qh = g * G + (row_ok ? row - qi * G : 0);
 
-  const int32_t* idx_row = a.idx + (int64_t)bg * geo.idx_stride;
-  const bf16_t* kbase = (const bf16_t*)(remap && !mem_part ? a.k_rot : a.k_store) + (int64_t)bg * a.capacity * D;
-  const bf16_t* vbase = (const bf16_t*)a.v_store + (int64_t)bg * a.capacity * D;
+  const int32_t* idx_row = nullptr;
+  const bf16_t *kbase, *vbase;
+  if constexpr (kStep) {
+    idx_row = a.idx + (int64_t)bg * geo.idx_stride;
+    kbase = (const bf16_t*)(remap && !mem_part ? a.k_rot : a.k_store) + (int64_t)bg * a.capacity * D;
+    vbase = (const bf16_t*)a.v_store + (int64_t)bg * a.capacity * D;
+  } else if constexpr (kPrompt) {
+    const int64_t at = seq_start * a.kv_tok + g * a.kv_head;
+    kbase = (const bf16_t*)a.k + at;
+    vbase = (const bf16_t*)a.v + at;
+  } else {
+    idx_row = a.idx + (int64_t)bg * geo.idx_stride;
+    const int64_t at = (pw.region == 2 ? bg * a.own_capacity : g * a.prefix_capacity) * D;
+    kbase = (const bf16_t*)(pw.region == 2 ? a.own_k : a.prefix_k) + at;
+    vbase = (const bf16_t*)(pw.region == 2 ? a.own_v : a.prefix_v) + at;
+  }
+  // First element of query row i of head h (of the group); in the shared region of the
+  // prefix attention i counts the queries of all continuations.
+  auto query_at = [&](int i, int h) -> int64_t {
+    if constexpr (kPrompt) return (seq_start + i) * a.q_tok + (g * G + h) * a.q_head;
+    else if constexpr (kPrefix) {
+      const int c = pw.region == 0 ? div_by(i, a.d_q) : b;
+      const int j = pw.region == 0 ? i - c * a.n_q : i;
+      return (int64_t)(c * a.n_q_heads + g * G + h) * a.q_head_stride + (int64_t)j * D;
+    }
+    return 0;
+  };
 
   // Whether a tile this workgroup loads (its own and those issued ahead, [t_begin,
   // t_end + 7)) may hold unit keys; only then does it need the lookup.
@@ -248,7 +324,8 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
   const bool sel_all = geo.n_sel == 0 || geo.n_sel == geo.n_units;  // every unit (or none) is looked up
   // by single waves, or by the radix select of all of them
   const bool sel_waves = SEL > 2 ? tk::long_select_fits<tk::kWavePer>(geo.n_units, geo.n_sel) : geo.n_sel <= tk::kWaveK;
-  const float* srow = SEL > 0 ? a.sel_scores + (int64_t)bg * a.sel_stride : nullptr;
+  const float* srow = nullptr;
+  if constexpr (SEL > 0) srow = a.sel_scores + (int64_t)bg * a.sel_stride;
   // scores of the single-wave select: short rows in the first wave, 16 per lane; long
   // rows 16 per lane of every wave (loaded before the queries, whose latency overlaps)
   constexpr int WPER = tk::kWavePer;
@@ -289,8 +366,12 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
   if (active && t_begin < t_end) {
     // within the kv head's query rows 32-bit byte offsets do, unless the heads lie
     // very far apart
-    const bf16_t* qg = (const bf16_t*)a.q + (int64_t)(b * a.n_q_heads + g * G) * a.q_head_stride;
-    const bool near = (int64_t)G * a.q_head_stride < (1ll << 30);
+    const bf16_t* qg = (const bf16_t*)a.q;
+    bool near = false;
+    if constexpr (kStep) {
+      qg += (int64_t)(b * a.n_q_heads + g * G) * a.q_head_stride;
+      near = (int64_t)G * a.q_head_stride < (1ll << 30);
+    }
     int i = li0, h = lh0;
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
@@ -298,7 +379,9 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
       const bool in = row0 + rr < R;
       const int ii = in ? i : 0, hh = in ? h : 0;
       const int gran = (lane % CH) ^ swz<D>(rr);
-      if (near) {
+      if constexpr (!kStep) {
+        lds_load_lane(lds_q + j * 1024, qg + query_at(ii, hh) + 8 * gran);
+      } else if (near) {
         lds_load(lds_q + j * 1024, qg, 2u * ((uint32_t)hh * (uint32_t)a.q_head_stride + (uint32_t)ii * D + 8u * gran));
       } else {
         lds_load_lane(lds_q + j * 1024, qg + hh * a.q_head_stride + (int64_t)ii * D + 8 * gran);
@@ -309,7 +392,7 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
   // The lane's rotary table entries under the remap (granule lane % CH, four pairs)
   double rev[4];
   float mcos[4], msin[4];
-  if (remap) {
+  if constexpr (kStep) if (remap) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       rev[j] = a.rope.rev[4 * (lane % CH) + j];
@@ -319,7 +402,7 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
   }
 
   bool has_invalid = false;
-  if constexpr (SEL == 0) {
+  if constexpr (SEL == 0 && !kPrompt) {
     // The lookup row goes to LDS; skipped (out-of-range) entries send every tile
     // through the validity mask.
     if (units_here) {
@@ -331,7 +414,7 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
       }
       has_invalid = __syncthreads_or(bad) != 0;
     }
-  } else if (sel_here) {
+  } else if constexpr (SEL > 0) if (sel_here) {
     // (the select's scratch lies in the position table, filled after it)
     static_assert(sizeof(tk::LongSelSmem) <= sizeof(sm.rows) && sizeof(tk::WaveSelSmem) <= sizeof(sm.rows), "scratch");
     bool done = sel_all, published = false;
@@ -397,9 +480,13 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
   // it (a ragged end, a tile past the axis) reads that row instead, which the
   // causal bound masks.
   const uint32_t last_row = (uint32_t)(geo.past_len + geo.n_q - 1);
+  uint32_t row_bytes = 2u * D;  // from one key's row to the next
+  if constexpr (kPrompt) row_bytes = 2u * (uint32_t)a.kv_tok;
   auto group_row = [&](int v) -> uint32_t {
     int64_t pos = v;
-    if (v >= geo.n_init) {
+    if constexpr (kPrompt) {
+      return min((uint32_t)v, last_row);
+    } else if (v >= geo.n_init) {
       const int w = v - geo.n_init;
       const int sel_len = geo.n_sel * geo.block_size;
       if (w >= sel_len) {
@@ -431,6 +518,10 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
   auto row_read = [&](int tile, uint32_t (&e)[NI]) {
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
+      if constexpr (kPrompt) {  // the keys are one run: no table
+        e[j] = (uint32_t)(tile * KB + ((lrow0 + RPI * j) & ~(int)gr_mask));
+        continue;
+      }
       const uint32_t at = lds_rows + 4u * ((uint32_t)(lrow0 + RPI * j) >> gshift);
       e[j] = *(const INFLLM_LDS uint32_t*)(uintptr_t)(at + 4u * (uint32_t)((tile - w0) * tile_groups));
     }
@@ -441,7 +532,8 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
       const uint32_t r = (uint32_t)(lrow0 + RPI * j);
       const uint32_t gran = (uint32_t)(lane % CH) ^ (uint32_t)swz<D>(lrow0 + RPI * j);
       const uint32_t base = has_invalid && e[j] == kNoRow ? 0u : e[j];
-      f.o[j] = (min(base + (r & gr_mask), last_row) * (2u * D)) | (16u * gran);
+      if constexpr (kPrompt) f.o[j] = min(base + (r & gr_mask), last_row) * row_bytes + 16u * gran;
+      else f.o[j] = (min(base + (r & gr_mask), last_row) * (2u * D)) | (16u * gran);
     }
   };
 
@@ -645,13 +737,14 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
   // the running max it was formed against.  Later rescales of l_run leave the
   // stored pair valid: it carries its own max.
   auto mass_tile = [&](int t, float half_sum) {
+    if constexpr (!MASS) return;
     const int ut = t - geo.n_init / KB;  // tile index within the units
     const int n_ut = geo.n_sel * (geo.block_size / KB);
     if (ut < 0 || ut >= n_ut) return;
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(half_sum), __float_as_uint(half_sum), false,
                                                       false);
     const float tsum = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    if (row_ok && gsel == 0)
+    if constexpr (MASS) if (row_ok && gsel == 0)
       a.mass_part[((int64_t)bg * a.mass_tiles + ut) * R + row] = make_float2(tsum, m_run);
   };
   // Two P values as a bf16 pair (one v_cvt_pk_bf16_f32), added unrounded to the
@@ -880,7 +973,7 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
       note_valid((t - t_begin + 3) % NBUF, e3);
       note_valid((t - t_begin) % NBUF, e4);
     }
-    if (t + 6 >= w0 + window) {
+    if constexpr (!kPrompt) if (t + 6 >= w0 + window) {
       // the second step reads the table for tiles t+5, t+6: move the window there
       // (its readers are past the barrier)
       fill_rows(t + 5);
@@ -911,8 +1004,10 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
     }
 #pragma unroll
     for (int j = 0; j < NI; ++j) load_k(0, off0, j);
-    fill_rows(t_begin);
-    lds_barrier();
+    if constexpr (!kPrompt) {
+      fill_rows(t_begin);
+      lds_barrier();
+    }
     {
       uint32_t e1[NI], e2[NI];
       row_read(t_begin + 1, e1);
@@ -1009,11 +1104,18 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
   // are free once every wave has passed the barrier below) so that each store
   // moves 16 contiguous bytes and a wave's store covers four whole rows.
   const float l_tot = l_run + __shfl_xor(l_run, 32);
-  const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-  const float lse_v = (m_run == -__builtin_inff() || l_tot <= 0.f)
+  float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+  float lse_v = (m_run == -__builtin_inff() || l_tot <= 0.f)
                           ? -__builtin_inff()
                           : (m_run + __log2f(l_tot)) * 0.6931471805599453f;
-  const bool one_part = a.parts == 1;
+  bool one_part = true;
+  if constexpr (!kPrompt) one_part = a.parts == 1;
+  if constexpr (!kStep) {
+    if (l_tot != l_tot) {  // a NaN among the row's scores is the row's, through the merge as well
+      inv = l_tot;
+      lse_v = one_part ? l_tot : __builtin_inff();
+    }
+  }
   float sc = inv;
   int ex = 0;
   if (!one_part) {
@@ -1053,7 +1155,107 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
       }
     }
   }
-  if (row_ok && gsel == 0) {
+  // Values that are not finite must not reach rows that do not see their key: in a masked
+  // tile such a value meets P = 0 and leaves a NaN.  A row that came out so is formed again
+  // by the wave from the keys it sees, 64 at a time, against its maximum (the scores'
+  // sums are right: masked scores never enter them).  Costs the others 64 multiply-adds.
+  if constexpr (!kStep) {
+    float z = 0.f;
+#pragma unroll
+    for (int db = 0; db < DBLK; ++db)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) z = __builtin_fmaf(oacc[db][j], 0.f, z);
+    const uint64_t odd = __ballot(row_ok && !(z == 0.f) && l_tot == l_tot);
+    uint32_t rows = (uint32_t)odd | (uint32_t)(odd >> 32);
+    if (__builtin_expect(rows != 0, 0)) {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+      __builtin_amdgcn_wave_barrier();
+      constexpr int DPL = D / 64;  // dims of a lane
+      INFLLM_LDS char* stage = (INFLLM_LDS char*)(INFLLM_LDS bf16_t*)sm.k[0] + wave * 32 * kStageRow;
+      for (; rows != 0; rows &= rows - 1) {
+        const int r = __builtin_ctz(rows);
+        const int i = div_by(row0 + r, a.d_group);
+        const u32x4* qp = (const u32x4*)((const bf16_t*)a.q + query_at(i, row0 + r - i * G));
+        const float m_r = __shfl(m_run, r), nm = m_r == -__builtin_inff() ? 0.f : -m_r, inv_r = __shfl(inv, r);
+        const int v_end = min(t_end * KB, __shfl(vlim, r) + 1);
+        float acc[DPL] = {};
+        for (int v0 = t_begin * KB; v0 < v_end; v0 += 64) {
+          const uint32_t pos = v0 + lane < v_end ? group_row(v0 + lane) : kNoRow;
+          float p = 0.f;
+          if (pos != kNoRow) {
+            const u32x4* kp = (const u32x4*)((const char*)kbase + (uint64_t)pos * row_bytes);
+            float s = 0.f;
+#pragma unroll 4
+            for (int c = 0; c < CH; ++c) {
+              const u32x4 kw = kp[c], qw = qp[c];
+#pragma unroll
+              for (int w = 0; w < 4; ++w) {
+                s = __builtin_fmaf(__uint_as_float(kw[w] << 16), __uint_as_float(qw[w] << 16), s);
+                s = __builtin_fmaf(__uint_as_float(kw[w] & 0xFFFF0000u), __uint_as_float(qw[w] & 0xFFFF0000u), s);
+              }
+            }
+            p = fast_exp2(__builtin_fmaf(s, c2, nm));
+          }
+          for (int j = 0; j < min(64, v_end - v0); ++j) {
+            const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)pos, j);
+            if (at == kNoRow) continue;
+            const float pj = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(p), j));
+            const bf16_t* vp = (const bf16_t*)((const char*)vbase + (uint64_t)at * row_bytes) + DPL * lane;
+#pragma unroll
+            for (int e = 0; e < DPL; ++e) acc[e] = __builtin_fmaf(pj, bf16_to_f32(vp[e]), acc[e]);
+          }
+        }
+        float amax = 0.f;  // (of the finite ones, which keep their precision)
+#pragma unroll
+        for (int e = 0; e < DPL; ++e) {
+          acc[e] *= inv_r;
+          const float x = fabsf(acc[e]);
+          amax = x < __builtin_inff() ? fmaxf(amax, x) : amax;
+        }
+        const int ex_r = one_part ? 0 : partial_row_exponent(wave_max(amax));
+        if (n == r) ex = ex_r;
+        const float back = exp2_int(-ex_r);
+#pragma unroll
+        for (int e = 0; e < DPL; ++e) {
+          const uint32_t w = one_part ? f32_to_bf16(acc[e]) : pack_f16x2(acc[e] * back, 0.f) & 0xFFFFu;
+          *(INFLLM_LDS uint16_t*)(stage + r * kStageRow + 2 * (DPL * lane + e)) = (uint16_t)w;
+        }
+      }
+    }
+  }
+  // Row of the partial arrays, and address, of query i of head h: see query_at.
+  int part_id = part;
+  if constexpr (kPrefix) part_id += prefix_first_part(a, pw.region);
+  auto partial_row = [&](int i, int h) -> int64_t {
+    if constexpr (kPrefix) {
+      const int c = pw.region == 0 ? div_by(i, a.d_q) : b;
+      const int64_t rows_total = (int64_t)a.batch * a.n_q_heads * a.n_q;
+      return part_id * rows_total + (int64_t)(c * a.n_q_heads + g * G + h) * a.n_q + (pw.region == 0 ? i - c * a.n_q : i);
+    }
+    return 0;
+  };
+  auto out_row = [&](int i, int h) -> char* {
+    if constexpr (kPrompt) return (char*)a.out + ((seq_start + i) * a.out_tok + (g * G + h) * a.out_head) * 2;
+    if constexpr (kPrefix) {
+      if (!one_part) return (char*)a.part_o + partial_row(i, h) * kRowBytes;
+      const int c = pw.region == 0 ? div_by(i, a.d_q) : b;
+      return (char*)a.out + ((int64_t)(c * a.n_q_heads + g * G + h) * a.out_head_stride + (int64_t)(pw.region == 0 ? i - c * a.n_q : i) * D) * 2;
+    }
+    return nullptr;
+  };
+  if constexpr (kPrompt) {
+    if (row_ok && gsel == 0 && a.lse != nullptr) a.lse[qh * a.lse_stride + seq_start + qi] = lse_v;
+  } else if constexpr (kPrefix) {
+    if (row_ok && gsel == 0) {
+      const int64_t at = partial_row(qi, qh - g * G);
+      if (!one_part) {
+        a.part_lse[at] = lse_v;
+        a.part_exp[at] = ex;
+      } else if (a.lse != nullptr) {
+        a.lse[at] = lse_v;
+      }
+    }
+  } else if (row_ok && gsel == 0) {
     const int64_t grow = ((int64_t)(b * a.n_q_heads + qh)) * geo.n_q + qi;
     if (one_part) {
       if (a.lse != nullptr) a.lse[grow] = lse_v;
@@ -1071,23 +1273,44 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(AttendArgs a
     const INFLLM_LDS char* stage = (const INFLLM_LDS char*)(const INFLLM_LDS bf16_t*)sm.k[0] + wave * 32 * kStageRow;
     static_assert(CPR == CH, "a lane stores the rows it loaded");
     // first row of the kv head's group: [G][n_q] rows of a partial, or of the output
-    const int64_t rows_total = (int64_t)a.batch * a.n_q_heads * geo.n_q;
-    const int64_t head0 = b * a.n_q_heads + g * G;
-    char* base = one_part ? (char*)a.out + head0 * a.out_head_stride * 2
-                          : (char*)a.part_o + ((int64_t)part * rows_total + head0 * geo.n_q) * kRowBytes;
-    const int64_t hstride = one_part ? a.out_head_stride * 2 : (int64_t)geo.n_q * kRowBytes;
+    char* base = nullptr;
+    int64_t hstride = 0;
+    if constexpr (kStep) {
+      const int64_t rows_total = (int64_t)a.batch * a.n_q_heads * geo.n_q;
+      const int64_t head0 = b * a.n_q_heads + g * G;
+      base = one_part ? (char*)a.out + head0 * a.out_head_stride * 2
+                      : (char*)a.part_o + ((int64_t)part * rows_total + head0 * geo.n_q) * kRowBytes;
+      hstride = one_part ? a.out_head_stride * 2 : (int64_t)geo.n_q * kRowBytes;
+    }
     int i = li0, h = lh0;
 #pragma unroll
     for (int k = 0; k < 32 * CPR / 64; ++k) {
       const int r = RPI * k + lane / CH, ch = lane % CH;
       const u32x4 w = *(const INFLLM_LDS u32x4*)(stage + r * kStageRow + ch * 16);
-      if (active && row0 + r < R) *(u32x4*)(base + h * hstride + (int64_t)i * kRowBytes + ch * 16) = w;
+      if (active && row0 + r < R) {
+        if constexpr (kStep) *(u32x4*)(base + h * hstride + (int64_t)i * kRowBytes + ch * 16) = w;
+        else *(u32x4*)(out_row(i, h) + ch * 16) = w;
+      }
       next_row(i, h);
     }
   }
 }
 
 }  // namespace
+
+hipError_t launch_prompt_mfma(const PromptArgs& a, hipStream_t s) {
+  const dim3 grid(a.n_tiles * a.n_kv_heads), block(64 * NWAVE);
+  if (a.head_dim == 128) hipLaunchKernelGGL((attend_mfma_kernel<128, 0, false, PromptArgs>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((attend_mfma_kernel<64, 0, false, PromptArgs>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_prefix_mfma(const PrefixArgs& a, hipStream_t s) {
+  const dim3 grid(prefix_workgroups(a)), block(64 * NWAVE);
+  if (a.head_dim == 128) hipLaunchKernelGGL((attend_mfma_kernel<128, 0, false, PrefixArgs>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((attend_mfma_kernel<64, 0, false, PrefixArgs>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
 
 hipError_t launch_attend_mfma(const AttendArgs& args, hipStream_t s) {
   AttendArgs a = args;

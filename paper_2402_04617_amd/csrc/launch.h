@@ -217,6 +217,181 @@ struct AttendArgs {
   FastDiv d_row_tiles, d_parts, d_kv, d_group, d_block;
   bool bf16;
 };
+// Packed prompts: whole causal self-attention of sequences that lie one after another.
+// Row (token t, head h) of a tensor starts at t * its token stride + h * its head
+// stride elements.  The sequences are listed by falling length, empty ones left out.
+// A row tile is a run of rows (query-major, the group's heads packed) of one sequence;
+// tiles are numbered from the last row tile of the longest sequence down, level by
+// level: the tiles that many sequences have at one level lie side by side, so that
+// tile numbers fall by the keys a tile sees.  first[i] is the number of the first tile
+// of the levels that exactly the i + 1 longest sequences reach.
+constexpr int kMaxPrompts = 256;  // of one launch
+struct PromptArgs {
+  int n_seqs, n_q_heads, n_kv_heads, head_dim;
+  int64_t q_tok, q_head, kv_tok, kv_head, out_tok, out_head;
+  int64_t lse_stride;  // tokens of the whole call
+  float sm_scale;
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;
+  float* lse;  // nullable, [n_q_heads][lse_stride]
+  int row_waves;  // waves of a workgroup that hold query rows, 32 each
+  int n_tiles;
+  FastDiv d_group, d_kv;
+  bool bf16;
+  int32_t start[kMaxPrompts];
+  int32_t len[kMaxPrompts];
+  int32_t first[kMaxPrompts];
+};
+struct PromptTile {
+  int start, len;  // the sequence
+  int tile;        // row tile of it
+};
+// Row tile number t (uniform over the wave).
+__device__ __forceinline__ PromptTile prompt_tile(const PromptArgs& a, int t, int rows_log2) {
+  int i = 1;
+  if (a.n_seqs > 1) {
+    i = 0;
+    const int lane = threadIdx.x & 63;
+    for (int j = 0; j < a.n_seqs; j += kWave)
+      i += __popcll(__ballot(j + lane < a.n_seqs && a.first[j + lane < kMaxPrompts ? j + lane : 0] <= t));
+    i = __builtin_amdgcn_readfirstlane(i);
+  }
+  const int u = t - a.first[i - 1], down = u / i, s = u - down * i;
+  const int rows = a.len[i - 1] * (int)a.d_group.d;
+  return PromptTile{a.start[s], a.len[s], ((rows - 1) >> rows_log2) - down};
+}
+hipError_t launch_prompt(const PromptArgs& a, hipStream_t s);
+
+// Attention of continuations over a document they share.  Three regions of keys, each
+// with parts of its own:
+//   shared: I and L of the document, met by the rows of all continuations together;
+//   units : the looked-up units of one continuation (document store);
+//   own   : the tokens of one continuation, X at their end (its own store, causal).
+struct PrefixArgs {
+  int batch, n_q_heads, n_kv_heads, head_dim, n_q;
+  int64_t prefix_capacity, own_capacity, q_head_stride, out_head_stride;
+  float sm_scale;
+  const void* q;
+  const void* prefix_k;
+  const void* prefix_v;
+  const void* own_k;
+  const void* own_v;
+  const int32_t* idx;  // [batch][n_kv_heads][idx_stride]
+  int n_init, n_units, n_sel, block_size, unit_base, idx_stride;
+  int64_t local_begin, prefix_len;
+  int parts_s, parts_u, parts_o;  // of the regions; parts = their sum
+  int parts;
+  int row_waves;                  // waves of a workgroup that hold query rows (matrix-core kernel)
+  int tiles_s, tiles_p;           // row tiles of the shared region and of one continuation
+  FastDiv d_group, d_block, d_kv, d_q, d_tiles_s, d_tiles_p, d_parts_u, d_parts_o;
+  void* out;
+  float* lse;
+  void* part_o;
+  float* part_lse;
+  int32_t* part_exp;
+  bool bf16;
+  int64_t own_len[kMaxVarBatch];
+};
+// Where a workgroup of the prefix attention works.
+struct PrefixWork {
+  int region;  // 0 shared, 1 units, 2 own
+  int g, b;    // b: the continuation (0 in the shared region)
+  int tile;    // row tile
+  int part;    // of the region's parts
+};
+__device__ __forceinline__ PrefixWork prefix_work(const PrefixArgs& a, int id) {
+  PrefixWork w;
+  int r = div_by(id, a.d_kv);
+  w.g = id - r * (int)a.d_kv.d;
+  const int n_shared = a.tiles_s * a.parts_s, n_units = a.batch * a.tiles_p * a.parts_u;
+  if (r < n_shared) {
+    w.region = 0;
+    w.b = 0;
+    w.part = div_by(r, a.d_tiles_s);
+    w.tile = r - w.part * a.tiles_s;
+    return w;
+  }
+  r -= n_shared;
+  w.region = r < n_units ? 1 : 2;
+  r -= w.region == 1 ? 0 : n_units;
+  const int c = div_by(r, a.d_tiles_p);
+  w.tile = r - c * a.tiles_p;
+  w.b = w.region == 1 ? div_by(c, a.d_parts_u) : div_by(c, a.d_parts_o);
+  w.part = c - w.b * (w.region == 1 ? a.parts_u : a.parts_o);
+  return w;
+}
+// The keys of a region as a step's key axis: every row sees all of the shared and the
+// units region (n_q = 0 there).
+__device__ __forceinline__ StepGeom prefix_geom(const PrefixArgs& a, const PrefixWork& w) {
+  StepGeom g;
+  g.n_units = a.n_units;
+  g.unit_base = a.unit_base;
+  g.idx_stride = a.idx_stride;
+  g.block_size = w.region == 1 ? a.block_size : 8;
+  g.n_init = w.region == 0 ? a.n_init : 0;
+  g.n_sel = w.region == 1 ? a.n_sel : 0;
+  g.local_begin = w.region == 0 ? a.local_begin : 0;
+  g.n_q = w.region == 2 ? a.n_q : 0;
+  g.past_len = w.region == 2 ? a.own_len[w.b] : a.prefix_len;
+  g.n_virtual = w.region == 1   ? a.n_sel * a.block_size
+                : w.region == 0 ? (int32_t)(a.n_init + (a.prefix_len - a.local_begin))
+                                : (int32_t)g.past_len + a.n_q;
+  return g;
+}
+// First part of a region among all parts, and the workgroups of the launch.
+__host__ __device__ inline int prefix_first_part(const PrefixArgs& a, int region) {
+  return region == 0 ? 0 : a.parts_s + (region == 1 ? 0 : a.parts_u);
+}
+__host__ inline int prefix_workgroups(const PrefixArgs& a) {
+  return a.n_kv_heads * (a.tiles_s * a.parts_s + a.batch * a.tiles_p * (a.parts_u + a.parts_o));
+}
+hipError_t launch_prefix(const PrefixArgs& a, hipStream_t s);
+
+// Copies of whole sequences between memories: the pairs are sorted by source, so that a
+// source's bytes are read once for all its copies.
+struct SeqCopyArgs {
+  int n_pairs, n_sources, n_kv_heads, row_bytes;  // row_bytes: of a K or V row
+  int64_t src_capacity, dst_capacity;
+  int src_units, dst_units, src_ring, dst_ring;
+  int repr_bytes;  // of a unit's representatives (0: none are kept)
+  int cells;       // 16-byte cells of a unit's key sum (head_dim / 4)
+  int ring_rows;   // rpart rows (head_dim / 8), 0 without rings
+  const char* src_k;
+  const char* src_v;
+  const char* src_rot;
+  const char* src_repr;
+  const char* src_ksum;
+  const char* src_qprefix;
+  const char* src_rpart;
+  char* dst_k;
+  char* dst_v;
+  char* dst_rot;
+  char* dst_repr;
+  char* dst_ksum;
+  char* dst_qprefix;
+  char* dst_rpart;
+  int32_t pair_begin[kMaxVarBatch + 1];  // of a source
+  int32_t block_begin[kMaxVarBatch + 1];
+  int32_t src_seq[kMaxVarBatch];         // of a source
+  int32_t dst_seq[kMaxVarBatch];         // of a pair
+  int32_t built[kMaxVarBatch];
+  int64_t len[kMaxVarBatch];
+};
+hipError_t launch_copy_sequences(const SeqCopyArgs& a, hipStream_t s);
+
+struct PrefixScoreArgs {
+  int batch, n_q_heads, n_kv_heads, head_dim, n_q, n_units, max_units;
+  int64_t q_head_stride;
+  const void* q;
+  const float* unit_ksum;
+  float* scores;      // [batch][n_kv_heads][n_units]
+  float* qbar_parts;  // workspace: score_qbar_parts per (sequence, kv head)
+  bool bf16;
+};
+hipError_t launch_prefix_score(const PrefixScoreArgs& a, hipStream_t s);
+
 struct ThinScoreArgs {
   const float* unit_ksum;
   float* scores;

@@ -64,10 +64,13 @@ __device__ __forceinline__ void join_parts(const MergeArgs& a, int row, int c, i
     }
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
-      const float w = (p0 + j * step < a.parts && l[j] != -__builtin_inff()) ? expf(l[j] - m_new) : 0.f;
+      const bool live = p0 + j * step < a.parts && l[j] != -__builtin_inff();
+      const float w = live ? expf(l[j] - m_new) : 0.f;
       tot += w;
+      // (no product with 0: a value that is not finite would leave a NaN, and the piece of
+      // a thread past the last part is that part's again)
 #pragma unroll
-      for (int e = 0; e < DPT; ++e) acc[e] += w * o[j][e];
+      for (int e = 0; e < DPT; ++e) acc[e] += live ? w * o[j][e] : 0.f;
     }
     M = m_new;
     if (ONCE) break;
@@ -89,7 +92,8 @@ __device__ __forceinline__ void store_piece(const MergeArgs& a, int row, int c, 
 #pragma unroll
     for (int e = 0; e < DPT; ++e) op[e] = acc[e] * inv;
   }
-  if (a.lse != nullptr && c == 0) a.lse[row] = tot > 0.f ? M + logf(tot) : -__builtin_inff();
+  // (tot is NaN where a part's scores hold a NaN: such a part comes with lse = +inf)
+  if (a.lse != nullptr && c == 0) a.lse[row] = tot > 0.f ? M + logf(tot) : tot != tot ? tot : -__builtin_inff();
 }
 
 template <typename T, bool HALF, int CH>

@@ -100,6 +100,52 @@ __global__ void __launch_bounds__(256) score_kernel(const ScoreArgs a, int parts
         ((part[0][lane] + part[1][lane]) + part[2][lane]) + part[3][lane];
 }
 
+// Relevance of one memory's units to every continuation of it.  A block holds the key
+// sums of 64 units in registers (split over its four waves as in score_kernel), which are
+// so read once, and takes the continuations kPrefixSeqs at a time: their query sums
+// through LDS, the four waves' partial products joined there in a fixed order.
+constexpr int kPrefixSeqs = 8;
+template <int D>
+__global__ void __launch_bounds__(256) prefix_score_kernel(const PrefixScoreArgs a, int parts) {
+  constexpr int NC = D / 4, CPW = NC / 4;
+  const int g = blockIdx.y;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int u = blockIdx.x * kScoreUnits + lane;
+  const bool live = u < a.n_units;
+  const float4* ks = (const float4*)a.unit_ksum + (int64_t)g * NC * a.max_units + (live ? u : 0);
+  float4 k4[CPW];
+#pragma unroll
+  for (int c = 0; c < CPW; ++c) k4[c] = ks[(int64_t)(w * CPW + c) * a.max_units];
+  __shared__ __attribute__((aligned(16))) float qbar[kPrefixSeqs][D];
+  __shared__ float part[kPrefixSeqs][4][kScoreUnits];
+  for (int b0 = 0; b0 < a.batch; b0 += kPrefixSeqs) {
+    const int nb = min(kPrefixSeqs, a.batch - b0);
+    for (int i = threadIdx.x; i < nb * D; i += 256) {
+      const float* qp = a.qbar_parts + (int64_t)((b0 + i / D) * a.n_kv_heads + g) * parts * D + i % D;
+      float s = 0.f;
+      for (int p = 0; p < parts; ++p) s += qp[p * D];
+      qbar[i / D][i % D] = s;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPrefixSeqs; ++j) {
+      if (j >= nb) break;
+      float acc = 0.f;
+#pragma unroll
+      for (int c = 0; c < CPW; ++c) {
+        const float4 q4 = *(const float4*)&qbar[j][4 * (w * CPW + c)];
+        acc += q4.x * k4[c].x + q4.y * k4[c].y + q4.z * k4[c].z + q4.w * k4[c].w;
+      }
+      part[j][w][lane] = acc;
+    }
+    __syncthreads();
+    for (int j = w; j < nb; j += 4)
+      if (live)
+        a.scores[((int64_t)(b0 + j) * a.n_kv_heads + g) * a.n_units + u] =
+            ((part[j][0][lane] + part[j][1][lane]) + part[j][2][lane]) + part[j][3][lane];
+  }
+}
+
 }  // namespace
 
 int score_qbar_parts(int G, int n_q) {
@@ -120,6 +166,21 @@ hipError_t launch_score(const ScoreArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(qbar_kernel<float>, g1, dim3(kQsumThreads), 0, s, (const float*)a.q, a.q_head_stride,
                        a.n_q_heads, a.n_kv_heads, a.head_dim, a.n_q, parts, a.qbar_parts);
   return launch_score_given_qbar(a, parts, s);
+}
+
+hipError_t launch_prefix_score(const PrefixScoreArgs& a, hipStream_t s) {
+  const int parts = score_qbar_parts(a.n_q_heads / a.n_kv_heads, a.n_q);
+  const dim3 g1(parts, a.batch * a.n_kv_heads);
+  if (a.bf16)
+    hipLaunchKernelGGL(qbar_kernel<bf16_t>, g1, dim3(kQsumThreads), 0, s, (const bf16_t*)a.q, a.q_head_stride,
+                       a.n_q_heads, a.n_kv_heads, a.head_dim, a.n_q, parts, a.qbar_parts);
+  else
+    hipLaunchKernelGGL(qbar_kernel<float>, g1, dim3(kQsumThreads), 0, s, (const float*)a.q, a.q_head_stride,
+                       a.n_q_heads, a.n_kv_heads, a.head_dim, a.n_q, parts, a.qbar_parts);
+  const dim3 g2((a.n_units + kScoreUnits - 1) / kScoreUnits, a.n_kv_heads);
+  if (a.head_dim == 128) hipLaunchKernelGGL(prefix_score_kernel<128>, g2, dim3(256), 0, s, a, parts);
+  else hipLaunchKernelGGL(prefix_score_kernel<64>, g2, dim3(256), 0, s, a, parts);
+  return hipGetLastError();
 }
 
 hipError_t launch_score_given_qbar(const ScoreArgs& a, int parts, hipStream_t s) {

@@ -26,7 +26,9 @@ STATUS = {0: "INFLLM_OK", 1: "INFLLM_E_NULL", 2: "INFLLM_E_SHAPE", 3: "INFLLM_E_
 EXPORTS = ["infllm_partition", "infllm_workspace_bytes", "infllm_attend_workspace_bytes", "infllm_append", "infllm_build_units",
            "infllm_score_units", "infllm_select_topk", "infllm_chunk_attend", "infllm_chunk_attend_noalloc",
            "infllm_attend_partial",
-           "infllm_lse_merge", "infllm_step", "infllm_step_mass", "infllm_step_varlen", "infllm_unit_mass",
+           "infllm_lse_merge", "infllm_prompt_workspace_bytes", "infllm_prompt_attend",
+           "infllm_prefix_workspace_bytes", "infllm_prefix_score", "infllm_prefix_attend", "infllm_copy_sequences",
+           "infllm_step", "infllm_step_mass", "infllm_step_varlen", "infllm_unit_mass",
            "infllm_status_string"]
 
 
@@ -92,6 +94,13 @@ def lib() -> ctypes.CDLL:
         "infllm_step_varlen": [P, M, vp, i64, vp, vp, i64, i32, ctypes.POINTER(i64), ctypes.POINTER(i32), vp, vp,
                                vp, i64, vp, vp, sz, vp],
         "infllm_unit_mass": [P, M, vp, i64, i32, i64, vp, i32, vp, ctypes.c_float, vp, vp, vp],
+        "infllm_prompt_attend": [P, i32, ctypes.POINTER(i32), vp, i64, i64, vp, vp, i64, i64, vp, i64, i64, vp, vp, sz,
+                                 vp],
+        "infllm_prefix_score": [P, M, i32, vp, i64, i32, i32, vp, vp, sz, vp],
+        "infllm_prefix_attend": [P, M, i64, M, ctypes.POINTER(i64), vp, i64, vp, vp, i64, i32, vp, i32, vp, i64, vp, vp,
+                                 sz, vp],
+        "infllm_copy_sequences": [P, M, M, i32, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(i64),
+                                  ctypes.POINTER(i32), vp],
     }
     for name, args in sig.items():
         f = getattr(L, name)
@@ -101,6 +110,10 @@ def lib() -> ctypes.CDLL:
     L.infllm_workspace_bytes.restype = ctypes.c_size_t
     L.infllm_attend_workspace_bytes.argtypes = [P, i32, i32]
     L.infllm_attend_workspace_bytes.restype = ctypes.c_size_t
+    L.infllm_prompt_workspace_bytes.argtypes = [P, i32, ctypes.POINTER(i32)]
+    L.infllm_prompt_workspace_bytes.restype = ctypes.c_size_t
+    L.infllm_prefix_workspace_bytes.argtypes = [P, i32, i32, i64, i64]
+    L.infllm_prefix_workspace_bytes.restype = ctypes.c_size_t
     L.infllm_status_string.argtypes = [ctypes.c_int]
     L.infllm_status_string.restype = ctypes.c_char_p
     _lib = L
@@ -234,6 +247,65 @@ def infllm_step_varlen(p, m, q, q_head_stride, k, v, kv_head_stride, n_q, past_l
     _check("infllm_step_varlen", lib().infllm_step_varlen(
         ctypes.byref(p), ctypes.byref(m), _ptr(q), q_head_stride, _ptr(k), _ptr(v), kv_head_stride, n_q, pl, ub,
         _ptr(scores), _ptr(idx), _ptr(out), out_head_stride, _ptr(lse), _ptr(workspace), wb, _stream(stream)))
+
+
+def _i32s(xs):
+    return (ctypes.c_int32 * len(xs))(*xs)
+
+
+def _i64s(xs):
+    return (ctypes.c_int64 * len(xs))(*xs)
+
+
+def _wb(workspace, workspace_bytes) -> int:
+    if workspace_bytes is not None:
+        return workspace_bytes
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def infllm_prompt_workspace_bytes(p: Params, seq_lens) -> int:
+    return int(lib().infllm_prompt_workspace_bytes(ctypes.byref(p), len(seq_lens), _i32s(seq_lens)))
+
+
+def infllm_prompt_attend(p, seq_lens, q, q_strides, k, v, kv_strides, out, out_strides, lse=None, workspace=None,
+                         workspace_bytes=None, stream=None):
+    """seq_lens: lengths (host ints); strides: (token, head) in elements."""
+    _check("infllm_prompt_attend", lib().infllm_prompt_attend(
+        ctypes.byref(p), len(seq_lens), _i32s(seq_lens), _ptr(q), q_strides[0], q_strides[1], _ptr(k), _ptr(v),
+        kv_strides[0], kv_strides[1], _ptr(out), out_strides[0], out_strides[1], _ptr(lse), _ptr(workspace),
+        _wb(workspace, workspace_bytes), _stream(stream)))
+
+
+def infllm_prefix_workspace_bytes(p: Params, batch: int, n_q: int, prefix_len: int, own_capacity: int) -> int:
+    return int(lib().infllm_prefix_workspace_bytes(ctypes.byref(p), batch, n_q, prefix_len, own_capacity))
+
+
+def infllm_prefix_score(p, prefix, batch, q, q_head_stride, n_q, n_units, scores, workspace, workspace_bytes=None,
+                        stream=None):
+    _check("infllm_prefix_score", lib().infllm_prefix_score(
+        ctypes.byref(p), ctypes.byref(prefix), batch, _ptr(q), q_head_stride, n_q, n_units, _ptr(scores),
+        _ptr(workspace), _wb(workspace, workspace_bytes), _stream(stream)))
+
+
+def infllm_prefix_attend(p, prefix, prefix_len, own, own_lens, q, q_head_stride, k, v, kv_head_stride, n_q, idx, n_idx,
+                         out, out_head_stride, lse=None, workspace=None, workspace_bytes=None, stream=None):
+    """own_lens: own.batch host ints."""
+    if len(own_lens) != own.batch:
+        raise ValueError(f"own_lens needs {own.batch} entries, got {len(own_lens)}")
+    _check("infllm_prefix_attend", lib().infllm_prefix_attend(
+        ctypes.byref(p), ctypes.byref(prefix), prefix_len, ctypes.byref(own), _i64s(own_lens), _ptr(q), q_head_stride,
+        _ptr(k), _ptr(v), kv_head_stride, n_q, _ptr(idx), n_idx, _ptr(out), out_head_stride, _ptr(lse),
+        _ptr(workspace), _wb(workspace, workspace_bytes), _stream(stream)))
+
+
+def infllm_copy_sequences(p, dst, src, dst_seq, src_seq, lens, units_built, stream=None):
+    """dst_seq, src_seq, lens, units_built: host ints, one of each per copy."""
+    n = len(dst_seq)
+    if not n == len(src_seq) == len(lens) == len(units_built):
+        raise ValueError("one destination, source, length and unit count per copy")
+    _check("infllm_copy_sequences", lib().infllm_copy_sequences(
+        ctypes.byref(p), ctypes.byref(dst), ctypes.byref(src), n, _i32s(dst_seq), _i32s(src_seq), _i64s(lens),
+        _i32s(units_built), _stream(stream)))
 
 
 # ------------------------------------------------------------------ allocation plumbing
