@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 
 #include "abi_util.h"
@@ -22,11 +23,153 @@ infllm_status check_strided(const infllm_params* p, const void* ptr, int64_t tok
   return INFLLM_OK;
 }
 
-// Waves of 32 query rows of a workgroup of the prompt attention.  bf16: 8, or 4 where 8
-// leave compute units without a workgroup; float32: as the rows of the longest sequence fill.
-int prompt_row_waves(bool bf16, int64_t rows8, int64_t longest_rows) {
-  if (bf16) return rows8 < kMfmaTargetWgs ? kMfmaWaves / 2 : kMfmaWaves;
-  return longest_rows > 64 ? 4 : longest_rows > 32 ? 2 : 1;
+int key_tile(bool bf16) { return bf16 ? 64 : 32; }
+
+// Workgroups that run at a time: the bf16 kernel's by their LDS, the float32 kernel's by
+// their registers.
+int resident_wgs(const infllm_params* p, int row_waves) {
+  if (p->dtype == INFLLM_BF16) return row_waves == kMfmaWaves ? kMfmaTargetWgs : 2 * kMfmaTargetWgs;
+  return kMfmaTargetWgs * 4 / row_waves * (p->head_dim == 64 && row_waves > 1 ? 2 : 1);
+}
+
+// Lengths of all sequences; false where they are not valid.
+struct PromptSizes {
+  int64_t total, longest;
+};
+bool prompt_sizes(int32_t n_seqs, const int32_t* lens, PromptSizes* r) {
+  r->total = r->longest = 0;
+  for (int i = 0; i < n_seqs; ++i) {
+    if (lens[i] < 0) return false;
+    r->total += lens[i];
+    r->longest = std::max<int64_t>(r->longest, lens[i]);
+  }
+  return true;
+}
+
+// Microseconds of a workgroup of the attention kernels, for each tile of keys and beside
+// them (prologue, epilogue): with the whole chip at work, and of one that runs longer than
+// the others (alone on its compute unit, at a higher clock).
+struct ItemCost {
+  float tile, item, lone_tile, lone_item;
+};
+ItemCost item_cost(const infllm_params* p, int row_waves) {
+  const bool wide = p->head_dim == 128;
+  if (p->dtype == INFLLM_BF16) {
+    if (row_waves == kMfmaWaves) return wide ? ItemCost{1.72f, 10.f, 1.4f, 8.2f} : ItemCost{1.02f, 9.f, 0.87f, 7.5f};
+    return wide ? ItemCost{1.76f, 9.f, 0.95f, 6.5f} : ItemCost{0.96f, 8.5f, 0.72f, 5.5f};
+  }
+  return wide ? ItemCost{6.6f, 12.f, 6.6f, 12.f} : row_waves > 1 ? ItemCost{6.2f, 10.f, 4.2f, 8.f} : ItemCost{3.7f, 8.f, 3.7f, 8.f};
+}
+constexpr float kMergeCost = 9.f;          // microseconds of a merge's launch
+constexpr float kPartialByteCost = 2.5e-7f;  // of a byte of a partial row, written and read
+
+// The sequences of the next launch, from lens[*i] on (first token *at): the shape fields,
+// tile numbers and key parts of `a`.  False when none is left.
+bool prompt_next(const infllm_params* p, int32_t n_seqs, const int32_t* lens, int* i, int64_t* at,
+                 PromptArgs* a) {
+  const int64_t G = p->n_q_heads / p->n_kv_heads;
+  const bool bf16 = p->dtype == INFLLM_BF16;
+  int n = 0;
+  int32_t start[kMaxPrompts], len[kMaxPrompts];
+  uint16_t order[kMaxPrompts];
+  for (; *i < n_seqs && n < kMaxPrompts; *at += lens[(*i)++]) {
+    if (lens[*i] == 0) continue;
+    start[n] = (int32_t)*at;
+    len[n] = lens[*i];
+    order[n] = (uint16_t)n;
+    ++n;
+  }
+  if (n == 0) return false;
+  // the longest first, equal ones in their order
+  std::sort(order, order + n, [&](uint16_t x, uint16_t y) { return len[x] != len[y] ? len[x] > len[y] : x < y; });
+  a->n_seqs = n;
+  a->n_kv_heads = p->n_kv_heads;
+  for (int j = 0; j < n; ++j) {
+    a->start[j] = start[order[j]];
+    a->len[j] = len[order[j]];
+  }
+  const int kt = key_tile(bf16);
+  int64_t rows_wg = 0;
+  // Row tiles of sequence j; tiles of keys that a row tile of level R sees at most; the
+  // first level that sees more than x of them; the row tiles of level R and above.
+  auto tiles = [&](int j) { return j < n ? ((int64_t)a->len[j] * G + rows_wg - 1) / rows_wg : 0; };
+  auto keys_of = [&](int64_t R) { return ((R + 1) * rows_wg - 1) / G / kt + 1; };
+  auto level_past = [&](int64_t x) { return x * kt * G / rows_wg; };
+  auto row_tiles_from = [&](int64_t R) {
+    int64_t c = 0;
+    for (int j = 0; j < n && tiles(j) > R; ++j) c += tiles(j) - R;
+    return c;
+  };
+  // The rows of a workgroup and the parts along the keys.  The launch lasts as long as its
+  // work shared over the workgroups that run at a time, or as a part, and where the parts
+  // do not all start at once about half a part more; a split costs the merge.  Measured,
+  // in us (bf16, D = 128): 16,000 tokens of 32 / 8 heads by 8 waves 1,716, by 4 1,757;
+  // 4,000 126 and 132; 2,000 53 and 43; 1,000 28 and 23, in two parts 29 and 29; 16 of 300
+  // 41 and 37; 4,000 of 4 / 1 heads by 4 waves 57, in 3 parts 35, in 8 43; 6,000 of 8 / 8
+  // by 8 waves 130, in 2 parts 90.  Float32, 5 prompts up to 1,600 tokens of 8 / 2 heads
+  // of 64: 174, in 6 parts 72.
+  const int64_t most_rows = (int64_t)a->len[0] * G;
+  const int least_waves = bf16 ? kMfmaWaves / 2 : most_rows > 64 ? 4 : most_rows > 32 ? 2 : 1;
+  const int most_waves = bf16 ? kMfmaWaves : least_waves;
+  float best_cost = -1.f;
+  for (int waves = most_waves; waves >= least_waves; waves /= 2) {
+    rows_wg = 32 * waves;
+    const ItemCost cost = item_cost(p, waves);
+    const float share = (float)p->n_kv_heads / (float)resident_wgs(p, waves);
+    const int64_t longest = std::min(keys_of(tiles(0) - 1), ((int64_t)a->len[0] + kt - 1) / kt);
+    float work = 0.f;  // tiles of keys of all row tiles
+    for (int j = 0; j < n; ++j) work += (float)tiles(j) * (float)(keys_of(0) + keys_of(tiles(j) - 1)) * 0.5f;
+    for (int c = 1; c <= kMaxPromptParts; ++c) {
+      const int64_t T = (longest + c - 1) / c;
+      if (c > 1 && T < 2) break;
+      int64_t items = row_tiles_from(0), full = 0;
+      for (int x = 1; x <= c; ++x) {
+        if (x < c) items += row_tiles_from(level_past(x * T));
+        full += row_tiles_from(level_past(x * T - 1));
+      }
+      const float even = share * (work * cost.tile + (float)items * cost.item);
+      const float part = (float)T * cost.lone_tile + cost.lone_item;
+      float t = std::max(even, part);
+      if (c > 1) {
+        if ((float)items * share > 1.f) t = std::max(even, part + 0.5f * (float)T * cost.tile + cost.item);
+        t += kMergeCost + (float)(full * p->n_kv_heads * rows_wg) * (float)part_row_bytes(p) * kPartialByteCost;
+      }
+      if (best_cost < 0.f || t < best_cost) {
+        best_cost = t;
+        a->row_waves = waves;
+        a->parts = c;
+        a->part_tiles = (int)T;
+      }
+      if (even >= part) break;  // (more parts add nothing but workgroups)
+    }
+  }
+  rows_wg = 32 * a->row_waves;
+  // the levels that exactly the j + 1 longest sequences reach hold j + 1 tiles each
+  a->n_tiles = 0;
+  for (int j = 0; j < n; ++j) {
+    a->first[j] = a->n_tiles;
+    a->n_tiles += (int)((j + 1) * (tiles(j) - tiles(j + 1)));
+  }
+  int counts[kMaxPromptParts], parts = 0;
+  const int64_t T = a->part_tiles;
+  a->items = 0;
+  for (int x = 0; x < a->parts; ++x) {
+    counts[x] = x == 0 ? a->n_tiles : (int)row_tiles_from(level_past(x * T));
+    if (counts[x] == 0) break;
+    a->full[x] = (int)row_tiles_from(level_past((x + 1) * T - 1));
+    a->full_begin[x] = a->items;
+    a->items += a->full[x];
+    parts = x + 1;
+  }
+  a->parts = parts;
+  a->split_tiles = parts > 1 ? counts[1] : 0;
+  a->full_begin[parts] = a->items;
+  for (int x = 0; x < parts; ++x) {
+    a->rest_begin[x] = a->items;
+    a->items += counts[parts - 1 - x] - a->full[parts - 1 - x];
+  }
+  a->rest_begin[parts] = a->items;
+  return true;
 }
 
 }  // namespace
@@ -34,10 +177,16 @@ int prompt_row_waves(bool bf16, int64_t rows8, int64_t longest_rows) {
 extern "C" {
 
 size_t infllm_prompt_workspace_bytes(const infllm_params* p, int32_t n_seqs, const int32_t* seq_lens) {
-  (void)seq_lens;
-  (void)n_seqs;
-  (void)p;
-  return 0;
+  PromptSizes sizes;
+  if (check_params(p) != INFLLM_OK || n_seqs < 0 || (n_seqs > 0 && seq_lens == nullptr) ||
+      !prompt_sizes(n_seqs, seq_lens, &sizes))
+    return 0;
+  PromptArgs a;
+  size_t most = 0;
+  int64_t at = 0;
+  for (int i = 0; prompt_next(p, n_seqs, seq_lens, &i, &at, &a);)
+    most = std::max(most, (size_t)prompt_partial_rows(a) * part_row_bytes(p));
+  return (most + 255) & ~(size_t)255;
 }
 
 infllm_status infllm_prompt_attend(const infllm_params* p, int32_t n_seqs, const int32_t* seq_lens, const void* q,
@@ -45,8 +194,6 @@ infllm_status infllm_prompt_attend(const infllm_params* p, int32_t n_seqs, const
                                    int64_t kv_token_stride, int64_t kv_head_stride, void* out,
                                    int64_t out_token_stride, int64_t out_head_stride, float* lse, void* workspace,
                                    size_t workspace_bytes, void* stream) {
-  (void)workspace;
-  (void)workspace_bytes;
   infllm_status st;
   if ((st = check_params(p)) != INFLLM_OK) return st;
   if (remap(p)) return INFLLM_E_UNSUPPORTED;
@@ -55,15 +202,13 @@ infllm_status infllm_prompt_attend(const infllm_params* p, int32_t n_seqs, const
   if (seq_lens == nullptr) return INFLLM_E_NULL;
   const int G = p->n_q_heads / p->n_kv_heads;
   const bool bf16 = p->dtype == INFLLM_BF16;
-  int64_t total = 0, tiles8 = 0, longest = 0;
-  for (int i = 0; i < n_seqs; ++i) {
-    if (seq_lens[i] < 0) return INFLLM_E_SHAPE;
-    total += seq_lens[i];
-    tiles8 += ((int64_t)seq_lens[i] * G + 32 * kMfmaWaves - 1) / (32 * kMfmaWaves);
-    longest = std::max<int64_t>(longest, seq_lens[i]);
-  }
+  PromptSizes sizes;
+  if (!prompt_sizes(n_seqs, seq_lens, &sizes)) return INFLLM_E_SHAPE;
+  const int64_t total = sizes.total, longest = sizes.longest;
   if (total == 0) return INFLLM_OK;
-  if (total > INT32_MAX || total * G > INT32_MAX || (total * G / 32 + n_seqs) * p->n_kv_heads > INT32_MAX)
+  // (room for every row tile, part and kv head in 32-bit numbers)
+  if (total > INT32_MAX || total * G > INT32_MAX ||
+      (total * G / 32 + n_seqs) * p->n_kv_heads * kMaxPromptParts > INT32_MAX)
     return INFLLM_E_UNSUPPORTED;
   if ((st = check_strided(p, q, q_token_stride, q_head_stride)) != INFLLM_OK) return st;
   if ((st = check_strided(p, k, kv_token_stride, kv_head_stride)) != INFLLM_OK) return st;
@@ -78,10 +223,19 @@ infllm_status infllm_prompt_attend(const infllm_params* p, int32_t n_seqs, const
   if (bf16 && ((uint64_t)kv_token_stride > 0x7FFFFFFFull ||
                (uint64_t)(longest - 1) * (uint64_t)kv_token_stride * 2u + (uint64_t)D * 2u > 0xFFFFFFFFull))
     return INFLLM_E_UNSUPPORTED;
-  if ((st = check_device()) != INFLLM_OK) return st;
-
   PromptArgs a;
   std::memset(&a, 0, sizeof(a));
+  int launches = 0;
+  int64_t at = 0;
+  size_t need = 0;
+  for (int i = 0; prompt_next(p, n_seqs, seq_lens, &i, &at, &a); ++launches)
+    need = std::max(need, (size_t)prompt_partial_rows(a) * part_row_bytes(p));
+  if (need > 0) {
+    if (workspace == nullptr || workspace_bytes < need) return INFLLM_E_WORKSPACE;
+    if (!aligned16(workspace)) return INFLLM_E_SHAPE;
+  }
+  if ((st = check_device()) != INFLLM_OK) return st;
+
   a.n_q_heads = p->n_q_heads;
   a.n_kv_heads = p->n_kv_heads;
   a.head_dim = p->head_dim;
@@ -101,36 +255,13 @@ infllm_status infllm_prompt_attend(const infllm_params* p, int32_t n_seqs, const
   a.bf16 = bf16;
   a.d_group = fast_div(G);
   a.d_kv = fast_div(p->n_kv_heads);
-  a.row_waves = prompt_row_waves(bf16, tiles8 * p->n_kv_heads, longest * G);
-  const int rows_wg = 32 * a.row_waves;
-  int64_t at = 0;
-  for (int i0 = 0; i0 < n_seqs;) {
-    // the next sequences that are not empty, the longest first (equal ones in their order)
-    int n = 0;
-    int32_t start[kMaxPrompts], len[kMaxPrompts];
-    uint16_t order[kMaxPrompts];
-    for (; i0 < n_seqs && n < kMaxPrompts; at += seq_lens[i0++]) {
-      if (seq_lens[i0] == 0) continue;
-      start[n] = (int32_t)at;
-      len[n] = seq_lens[i0];
-      order[n] = (uint16_t)n;
-      ++n;
-    }
-    if (n == 0) break;
-    std::sort(order, order + n, [&](uint16_t x, uint16_t y) { return len[x] != len[y] ? len[x] > len[y] : x < y; });
-    a.n_seqs = n;
-    a.n_tiles = 0;
-    auto tiles = [&](int j) { return (int)(((int64_t)a.len[j] * G + rows_wg - 1) / rows_wg); };
-    for (int j = 0; j < n; ++j) {
-      a.start[j] = start[order[j]];
-      a.len[j] = len[order[j]];
-    }
-    for (int j = 0; j < n; ++j) {
-      // the levels that exactly the j + 1 longest sequences reach hold j + 1 tiles each
-      a.first[j] = a.n_tiles;
-      a.n_tiles += (j + 1) * (tiles(j) - (j + 1 < n ? tiles(j + 1) : 0));
-    }
+  at = 0;
+  // (the shape of a call's only launch is there already)
+  for (int i = 0, l = 0; l < launches && (launches == 1 || prompt_next(p, n_seqs, seq_lens, &i, &at, &a)); ++l) {
+    const int64_t rows = prompt_partial_rows(a);
+    if (rows > 0) partial_layout(p, workspace, 1, rows, &a.part_o, &a.part_lse, &a.part_exp);
     if ((st = launch_status(launch_prompt(a, (hipStream_t)stream))) != INFLLM_OK) return st;
+    if (rows > 0 && (st = launch_status(launch_prompt_merge(a, (hipStream_t)stream))) != INFLLM_OK) return st;
   }
   return INFLLM_OK;
 }
@@ -146,8 +277,6 @@ struct PrefixPlan {
   int parts_s, parts_u, parts_o;
 };
 
-int key_tile(bool bf16) { return bf16 ? 64 : 32; }
-int prefix_target(bool bf16, int row_waves) { return bf16 ? kMfmaTargetWgs : kMfmaTargetWgs * 4 / row_waves; }
 
 // The part counts' bounds follow from the shape alone, so that the workspace does.
 PrefixPlan prefix_shape(const infllm_params* p, int batch, int n_q, int64_t shared_keys, int64_t unit_keys,
@@ -158,7 +287,7 @@ PrefixPlan prefix_shape(const infllm_params* p, int batch, int n_q, int64_t shar
   const int64_t most_rows = shared_keys > 0 ? rows_s : rows_p;
   r.row_waves = bf16 ? (most_rows > 32 * kMfmaWaves / 2 ? kMfmaWaves : kMfmaWaves / 2)
                      : (most_rows > 64 ? 4 : most_rows > 32 ? 2 : 1);
-  const int rows_wg = 32 * r.row_waves, target = prefix_target(bf16, r.row_waves);
+  const int rows_wg = 32 * r.row_waves, target = resident_wgs(p, r.row_waves);
   r.tiles_s = (int)((rows_s + rows_wg - 1) / rows_wg);
   r.tiles_p = (int)((rows_p + rows_wg - 1) / rows_wg);
   auto most = [&](int64_t keys, int64_t wgs) {
@@ -177,7 +306,7 @@ PrefixPlan prefix_shape(const infllm_params* p, int batch, int n_q, int64_t shar
 void prefix_parts(const infllm_params* p, int batch, int64_t shared_keys, int64_t unit_keys, int64_t own_keys,
                   PrefixPlan* r) {
   const bool bf16 = p->dtype == INFLLM_BF16;
-  const int kt = key_tile(bf16), target = prefix_target(bf16, r->row_waves);
+  const int kt = key_tile(bf16), target = resident_wgs(p, r->row_waves);
   const int64_t ts = (shared_keys + kt - 1) / kt, tu = (unit_keys + kt - 1) / kt, to = (own_keys + kt - 1) / kt;
   auto parts = [](int64_t tiles, int64_t T, int most) { return (int)std::min<int64_t>((tiles + T - 1) / T, most); };
   auto wgs = [&](int64_t T) {

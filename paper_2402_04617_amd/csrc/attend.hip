@@ -54,10 +54,14 @@ constexpr int kF32Sel = 2048;  // lookup entries kept in LDS
 // With the positional remap (ROPE) a wave holds both forms of its query rows; a tile
 // of memory keys takes the one at distance l_L, a tile of local keys the other, and
 // the tile that holds both kinds takes both and picks per key.
+// Waves of the kernel on a SIMD.  Prompts and the prefix attention at D = 64 run two, at
+// half the registers (222 to 230): one's softmax overlaps the other's products.
+constexpr int f32_waves_per_simd(int head_dim, int waves, bool step) { return head_dim == 64 && waves > 1 && !step ? 2 : 1; }
 // Args: a step's arguments, packed prompts' (the keys of a row tile are one run of
 // strided rows) or the prefix attention's (one of its regions), without the remap.
 template <int D, int NW, bool ROPE, typename Args = AttendArgs>
-__global__ void __launch_bounds__(64 * NW, 1) attend_f32_kernel(Args a) {
+__global__ void __launch_bounds__(64 * NW, f32_waves_per_simd(D, NW, std::is_same_v<Args, AttendArgs>))
+attend_f32_kernel(Args a) {
   constexpr bool kStep = std::is_same_v<Args, AttendArgs>;
   constexpr bool kPrompt = std::is_same_v<Args, PromptArgs>;
   constexpr bool kPrefix = std::is_same_v<Args, PrefixArgs>;
@@ -77,6 +81,7 @@ __global__ void __launch_bounds__(64 * NW, 1) attend_f32_kernel(Args a) {
   int R, rt, part, bg, b, g, parts = 1;
   SeqStep sq;
   int64_t seq_start = 0;  // first token of a packed prompt
+  int prompt_t = 0;       // number of its row tile
   PrefixWork pw = {};
   if constexpr (kStep) {
     R = G * a.geom.n_q;
@@ -92,11 +97,12 @@ __global__ void __launch_bounds__(64 * NW, 1) attend_f32_kernel(Args a) {
     sq = seq_step(a, b);
     parts = a.parts;
   } else if constexpr (kPrompt) {
-    const int t = div_by(blockIdx.x, a.d_kv);
+    const int item = div_by(blockIdx.x, a.d_kv);
+    prompt_item(a, item, part, prompt_t);
     static_assert(RW == 32 || RW == 64 || RW == 128, "row tiles of a power of two");
-    const PromptTile pt = prompt_tile(a, t, NW == 4 ? 7 : NW == 2 ? 6 : 5);
-    g = bg = (int)blockIdx.x - t * (int)a.d_kv.d;
-    b = part = 0;
+    const PromptTile pt = prompt_tile(a, prompt_t, NW == 4 ? 7 : NW == 2 ? 6 : 5);
+    g = bg = (int)blockIdx.x - item * (int)a.d_kv.d;
+    b = 0;
     rt = pt.tile;
     R = G * pt.len;
     seq_start = pt.start;
@@ -124,7 +130,14 @@ __global__ void __launch_bounds__(64 * NW, 1) attend_f32_kernel(Args a) {
   // (every row sees every key of the prefix attention's first two regions)
   const bool no_causal = kPrefix && pw.region != 2;
   const int n_tiles = no_causal ? (geo.n_virtual + KT - 1) / KT : (v_x0 + (min(R, (rt + 1) * RW) - 1) / G) / KT + 1;
-  const int t_begin = (int)((int64_t)n_tiles * part / parts), t_end = (int)((int64_t)n_tiles * (part + 1) / parts);
+  int t_begin, t_end;
+  if constexpr (kPrompt) {
+    t_begin = min(part * a.part_tiles, n_tiles);
+    t_end = min(t_begin + a.part_tiles, n_tiles);
+  } else {
+    t_begin = (int)((int64_t)n_tiles * part / parts);
+    t_end = (int)((int64_t)n_tiles * (part + 1) / parts);
+  }
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -389,8 +402,15 @@ __global__ void __launch_bounds__(64 * NW, 1) attend_f32_kernel(Args a) {
     op = n_parts == 1 ? (float*)a.out + (int64_t)(b * a.n_q_heads + qh) * a.out_head_stride + (int64_t)qi * D
                       : (float*)a.part_o + ((int64_t)part * rows_total + grow) * D;
   } else if constexpr (kPrompt) {
-    grow = qh * a.lse_stride + seq_start + qi;
-    op = (float*)a.out + (seq_start + qi) * a.out_tok + qh * a.out_head;
+    if (prompt_t < a.split_tiles) {
+      n_parts = a.parts;
+      grow = ((int64_t)prompt_item_of(a, part, prompt_t) * a.n_kv_heads + g) * RW + (row - rt * RW);
+      part = 0;
+      op = (float*)a.part_o + grow * D;
+    } else {
+      grow = qh * a.lse_stride + seq_start + qi;
+      op = (float*)a.out + (seq_start + qi) * a.out_tok + qh * a.out_head;
+    }
   } else {
     grow = (int64_t)(qb * a.n_q_heads + qh) * a.n_q + qj;
     rows_total = (int64_t)a.batch * a.n_q_heads * a.n_q;
@@ -414,10 +434,8 @@ __global__ void __launch_bounds__(64 * NW, 1) attend_f32_kernel(Args a) {
     *(orow_t*)(op + DBLK * (8 * (j >> 2) + 4 * gsel + (j & 3))) = w;
   }
   if (gsel == 0) {
-    if constexpr (!kPrompt) {
-      if (n_parts > 1) a.part_lse[(int64_t)part * rows_total + grow] = lse_v;
-    }
-    if (n_parts == 1 && a.lse != nullptr) a.lse[grow] = lse_v;
+    if (n_parts > 1) a.part_lse[(int64_t)part * rows_total + grow] = lse_v;
+    else if (a.lse != nullptr) a.lse[grow] = lse_v;
   }
 }
 
@@ -440,7 +458,7 @@ void launch_f32_d(const AttendArgs& a, hipStream_t s) {
 
 template <int D, int NW>
 void launch_prompt_f32(const PromptArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((attend_f32_kernel<D, NW, false, PromptArgs>), dim3(a.n_tiles * a.n_kv_heads), dim3(64 * NW), 0, s, a);
+  hipLaunchKernelGGL((attend_f32_kernel<D, NW, false, PromptArgs>), dim3(a.items * a.n_kv_heads), dim3(64 * NW), 0, s, a);
 }
 template <int D, int NW>
 void launch_prefix_f32(const PrefixArgs& a, hipStream_t s) {

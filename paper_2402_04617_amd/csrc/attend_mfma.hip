@@ -28,7 +28,6 @@ namespace infllm {
 namespace {
 
 constexpr int KB = 64;      // keys per tile
-constexpr int NWAVE = kMfmaWaves;
 
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 #define INFLLM_LDS __attribute__((address_space(3)))
@@ -78,7 +77,6 @@ __device__ __forceinline__ int swz(int r) {
 template <int D>
 __device__ __forceinline__ int tile_off(int r, int g) { return r * D + 8 * (g ^ swz<D>(r)); }
 
-constexpr int NBUF = 4;         // K and V tile buffers: a pair of tiles in use, the next pair in flight
 constexpr float kMaskCost = 1.5f;  // cost of a masked tile, in plain tiles
 // The in-prologue unit selection, in plain tiles.  Rows of at most 1,024 units: 0.5, 1, 1.5 and 2
 // tiles make a 128K chunk 90.1, 89.3, 89.2 and 90.2 us, a 389-query chunk at 32K 62.1, 63.1,
@@ -91,11 +89,12 @@ static_assert(kFusedSelectMaxK <= kSelLds, "a selected lookup row fits in LDS");
 
 constexpr uint32_t kNoRow = 0xFFFFFFFFu;
 
-template <int D>
+// NBUF: K and V tile buffers; ROWS: entries of the position table.
+template <int D, int NBUF = 4, int ROWS = kRowTable>
 struct Smem {
   bf16_t k[NBUF][KB * D];
   bf16_t v[NBUF][KB * D];
-  uint32_t rows[kRowTable];  // store position of each key group of a window of tiles (kNoRow: skipped entry)
+  uint32_t rows[ROWS];      // store position of each key group of a window of tiles (kNoRow: skipped entry)
   int32_t sidx[kSelLds];    // the lookup row (its first kSelLds entries)
   int32_t sel_ok;           // whether the first wave's select wrote it
   uint8_t kvalid[NBUF][KB];
@@ -122,8 +121,13 @@ __device__ __forceinline__ void publish_barrier() {
 // Args: a step's arguments, or those of another job that the same tile loop does:
 // packed prompts (PromptArgs: a row tile of one sequence, its keys one run of strided
 // rows) or one region of the prefix attention (PrefixArgs).
-template <int D, int SEL, bool MASS, typename Args = AttendArgs>
-__global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
+// NWAVE: 8 waves, one workgroup per compute unit and a barrier per pair of tiles; or 4,
+// two workgroups per compute unit with two buffers each and a barrier per tile, whose
+// prologues and epilogues run beside the other's loop.
+template <int D, int SEL, bool MASS, typename Args = AttendArgs, int NWAVE = kMfmaWaves>
+__global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) attend_mfma_kernel(Args a) {
+  constexpr bool kPairs = NWAVE == kMfmaWaves;
+  constexpr int NBUF = kPairs ? 4 : 2;  // pairs: two tiles in use, the next two in flight
   constexpr bool kStep = std::is_same_v<Args, AttendArgs>;
   constexpr bool kPrompt = std::is_same_v<Args, PromptArgs>;
   constexpr bool kPrefix = std::is_same_v<Args, PrefixArgs>;
@@ -133,7 +137,9 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
   constexpr int RPI = 64 / CH;                // tile rows per 1 KB load instruction
   constexpr int NI = KB * D * 2 / (NWAVE * 1024);  // load instructions per wave per tile (K or V)
   static_assert(NI * NWAVE * RPI == KB, "tile rows covered exactly once");
-  __shared__ __attribute__((aligned(256))) Smem<D> sm;
+  constexpr int kRows = kPairs ? kRowTable : kPrompt ? 4 : 1024;
+  __shared__ __attribute__((aligned(256))) Smem<D, NBUF, kRows> sm;
+  static_assert(kPairs || sizeof(sm) <= 80 * 1024, "two workgroups share a compute unit's LDS");
 
   // The prologue is latency: 10 us for a selecting workgroup and 6.7 for another of a
   // 128K step's 79, 7.4 and 4.7 since (arguments, divisions and the part bounds
@@ -157,6 +163,7 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
   int R, rt, bg, part, b, g;
   SeqStep sq;
   int64_t seq_start = 0;  // first token of a packed prompt
+  int prompt_t = 0;       // number of its row tile
   PrefixWork pw = {};
   if constexpr (kStep) {
     R = G * a.geom.n_q;
@@ -176,10 +183,11 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
   } else if constexpr (kPrompt) {
     // the kv heads side by side (8 of them: one per XCD, whose L2 then holds its keys),
     // the row tiles by falling work
-    const int t = div_by(blockIdx.x, a.d_kv);
-    const PromptTile pt = prompt_tile(a, t, a.row_waves == NWAVE ? 8 : 7);
-    g = bg = (int)blockIdx.x - t * (int)a.d_kv.d;
-    b = part = 0;
+    const int item = div_by(blockIdx.x, a.d_kv);
+    prompt_item(a, item, part, prompt_t);
+    const PromptTile pt = prompt_tile(a, prompt_t, kPairs ? 8 : 7);
+    g = bg = (int)blockIdx.x - item * (int)a.d_kv.d;
+    b = 0;
     rt = pt.tile;
     R = G * pt.len;
     seq_start = pt.start;
@@ -198,7 +206,8 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
     sq.geom = prefix_geom(a, pw);
     sq.mem_len = sq.parts_mem = 0;
   }
-  const int rows_wg = 32 * a.row_waves;
+  int rows_wg = 32 * NWAVE;
+  if constexpr (kStep) rows_wg = 32 * a.row_waves;
   const StepGeom& geo = sq.geom;
   const int mem_len = sq.mem_len, parts_mem = sq.parts_mem;
 
@@ -261,8 +270,14 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
                                  : a_m + (int)((c - c_plain) * (1.f / kMaskCost) + 0.5f);
     return min(max(t, rt0), rt1);
   };
-  const int t_begin = part_bound(rpart);
-  const int t_end = part_bound(rpart + 1);
+  int t_begin, t_end;
+  if constexpr (kPrompt) {
+    t_begin = min(part * a.part_tiles, rt1);
+    t_end = min(t_begin + a.part_tiles, rt1);
+  } else {
+    t_begin = part_bound(rpart);
+    t_end = part_bound(rpart + 1);
+  }
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -273,7 +288,8 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
   // unused half of a half-filled workgroup) computes nothing: it only loads its rows
   // of the tiles and keeps the barriers, which leaves its SIMD's matrix core and the
   // power budget to the others.
-  const bool active = wave < a.row_waves && row0 < R;
+  bool active = row0 < R;
+  if constexpr (kStep) active = wave < a.row_waves && row0 < R;
   const int row = row0 + n;
   const bool row_ok = active && row < R;
   const int qi = row_ok ? div_by(row, a.d_group) : 0;
@@ -318,7 +334,8 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
   // workgroup of row tile 0 and part 0 always does, and writes the row out (also
   // without units: it is then all -1).  Every entry is valid.
   static_assert(SEL == 0 || SEL == 2 || SEL == tk::kMaxPer, "select variants");
-  static_assert(tk::kThreads == 64 * NWAVE && tk::kMaxPer * tk::kThreads >= kFusedSelectMax, "select layout");
+  static_assert(SEL == 0 || tk::kThreads == 64 * NWAVE);
+  static_assert( tk::kMaxPer * tk::kThreads >= kFusedSelectMax, "select layout");
   const bool sel_writer = SEL > 0 && rt == 0 && part == 0;
   const bool sel_here = SEL > 0 && (sel_writer || units_here);
   const bool sel_all = geo.n_sel == 0 || geo.n_sel == geo.n_units;  // every unit (or none) is looked up
@@ -460,10 +477,9 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
 
   // Direct loads: instruction j of wave w fills LDS granules [(NI*w + j)*64, +64)
   // of the tile, lane l writing granule slot l; that slot belongs to tile row
-  // r_j = r_0 + RPI*j, r_0 = 8*w + l / CH, and holds its global granule
+  // r_j = r_0 + RPI*j, r_0 = KB/NWAVE*w + l / CH, and holds its global granule
   // (l % CH) ^ swz(r_j); a wave's loads cover the eight rows [8w, 8w + 8).
-  static_assert(NI * RPI == 8, "a wave loads eight rows of a tile");
-  const int lrow0 = 8 * wave + lane / CH;
+  const int lrow0 = KB / NWAVE * wave + lane / CH;
 
   // Store positions of the keys.  The virtual axis is cut into groups of 8 keys
   // when no group crosses a boundary between I, the units and the local run
@@ -475,7 +491,7 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
   // between the matrix phases took 870 of an iteration's 3,600 cycles.)
   const int gshift = ((geo.n_init | geo.block_size) & 7) == 0 ? 3 : 0;
   const int tile_groups = KB >> gshift;
-  const int window = kRowTable / tile_groups;  // tiles in the table
+  const int window = kRows / tile_groups;  // tiles in the table
   // The last position of the axis is the store's last written row: an offset past
   // it (a ragged end, a tile past the axis) reads that row instead, which the
   // causal bound masks.
@@ -503,7 +519,7 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
   int w0 = t_begin;  // first tile of the table's window
   auto fill_rows = [&](int first) {
     w0 = first;
-    const int n = min(kRowTable, (t_end + 7 - first) * tile_groups);
+    const int n = min(kRows, (t_end + 7 - first) * tile_groups);
     for (int i = tid; i < n; i += 64 * NWAVE) sm.rows[i] = group_row(first * KB + (i << gshift));
   };
   // this lane's table entry of a tile, and its row within the group
@@ -821,12 +837,19 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
   TileOff off2, off3, off4;
   uint32_t e3[NI], e4[NI];
   // the offsets of the pair after the one whose second tile is t, in one go
+  // (single tiles: off2 is tile t+1, off3 tile t+2, and e3 its entries)
   auto next_offsets = [&](int t) {
-    off2 = off4;
-    row_read(t + 4, e3);
-    row_read(t + 5, e4);
-    row_off(e3, off3);
-    row_off(e4, off4);
+    if constexpr (kPairs) {
+      off2 = off4;
+      row_read(t + 4, e3);
+      row_read(t + 5, e4);
+      row_off(e3, off3);
+      row_off(e4, off4);
+    } else {
+      off2 = off3;
+      row_read(t + 3, e3);
+      row_off(e3, off3);
+    }
   };
   // One tile's step: FIRST of the pair (issues the pair's loads) or second (forms
   // the next pair's load offsets); NEXT_MASK: tile t+1 is masked.
@@ -850,7 +873,7 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
       a1[0] = kfrag(1, 0);
       constexpr int EPC = 16 / KSTEPS;  // elements of P(t)'s keys [32, 64) half per chunk
       static_assert(EPC % 2 == 0, "P elements are formed in bf16 pairs");
-      static_assert(4 * NI <= KSTEPS, "one load per chunk");
+      static_assert((kPairs ? 4 : 2) * NI <= KSTEPS, "one load per chunk");
 #pragma unroll
       for (int s = 0; s < KSTEPS; ++s) {
         if (s + 1 < KSTEPS) {
@@ -868,7 +891,12 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
           nxt[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0[s & 1], qreg[s], nxt[0], 0, 0, 0);
           nxt[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1[s & 1], qreg[s], nxt[1], 0, 0, 0);
         }
-        if constexpr (FIRST) {
+        if constexpr (!kPairs) {
+          // the s-th of this wave's 2*NI loads: K(t+2), V(t+1)
+          const int i = s / NI, j = s % NI;
+          if (i == 0) load_k(bc, off3, j);
+          else if (i == 1) load_v(bn, off2, j);
+        } else if constexpr (FIRST) {
           // the s-th of this wave's 4*NI loads: K(t+3), V(t+2), K(t+4), V(t+3)
           const int i = s / NI, j = s % NI;
           if (i == 0) load_k((bc + 3) % NBUF, off3, j);
@@ -912,7 +940,14 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if constexpr (!FIRST) {
+        if constexpr (!kPairs) {
+          if (j == 0) {
+            off2 = off3;
+            row_read(t + 3, e3);
+          } else if (j == 2) {
+            row_off(e3, off3);
+          }
+        } else if constexpr (!FIRST) {
           // the next pair's load offsets: V(t+3) .. of this pair's last K tile, then
           // the table entries of the two K tiles after it
           if (j == 0) {
@@ -970,13 +1005,23 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
     __builtin_amdgcn_s_setprio(0);
     publish_barrier<0>();
     if (has_invalid) {
-      note_valid((t - t_begin + 3) % NBUF, e3);
-      note_valid((t - t_begin) % NBUF, e4);
+      if constexpr (kPairs) {
+        note_valid((t - t_begin + 3) % NBUF, e3);
+        note_valid((t - t_begin) % NBUF, e4);
+      } else {
+        note_valid((t - t_begin) % NBUF, e3);
+      }
     }
-    if constexpr (!kPrompt) if (t + 6 >= w0 + window) {
-      // the second step reads the table for tiles t+5, t+6: move the window there
-      // (its readers are past the barrier)
-      fill_rows(t + 5);
+    if constexpr (kPrompt) {
+    } else if constexpr (kPairs) {
+      if (t + 6 >= w0 + window) {
+        // the second step reads the table for tiles t+5, t+6: move the window there
+        // (its readers are past the barrier)
+        fill_rows(t + 5);
+        publish_barrier<0>();
+      }
+    } else if (t + 3 >= w0 + window) {
+      fill_rows(t + 3);
       publish_barrier<0>();
     }
     // The matrix phases run at raised wave priority: a wave in its MFMA phases
@@ -1011,31 +1056,52 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
     {
       uint32_t e1[NI], e2[NI];
       row_read(t_begin + 1, e1);
-      row_read(t_begin + 2, e2);
-      row_read(t_begin + 3, e3);
-      row_read(t_begin + 4, e4);
-      row_off(e1, off1);
-      row_off(e2, off2);
-      row_off(e3, off3);
-      row_off(e4, off4);
-      note_valid(1, e1);
-      note_valid(2, e2);
+      if constexpr (kPairs) {
+        row_read(t_begin + 2, e2);
+        row_read(t_begin + 3, e3);
+        row_read(t_begin + 4, e4);
+        row_off(e1, off1);
+        row_off(e2, off2);
+        row_off(e3, off3);
+        row_off(e4, off4);
+        note_valid(1, e1);
+        note_valid(2, e2);
+      } else {
+        row_read(t_begin + 2, e3);
+        row_off(e1, off1);
+        off2 = off1;
+        row_off(e3, off3);
+        note_valid(1, e1);
+      }
     }
 #pragma unroll
     for (int j = 0; j < NI; ++j) load_k(1, off1, j);
+    if constexpr (kPairs) {
 #pragma unroll
-    for (int j = 0; j < NI; ++j) load_k(2, off2, j);
+      for (int j = 0; j < NI; ++j) load_k(2, off2, j);
+    }
     // the query rows and K(t0) have landed ("memory": the reads of the rows stay behind it)
-    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * NI) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"((kPairs ? 2 : 1) * NI) : "memory");
     if (active) read_q();
     lds_barrier();  // K(t0) published, the query rows read
 #pragma unroll
     for (int j = 0; j < NI; ++j) load_v(0, off0, j);
+    if constexpr (kPairs) {
 #pragma unroll
-    for (int j = 0; j < NI; ++j) load_v(1, off1, j);
+      for (int j = 0; j < NI; ++j) load_v(1, off1, j);
+    }
     if (!active) {
       int t = t_begin;
-      for (; t + 2 < t_end; t += 2) {
+      if constexpr (!kPairs) {
+        for (; t + 1 < t_end; ++t) {
+          pair_top(t);
+#pragma unroll
+          for (int j = 0; j < NI; ++j) load_k((t - t_begin) % NBUF, off3, j);
+#pragma unroll
+          for (int j = 0; j < NI; ++j) load_v((t - t_begin + 1) % NBUF, off2, j);
+          next_offsets(t);
+        }
+      } else for (; t + 2 < t_end; t += 2) {
         pair_top(t);
 #pragma unroll
         for (int j = 0; j < NI; ++j) load_k((t - t_begin + 3) % NBUF, off3, j);
@@ -1068,11 +1134,13 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
     for (; t + 2 < t_plain; t += 2) {
       pair_top(t);
       tile_step(t, sA, sB, std::true_type{}, std::false_type{});
+      if constexpr (!kPairs) pair_top(t + 1);
       tile_step(t + 1, sB, sA, std::false_type{}, std::false_type{});
     }
     for (; t + 2 < t_end; t += 2) {
       pair_top(t);
       tile_step(t, sA, sB, std::true_type{}, std::true_type{});
+      if constexpr (!kPairs) pair_top(t + 1);
       tile_step(t + 1, sB, sA, std::false_type{}, std::true_type{});
     }
     pair_top(t);
@@ -1080,6 +1148,7 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
       tile_step(t, sA, sB, std::true_type{}, std::true_type{});
       copy_state(sA, sB);
       ++t;
+      if constexpr (!kPairs) pair_top(t);
     }
     // drain: P and PV of the last tile
     u32x4 w1[2];
@@ -1108,8 +1177,9 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
   float lse_v = (m_run == -__builtin_inff() || l_tot <= 0.f)
                           ? -__builtin_inff()
                           : (m_run + __log2f(l_tot)) * 0.6931471805599453f;
-  bool one_part = true;
-  if constexpr (!kPrompt) one_part = a.parts == 1;
+  bool one_part;
+  if constexpr (kPrompt) one_part = prompt_t >= a.split_tiles;
+  else one_part = a.parts == 1;
   if constexpr (!kStep) {
     if (l_tot != l_tot) {  // a NaN among the row's scores is the row's, through the merge as well
       inv = l_tot;
@@ -1231,27 +1301,29 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
       const int c = pw.region == 0 ? div_by(i, a.d_q) : b;
       const int64_t rows_total = (int64_t)a.batch * a.n_q_heads * a.n_q;
       return part_id * rows_total + (int64_t)(c * a.n_q_heads + g * G + h) * a.n_q + (pw.region == 0 ? i - c * a.n_q : i);
+    } else if constexpr (kPrompt) {  // by the place in the row tile
+      return ((int64_t)prompt_item_of(a, part, prompt_t) * a.n_kv_heads + g) * rows_wg + (i * G + h - rt * rows_wg);
     }
     return 0;
   };
   auto out_row = [&](int i, int h) -> char* {
+    if constexpr (!kStep)
+      if (!one_part) return (char*)a.part_o + partial_row(i, h) * kRowBytes;
     if constexpr (kPrompt) return (char*)a.out + ((seq_start + i) * a.out_tok + (g * G + h) * a.out_head) * 2;
     if constexpr (kPrefix) {
-      if (!one_part) return (char*)a.part_o + partial_row(i, h) * kRowBytes;
       const int c = pw.region == 0 ? div_by(i, a.d_q) : b;
       return (char*)a.out + ((int64_t)(c * a.n_q_heads + g * G + h) * a.out_head_stride + (int64_t)(pw.region == 0 ? i - c * a.n_q : i) * D) * 2;
     }
     return nullptr;
   };
-  if constexpr (kPrompt) {
-    if (row_ok && gsel == 0 && a.lse != nullptr) a.lse[qh * a.lse_stride + seq_start + qi] = lse_v;
-  } else if constexpr (kPrefix) {
+  if constexpr (!kStep) {
     if (row_ok && gsel == 0) {
-      const int64_t at = partial_row(qi, qh - g * G);
+      int64_t at = partial_row(qi, qh - g * G);
       if (!one_part) {
         a.part_lse[at] = lse_v;
         a.part_exp[at] = ex;
       } else if (a.lse != nullptr) {
+        if constexpr (kPrompt) at = qh * a.lse_stride + seq_start + qi;
         a.lse[at] = lse_v;
       }
     }
@@ -1299,16 +1371,22 @@ __global__ void __launch_bounds__(64 * NWAVE, 1) attend_mfma_kernel(Args a) {
 }  // namespace
 
 hipError_t launch_prompt_mfma(const PromptArgs& a, hipStream_t s) {
-  const dim3 grid(a.n_tiles * a.n_kv_heads), block(64 * NWAVE);
-  if (a.head_dim == 128) hipLaunchKernelGGL((attend_mfma_kernel<128, 0, false, PromptArgs>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((attend_mfma_kernel<64, 0, false, PromptArgs>), grid, block, 0, s, a);
+  const dim3 grid(a.items * a.n_kv_heads), block(64 * a.row_waves);
+  const bool wide = a.head_dim == 128, eight = a.row_waves == 8;
+  if (wide && eight) hipLaunchKernelGGL((attend_mfma_kernel<128, 0, false, PromptArgs, 8>), grid, block, 0, s, a);
+  else if (wide) hipLaunchKernelGGL((attend_mfma_kernel<128, 0, false, PromptArgs, 4>), grid, block, 0, s, a);
+  else if (eight) hipLaunchKernelGGL((attend_mfma_kernel<64, 0, false, PromptArgs, 8>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((attend_mfma_kernel<64, 0, false, PromptArgs, 4>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_prefix_mfma(const PrefixArgs& a, hipStream_t s) {
-  const dim3 grid(prefix_workgroups(a)), block(64 * NWAVE);
-  if (a.head_dim == 128) hipLaunchKernelGGL((attend_mfma_kernel<128, 0, false, PrefixArgs>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((attend_mfma_kernel<64, 0, false, PrefixArgs>), grid, block, 0, s, a);
+  const dim3 grid(prefix_workgroups(a)), block(64 * a.row_waves);
+  const bool wide = a.head_dim == 128, eight = a.row_waves == 8;
+  if (wide && eight) hipLaunchKernelGGL((attend_mfma_kernel<128, 0, false, PrefixArgs, 8>), grid, block, 0, s, a);
+  else if (wide) hipLaunchKernelGGL((attend_mfma_kernel<128, 0, false, PrefixArgs, 4>), grid, block, 0, s, a);
+  else if (eight) hipLaunchKernelGGL((attend_mfma_kernel<64, 0, false, PrefixArgs, 8>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((attend_mfma_kernel<64, 0, false, PrefixArgs, 4>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
@@ -1323,7 +1401,7 @@ hipError_t launch_attend_mfma(const AttendArgs& args, hipStream_t s) {
   a.d_group = fast_div(G);
   a.d_block = fast_div(a.geom.block_size);
   const int blocks = n_row_tiles * a.parts * a.batch * a.n_kv_heads;
-  const dim3 grid(blocks), block(64 * NWAVE);
+  const dim3 grid(blocks), block(64 * kMfmaWaves);
   const bool sel = a.idx_out != nullptr, mass = sel && a.mass_part != nullptr;
   if (sel && (a.sel_units < 0 || a.sel_units > kFusedSelectMax)) return hipErrorInvalidValue;
   const bool long_rows = sel && a.sel_units > kFusedSelectShort;

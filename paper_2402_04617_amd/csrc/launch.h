@@ -225,7 +225,17 @@ struct AttendArgs {
 // level: the tiles that many sequences have at one level lie side by side, so that
 // tile numbers fall by the keys a tile sees.  first[i] is the number of the first tile
 // of the levels that exactly the i + 1 longest sequences reach.
+//
+// The row tiles that see the most keys are split along the keys: part p takes the key
+// tiles [p * part_tiles, (p + 1) * part_tiles), and a tile has as many parts as its level
+// can see.  The row tiles with a part p are the first ones, those whose part p is a full
+// one of part_tiles the first full[p] of them.  So that the workgroups which start last
+// are short ones, the items of the launch are numbered full parts first, by part, then the
+// rest from the last part down to part 0 (row tiles that are whole).  Where a tile has
+// several parts (the first split_tiles) they leave partial rows (see common.h), rows_wg of
+// them per item and kv head, and a merge.
 constexpr int kMaxPrompts = 256;  // of one launch
+constexpr int kMaxPromptParts = 16;
 struct PromptArgs {
   int n_seqs, n_q_heads, n_kv_heads, head_dim;
   int64_t q_tok, q_head, kv_tok, kv_head, out_tok, out_head;
@@ -238,6 +248,16 @@ struct PromptArgs {
   float* lse;  // nullable, [n_q_heads][lse_stride]
   int row_waves;  // waves of a workgroup that hold query rows, 32 each
   int n_tiles;
+  int parts;       // most parts of a row tile
+  int part_tiles;  // key tiles of a part
+  int split_tiles;
+  int items;
+  int full[kMaxPromptParts];
+  int full_begin[kMaxPromptParts + 1];  // first item of the full parts p; of the rest
+  int rest_begin[kMaxPromptParts + 1];  // first item of the rest of part parts - 1 - x; all items
+  void* part_o;
+  float* part_lse;
+  int32_t* part_exp;
   FastDiv d_group, d_kv;
   bool bf16;
   int32_t start[kMaxPrompts];
@@ -248,6 +268,25 @@ struct PromptTile {
   int start, len;  // the sequence
   int tile;        // row tile of it
 };
+// The part and row tile of an item, and back.
+__device__ __forceinline__ void prompt_item(const PromptArgs& a, int item, int& p, int& t) {
+  const int* begin = item < a.full_begin[a.parts] ? a.full_begin : a.rest_begin;
+  int x = 0;
+  for (int i = 1; i < a.parts; ++i) x += item >= begin[i] ? 1 : 0;
+  p = begin == a.full_begin ? x : a.parts - 1 - x;
+  t = item - begin[x] + (begin == a.full_begin ? 0 : a.full[p]);
+}
+__device__ __forceinline__ int prompt_item_of(const PromptArgs& a, int p, int t) {
+  return t < a.full[p] ? a.full_begin[p] + t : a.rest_begin[a.parts - 1 - p] + t - a.full[p];
+}
+// Row tiles with a part p.
+__device__ __forceinline__ int prompt_part_count(const PromptArgs& a, int p) {
+  return a.full[p] + a.rest_begin[a.parts - p] - a.rest_begin[a.parts - 1 - p];
+}
+// Rows that the items with partial rows take: those before the row tiles that are whole.
+__host__ inline int64_t prompt_partial_rows(const PromptArgs& a) {
+  return a.parts > 1 ? (int64_t)a.rest_begin[a.parts - 1] * a.n_kv_heads * 32 * a.row_waves : 0;
+}
 // Row tile number t (uniform over the wave).
 __device__ __forceinline__ PromptTile prompt_tile(const PromptArgs& a, int t, int rows_log2) {
   int i = 1;
@@ -263,6 +302,7 @@ __device__ __forceinline__ PromptTile prompt_tile(const PromptArgs& a, int t, in
   return PromptTile{a.start[s], a.len[s], ((rows - 1) >> rows_log2) - down};
 }
 hipError_t launch_prompt(const PromptArgs& a, hipStream_t s);
+hipError_t launch_prompt_merge(const PromptArgs& a, hipStream_t s);
 
 // Attention of continuations over a document they share.  Three regions of keys, each
 // with parts of its own:

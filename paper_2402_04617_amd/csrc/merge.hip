@@ -15,8 +15,8 @@ namespace infllm {
 namespace {
 
 // One piece of one part's row: its values in float, and its lse.
-template <bool HALF>
-__device__ __forceinline__ void load_piece(const MergeArgs& a, int64_t pr, int c, float (&o)[HALF ? 8 : 4], float& l) {
+template <bool HALF, typename Args>
+__device__ __forceinline__ void load_piece(const Args& a, int64_t pr, int c, float (&o)[HALF ? 8 : 4], float& l) {
   l = a.part_lse[pr];
   if constexpr (HALF) {
     const uint4 w = *(const uint4*)((const uint16_t*)a.part_o + pr * a.head_dim + 8 * c);
@@ -35,6 +35,33 @@ __device__ __forceinline__ void load_piece(const MergeArgs& a, int64_t pr, int c
     o[3] = w.w;
   }
 }
+// Adds the first `n` of CH pieces to a running maximum, weight sum and weighted row.
+template <int DPT, int CH>
+__device__ __forceinline__ void add_parts(const float (&l)[CH], const float (&o)[CH][DPT], int n, bool rescale, float& M,
+                                          float& tot, float (&acc)[DPT]) {
+  float m_new = M;
+#pragma unroll
+  for (int j = 0; j < CH; ++j)
+    if (j < n) m_new = fmaxf(m_new, l[j]);
+  if (m_new == -__builtin_inff()) return;  // nothing visible yet
+  if (rescale) {
+    const float r = M == -__builtin_inff() ? 0.f : expf(M - m_new);
+    tot *= r;
+#pragma unroll
+    for (int e = 0; e < DPT; ++e) acc[e] *= r;
+  }
+#pragma unroll
+  for (int j = 0; j < CH; ++j) {
+    const bool live = j < n && l[j] != -__builtin_inff();
+    const float w = live ? expf(l[j] - m_new) : 0.f;
+    tot += w;
+    // (no value times 0: one that is not finite would leave a NaN, and the piece of a
+    // thread past the last part is that part's again)
+#pragma unroll
+    for (int e = 0; e < DPT; ++e) acc[e] += w * (live ? o[j][e] : 0.f);
+  }
+  M = m_new;
+}
 // Joins parts first, first + step, ... (every load of CH of them issued before the
 // first use) into a running maximum, weight sum and weighted row.  ONCE: there are at
 // most CH of them.
@@ -51,36 +78,13 @@ __device__ __forceinline__ void join_parts(const MergeArgs& a, int row, int c, i
 #pragma unroll
     for (int j = 0; j < CH; ++j)
       load_piece<HALF>(a, (int64_t)min(p0 + j * step, a.parts - 1) * a.rows + row, c, o[j], l[j]);
-    float m_new = M;
-#pragma unroll
-    for (int j = 0; j < CH; ++j)
-      if (p0 + j * step < a.parts) m_new = fmaxf(m_new, l[j]);
-    if (m_new == -__builtin_inff()) continue;  // nothing visible yet
-    if constexpr (!ONCE) {
-      const float r = M == -__builtin_inff() ? 0.f : expf(M - m_new);
-      tot *= r;
-#pragma unroll
-      for (int e = 0; e < DPT; ++e) acc[e] *= r;
-    }
-#pragma unroll
-    for (int j = 0; j < CH; ++j) {
-      const bool live = p0 + j * step < a.parts && l[j] != -__builtin_inff();
-      const float w = live ? expf(l[j] - m_new) : 0.f;
-      tot += w;
-      // (no product with 0: a value that is not finite would leave a NaN, and the piece of
-      // a thread past the last part is that part's again)
-#pragma unroll
-      for (int e = 0; e < DPT; ++e) acc[e] += live ? w * o[j][e] : 0.f;
-    }
-    M = m_new;
+    add_parts<DPT, CH>(l, o, (a.parts - p0 + step - 1) / step, !ONCE, M, tot, acc);
     if (ONCE) break;
   }
 }
 template <typename T, int DPT>
-__device__ __forceinline__ void store_piece(const MergeArgs& a, int row, int c, float M, float tot, const float (&acc)[DPT]) {
+__device__ __forceinline__ void store_row_piece(T* op, float* lse, float M, float tot, const float (&acc)[DPT]) {
   const float inv = tot > 0.f ? 1.f / tot : 0.f;
-  const int bh = row / a.n_q, i = row - bh * a.n_q;
-  T* op = (T*)a.out + (int64_t)bh * a.out_head_stride + (int64_t)i * a.head_dim + DPT * c;
   if constexpr (sizeof(T) == 2) {
     uint32_t w[DPT / 2];
 #pragma unroll
@@ -93,7 +97,13 @@ __device__ __forceinline__ void store_piece(const MergeArgs& a, int row, int c, 
     for (int e = 0; e < DPT; ++e) op[e] = acc[e] * inv;
   }
   // (tot is NaN where a part's scores hold a NaN: such a part comes with lse = +inf)
-  if (a.lse != nullptr && c == 0) a.lse[row] = tot > 0.f ? M + logf(tot) : tot != tot ? tot : -__builtin_inff();
+  if (lse != nullptr) *lse = tot > 0.f ? M + logf(tot) : tot != tot ? tot : -__builtin_inff();
+}
+template <typename T, int DPT>
+__device__ __forceinline__ void store_piece(const MergeArgs& a, int row, int c, float M, float tot, const float (&acc)[DPT]) {
+  const int bh = row / a.n_q, i = row - bh * a.n_q;
+  store_row_piece<T, DPT>((T*)a.out + (int64_t)bh * a.out_head_stride + (int64_t)i * a.head_dim + DPT * c,
+                          a.lse != nullptr && c == 0 ? a.lse + row : nullptr, M, tot, acc);
 }
 
 template <typename T, bool HALF, int CH>
@@ -147,6 +157,36 @@ __global__ void __launch_bounds__(256) merge_many_kernel(MergeArgs a) {
   store_piece<T, DPT>(a, row, c, M, tot, acc);
 }
 
+// The split row tiles of packed prompts: workgroups (row tile, kv head, rows of it); a
+// row's parts lie in the items of its row tile.
+template <typename T, bool HALF, int CH>
+__global__ void __launch_bounds__(256) prompt_merge_kernel(PromptArgs a, int rows_log2) {
+  constexpr int DPT = HALF ? 8 : 4;
+  const int tpr = a.head_dim / DPT, rows_per_wg = 256 / tpr;
+  const int per_tile = (1 << rows_log2) / rows_per_wg;  // workgroups of a row tile
+  const int tg = (int)blockIdx.x / per_tile, sub = (int)blockIdx.x - tg * per_tile;
+  const int t = div_by(tg, a.d_kv), g = tg - t * (int)a.d_kv.d;
+  const PromptTile pt = prompt_tile(a, t, rows_log2);
+  const int r = sub * rows_per_wg + (int)threadIdx.x / tpr, c = threadIdx.x % tpr;
+  const int row = (pt.tile << rows_log2) + r, G = (int)a.d_group.d;
+  if (row >= pt.len * G) return;
+  int parts = 1;
+  for (int p = 1; p < a.parts; ++p) parts += t < prompt_part_count(a, p) ? 1 : 0;
+  float l[CH], o[CH][DPT];
+  float M = -__builtin_inff(), tot = 0.f, acc[DPT] = {};
+  for (int p0 = 0; p0 < parts; p0 += CH) {
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      const int64_t pr = (((int64_t)prompt_item_of(a, min(p0 + j, parts - 1), t) * a.n_kv_heads + g) << rows_log2) + r;
+      load_piece<HALF>(a, pr, c, o[j], l[j]);
+    }
+    add_parts<DPT, CH>(l, o, parts - p0, p0 > 0, M, tot, acc);
+  }
+  const int i = div_by(row, a.d_group), h = g * G + row - i * G;
+  store_row_piece<T, DPT>((T*)a.out + (pt.start + i) * a.out_tok + h * a.out_head + DPT * c,
+                          a.lse != nullptr && c == 0 ? a.lse + h * a.lse_stride + pt.start + i : nullptr, M, tot, acc);
+}
+
 constexpr int kManyRows = 1024;  // most rows whose many parts are split over threads
 
 template <typename T, bool HALF>
@@ -171,6 +211,21 @@ hipError_t launch_merge_t(const MergeArgs& a, hipStream_t s) {
 }
 
 }  // namespace
+
+hipError_t launch_prompt_merge(const PromptArgs& a, hipStream_t s) {
+  const int rows_wg = 32 * a.row_waves, log2 = __builtin_ctz((unsigned)rows_wg);
+  const int rows_per_wg = 256 / (a.head_dim / (a.bf16 ? 8 : 4));
+  const dim3 grid(a.split_tiles * a.n_kv_heads * (rows_wg / rows_per_wg)), block(256);
+  const bool few = a.parts <= 4;
+  if (a.bf16) {
+    if (few) hipLaunchKernelGGL((prompt_merge_kernel<bf16_t, true, 4>), grid, block, 0, s, a, log2);
+    else hipLaunchKernelGGL((prompt_merge_kernel<bf16_t, true, 8>), grid, block, 0, s, a, log2);
+  } else {
+    if (few) hipLaunchKernelGGL((prompt_merge_kernel<float, false, 4>), grid, block, 0, s, a, log2);
+    else hipLaunchKernelGGL((prompt_merge_kernel<float, false, 8>), grid, block, 0, s, a, log2);
+  }
+  return hipGetLastError();
+}
 
 hipError_t launch_merge(const MergeArgs& a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
