@@ -272,74 +272,88 @@ namespace {
 
 // Launch shape of the prefix attention.
 struct PrefixPlan {
-  int row_waves, tiles_s, tiles_p;
-  int most_s, most_u, most_o;  // most parts of the regions
+  int row_waves, tiles_s, tiles_p;   // row tiles of the shared region, and of one continuation
+  int64_t keys_s, keys_u;            // tiles of keys
+  int most_s, most_u, most_o;        // most parts of the regions
   int parts_s, parts_u, parts_o;
 };
 
+int64_t key_tiles(const infllm_params* p, int64_t keys) {
+  const int kt = key_tile(p->dtype == INFLLM_BF16);
+  return (keys + kt - 1) / kt;
+}
 
-// The part counts' bounds follow from the shape alone, so that the workspace does.
+// The part counts' bounds follow from the shape alone, so that the workspace does: no
+// region takes more than one round of workgroups.
 PrefixPlan prefix_shape(const infllm_params* p, int batch, int n_q, int64_t shared_keys, int64_t unit_keys,
                         int64_t own_keys) {
   PrefixPlan r;
   const bool bf16 = p->dtype == INFLLM_BF16;
   const int64_t G = p->n_q_heads / p->n_kv_heads, rows_p = G * n_q, rows_s = rows_p * batch;
   const int64_t most_rows = shared_keys > 0 ? rows_s : rows_p;
-  r.row_waves = bf16 ? (most_rows > 32 * kMfmaWaves / 2 ? kMfmaWaves : kMfmaWaves / 2)
-                     : (most_rows > 64 ? 4 : most_rows > 32 ? 2 : 1);
-  const int rows_wg = 32 * r.row_waves, target = resident_wgs(p, r.row_waves);
+  // (bf16: eight waves a workgroup are slower throughout, by up to 2 times with few rows;
+  // of 3,200 rows over 68 tiles of keys 165 us against 163)
+  r.row_waves = bf16 ? kMfmaWaves / 2 : most_rows > 64 ? 4 : most_rows > 32 ? 2 : 1;
+  const int rows_wg = 32 * r.row_waves, at_a_time = resident_wgs(p, r.row_waves);
   r.tiles_s = (int)((rows_s + rows_wg - 1) / rows_wg);
   r.tiles_p = (int)((rows_p + rows_wg - 1) / rows_wg);
-  auto most = [&](int64_t keys, int64_t wgs) {
-    const int64_t tiles = (keys + key_tile(bf16) - 1) / key_tile(bf16);
-    return (int)std::min<int64_t>(tiles, 2 * target / std::max<int64_t>(1, wgs * p->n_kv_heads) + 1);
+  r.keys_s = key_tiles(p, shared_keys);
+  r.keys_u = key_tiles(p, unit_keys);
+  auto most = [&](int64_t tiles, int64_t wgs) {
+    return (int)std::min<int64_t>(tiles, at_a_time / std::max<int64_t>(1, wgs * p->n_kv_heads) + 1);
   };
-  r.most_s = most(shared_keys, r.tiles_s);
-  r.most_u = most(unit_keys, (int64_t)batch * r.tiles_p);
-  r.most_o = std::max(1, most(own_keys, (int64_t)batch * r.tiles_p));
+  r.most_s = most(r.keys_s, r.tiles_s);
+  r.most_u = most(r.keys_u, (int64_t)batch * r.tiles_p);
+  r.most_o = most(key_tiles(p, own_keys), (int64_t)batch * r.tiles_p);
   r.parts_s = r.parts_u = r.parts_o = 0;
   return r;
 }
 
-// Parts of at most T tiles each, T the least that keeps the workgroups within a number of
-// rounds: of one to four rounds the one whose time, a prologue and T tiles for each, is least.
-void prefix_parts(const infllm_params* p, int batch, int64_t shared_keys, int64_t unit_keys, int64_t own_keys,
-                  PrefixPlan* r) {
-  const bool bf16 = p->dtype == INFLLM_BF16;
-  const int kt = key_tile(bf16), target = resident_wgs(p, r->row_waves);
-  const int64_t ts = (shared_keys + kt - 1) / kt, tu = (unit_keys + kt - 1) / kt, to = (own_keys + kt - 1) / kt;
+// Parts of at most T tiles of keys each.  As for the prompts, the launch lasts as long as
+// its work shared over the workgroups that run at a time, or as a part; where the last
+// workgroups (the own tokens') have to wait for full parts of the other regions, as a part
+// and one of theirs; the longer the parts, the longer its end, when few still run.  A tile of a row tile's own keys takes its share of the memory's
+// rate, one that several row tiles read the matrix cores'; the merge adds its launch, a
+// round trip for every eight parts of a lane group, and the partial rows' bytes.  Measured
+// in us at T = 8, 12, 16, 24, 32, 48: 32 continuations of 64K tokens 89, 81, 79, 68, 70,
+// 81; 8 of 8 tokens at 128K 48, 49, 41, 43, 46, 46; 64 of 8K tokens 34, 31, 32, 36, 46, 55.
+void prefix_parts(const infllm_params* p, int batch, int n_q, const int64_t* own_lens, int64_t own_keys, PrefixPlan* r) {
+  const bool bf16 = p->dtype == INFLLM_BF16, wide = p->head_dim == 128;
+  const int Hkv = p->n_kv_heads, rows = batch * p->n_q_heads * n_q;
+  const int64_t to = key_tiles(p, own_keys), pairs = (int64_t)batch * r->tiles_p;
+  int64_t own_sum = 0;
+  for (int b = 0; b < batch; ++b) own_sum += key_tiles(p, own_lens[b]);
+  const float memory_tile = wide ? 2.8f : 1.4f, core_tile = item_cost(p, r->row_waves).tile;
+  const float tile_s = bf16 && r->tiles_s < 2 ? memory_tile : core_tile;
+  const float tile_p = bf16 && r->tiles_p < 2 ? memory_tile : core_tile;
+  const float item = bf16 ? (r->tiles_s < 2 && r->tiles_p < 2 ? 5.f : 9.f) : 8.f;
+  const float lone_tile = bf16 ? (wide ? 1.35f : 0.75f) : wide ? 5.9f : 3.4f, lone_item = bf16 ? 6.5f : wide ? 7.f : 5.f;
+  const float share = (float)Hkv / (float)resident_wgs(p, r->row_waves);
+  const int groups = 64 / (p->head_dim / (bf16 ? 8 : 4));  // lane groups of the merge
+  const int64_t most_tiles = std::max<int64_t>(std::max(r->keys_s, r->keys_u), std::max<int64_t>(to, 1));
   auto parts = [](int64_t tiles, int64_t T, int most) { return (int)std::min<int64_t>((tiles + T - 1) / T, most); };
-  auto wgs = [&](int64_t T) {
-    return p->n_kv_heads * ((int64_t)r->tiles_s * parts(ts, T, r->most_s) +
-                            (int64_t)batch * r->tiles_p * (parts(tu, T, r->most_u) + parts(to, T, r->most_o)));
-  };
-  auto longest = [&](int64_t T) {  // tiles of the longest part, under the bounds
-    int64_t x = 0;
-    if (ts > 0) x = std::max(x, (ts + parts(ts, T, r->most_s) - 1) / parts(ts, T, r->most_s));
-    if (tu > 0) x = std::max(x, (tu + parts(tu, T, r->most_u) - 1) / parts(tu, T, r->most_u));
-    if (to > 0) x = std::max(x, (to + parts(to, T, r->most_o) - 1) / parts(to, T, r->most_o));
-    return x;
-  };
-  const int64_t most_tiles = std::max(std::max(ts, tu), std::max<int64_t>(to, 1));
-  constexpr int kPartCost = 5;  // prologue and epilogue of a workgroup, in tiles
-  int64_t best = most_tiles, best_cost = -1;
-  for (int rounds = 1; rounds <= 4; ++rounds) {
-    int64_t lo = 1, hi = most_tiles;
-    while (lo < hi) {
-      const int64_t mid = (lo + hi) / 2;
-      if (wgs(mid) <= (int64_t)rounds * target) hi = mid;
-      else lo = mid + 1;
+  auto longest = [](int64_t tiles, int n) { return n > 0 ? (tiles + n - 1) / n : 0; };
+  const float work = ((float)(r->tiles_s * r->keys_s) * tile_s + (float)(pairs * r->keys_u + r->tiles_p * own_sum) * tile_p) * share;
+  float best = -1.f;
+  for (int64_t T = 1;; T += T < 6 ? 1 : T / 4) {  // (1 to 6, then steps of a quarter)
+    T = std::min(T, most_tiles);
+    const int ps = parts(r->keys_s, T, r->most_s), pu = parts(r->keys_u, T, r->most_u), po = parts(to, T, r->most_o);
+    const int64_t full = (int64_t)r->tiles_s * ps + pairs * pu, items = full + pairs * po;
+    const int64_t long_o = longest(to, po), long_p = std::max(std::max(longest(r->keys_s, ps), longest(r->keys_u, pu)), long_o);
+    const float part = (float)long_p * lone_tile + lone_item;
+    const float late = (float)items * share - 1.f;  // rounds of workgroups past the first
+    float t = std::max(part, work + (float)items * share * item);
+    if (late > 0.f && (float)full * share + late > 1.f) t = std::max(t, part + (float)long_o * lone_tile + lone_item);
+    const int all = ps + pu + po;
+    t += 0.2f * part + 4.f + 1.5f * (float)((all + 8 * groups - 1) / (8 * groups)) + (float)all * (float)rows * (float)part_row_bytes(p) * kPartialByteCost;
+    if (best < 0.f || t < best) {
+      best = t;
+      r->parts_s = ps;
+      r->parts_u = pu;
+      r->parts_o = po;
     }
-    const int64_t real = (wgs(lo) + target - 1) / target;
-    const int64_t cost = real * (kPartCost + longest(lo));
-    if (best_cost < 0 || cost < best_cost) {
-      best = lo;
-      best_cost = cost;
-    }
+    if (T == most_tiles) break;
   }
-  r->parts_s = ts > 0 ? parts(ts, best, r->most_s) : 0;
-  r->parts_u = tu > 0 ? parts(tu, best, r->most_u) : 0;
-  r->parts_o = std::max(1, parts(to, best, r->most_o));
 }
 
 // Keys of the shared region at document length `len`, and of the looked-up units.
@@ -433,22 +447,25 @@ infllm_status infllm_prefix_attend(const infllm_params* p, const infllm_memory* 
   if (units > 0 && idx == nullptr) return INFLLM_E_NULL;
   const bool bf16 = p->dtype == INFLLM_BF16;
   const int64_t G = p->n_q_heads / p->n_kv_heads, D = p->head_dim;
-  if (shared > INT32_MAX || units > INT32_MAX || own_most + n_q > INT32_MAX || G * n_q * B > INT32_MAX)
+  if (shared > INT32_MAX || units > INT32_MAX || own_most + n_q > INT32_MAX || G * n_q * B * p->n_kv_heads > INT32_MAX)
     return INFLLM_E_UNSUPPORTED;
   // the bf16 kernel addresses one (sequence, kv head) slice of a store with 32-bit byte offsets
   if (bf16 && ((uint64_t)prefix->capacity * D * 2u > 0xFFFFFFFFull || (uint64_t)own->capacity * D * 2u > 0xFFFFFFFFull))
     return INFLLM_E_UNSUPPORTED;
   if (n_q == 0) return INFLLM_OK;
   PrefixPlan r = prefix_shape(p, B, n_q, shared, units, own->capacity);
-  prefix_parts(p, B, shared, units, own_most + n_q, &r);
+  // a few current tokens are met by the merge, and not in the own region
+  const bool merge_x = k != nullptr && n_q <= kPrefixMergeTokens;
+  prefix_parts(p, B, n_q, own_lens, own_most + (merge_x ? 0 : n_q), &r);
   const int parts = r.parts_s + r.parts_u + r.parts_o;
-  if (parts > 1) {
+  const bool direct = parts == 1 && !merge_x;
+  if (parts > 0 && !direct) {
     if (workspace == nullptr || workspace_bytes < attend_ws_bytes(p, B, n_q, parts)) return INFLLM_E_WORKSPACE;
     if (!aligned16(workspace)) return INFLLM_E_SHAPE;
   }
   if ((st = check_device()) != INFLLM_OK) return st;
   hipStream_t s = (hipStream_t)stream;
-  if (k != nullptr) {
+  if (k != nullptr && !merge_x) {
     // X joins the own stores: the copy role of the append (no ring, no scores)
     AppendArgs aa;
     std::memset(&aa, 0, sizeof(aa));
@@ -501,6 +518,12 @@ infllm_status infllm_prefix_attend(const infllm_params* p, const infllm_memory* 
   a.parts_u = r.parts_u;
   a.parts_o = r.parts_o;
   a.parts = parts;
+  a.direct = direct;
+  if (merge_x) {
+    a.x_k = k;
+    a.x_v = v;
+    a.x_head_stride = kv_head_stride;
+  }
   a.row_waves = r.row_waves;
   a.tiles_s = r.tiles_s;
   a.tiles_p = r.tiles_p;
@@ -511,16 +534,14 @@ infllm_status infllm_prefix_attend(const infllm_params* p, const infllm_memory* 
   a.d_tiles_s = fast_div(r.tiles_s);
   a.d_tiles_p = fast_div(r.tiles_p);
   a.d_parts_u = fast_div(std::max(1, r.parts_u));
-  a.d_parts_o = fast_div(r.parts_o);
+  a.d_parts_o = fast_div(std::max(1, r.parts_o));
   a.out = out;
   a.lse = lse;
   a.bf16 = bf16;
   for (int b = 0; b < B; ++b) a.own_len[b] = own_lens[b];
-  if (parts > 1) partial_layout(p, workspace, parts, (int64_t)B * p->n_q_heads * n_q, &a.part_o, &a.part_lse, &a.part_exp);
-  if ((st = launch_status(launch_prefix(a, s))) != INFLLM_OK) return st;
-  if (parts == 1) return INFLLM_OK;
-  MergeArgs ma = merge_args(p, B, n_q, parts, workspace, out, out_head_stride, lse);
-  return launch_status(launch_merge(ma, s));
+  if (!direct) partial_layout(p, workspace, parts, (int64_t)B * p->n_q_heads * n_q, &a.part_o, &a.part_lse, &a.part_exp);
+  if (parts > 0 && (st = launch_status(launch_prefix(a, s))) != INFLLM_OK) return st;
+  return direct ? INFLLM_OK : launch_status(launch_prefix_merge(a, s));
 }
 
 infllm_status infllm_copy_sequences(const infllm_params* p, const infllm_memory* dst, const infllm_memory* src, int32_t n,

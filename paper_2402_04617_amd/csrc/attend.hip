@@ -128,7 +128,7 @@ attend_f32_kernel(Args a) {
   // the tiles the row tile's queries see, split evenly over the parts
   const int v_x0 = geo.n_virtual - geo.n_q;
   // (every row sees every key of the prefix attention's first two regions)
-  const bool no_causal = kPrefix && pw.region != 2;
+  const bool no_causal = kPrefix && geo.n_q == 0;
   const int n_tiles = no_causal ? (geo.n_virtual + KT - 1) / KT : (v_x0 + (min(R, (rt + 1) * RW) - 1) / G) / KT + 1;
   int t_begin, t_end;
   if constexpr (kPrompt) {
@@ -414,7 +414,7 @@ attend_f32_kernel(Args a) {
   } else {
     grow = (int64_t)(qb * a.n_q_heads + qh) * a.n_q + qj;
     rows_total = (int64_t)a.batch * a.n_q_heads * a.n_q;
-    n_parts = a.parts;
+    n_parts = a.direct ? 1 : 2;
     part += prefix_first_part(a, pw.region);
     op = n_parts == 1 ? (float*)a.out + (int64_t)(qb * a.n_q_heads + qh) * a.out_head_stride + (int64_t)qj * D
                       : (float*)a.part_o + ((int64_t)part * rows_total + grow) * D;

@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
     rparts = pw.region == 0 ? a.parts_s : pw.region == 1 ? a.parts_u : a.parts_o;
   }
   // whether every row sees every key of the part's region
-  const bool no_causal = kPrefix ? pw.region != 2 : mem_part;
+  const bool no_causal = kPrefix ? geo.n_q == 0 : mem_part;
   const int region_keys = kPrefix ? geo.n_virtual : mem_len;
   // The parts split the tiles this row tile's queries see by cost rather than by
   // count, so that they end together: a masked tile (the causal diagonal) costs
@@ -1179,6 +1179,7 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
                           : (m_run + __log2f(l_tot)) * 0.6931471805599453f;
   bool one_part;
   if constexpr (kPrompt) one_part = prompt_t >= a.split_tiles;
+  else if constexpr (kPrefix) one_part = a.direct;
   else one_part = a.parts == 1;
   if constexpr (!kStep) {
     if (l_tot != l_tot) {  // a NaN among the row's scores is the row's, through the merge as well
@@ -1382,10 +1383,7 @@ hipError_t launch_prompt_mfma(const PromptArgs& a, hipStream_t s) {
 
 hipError_t launch_prefix_mfma(const PrefixArgs& a, hipStream_t s) {
   const dim3 grid(prefix_workgroups(a)), block(64 * a.row_waves);
-  const bool wide = a.head_dim == 128, eight = a.row_waves == 8;
-  if (wide && eight) hipLaunchKernelGGL((attend_mfma_kernel<128, 0, false, PrefixArgs, 8>), grid, block, 0, s, a);
-  else if (wide) hipLaunchKernelGGL((attend_mfma_kernel<128, 0, false, PrefixArgs, 4>), grid, block, 0, s, a);
-  else if (eight) hipLaunchKernelGGL((attend_mfma_kernel<64, 0, false, PrefixArgs, 8>), grid, block, 0, s, a);
+  if (a.head_dim == 128) hipLaunchKernelGGL((attend_mfma_kernel<128, 0, false, PrefixArgs, 4>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((attend_mfma_kernel<64, 0, false, PrefixArgs, 4>), grid, block, 0, s, a);
   return hipGetLastError();
 }

@@ -309,6 +309,9 @@ hipError_t launch_prompt_merge(const PromptArgs& a, hipStream_t s);
 //   shared: I and L of the document, met by the rows of all continuations together;
 //   units : the looked-up units of one continuation (document store);
 //   own   : the tokens of one continuation, X at their end (its own store, causal).
+// A few current tokens (x_k given) are not in the own region: the merge meets them, and
+// writes them to the own stores.
+constexpr int kPrefixMergeTokens = 8;
 struct PrefixArgs {
   int batch, n_q_heads, n_kv_heads, head_dim, n_q;
   int64_t prefix_capacity, own_capacity, q_head_stride, out_head_stride;
@@ -321,8 +324,12 @@ struct PrefixArgs {
   const int32_t* idx;  // [batch][n_kv_heads][idx_stride]
   int n_init, n_units, n_sel, block_size, unit_base, idx_stride;
   int64_t local_begin, prefix_len;
+  const void* x_k;  // [batch][n_kv_heads] heads of n_q rows with x_head_stride, or null
+  const void* x_v;
+  int64_t x_head_stride;
   int parts_s, parts_u, parts_o;  // of the regions; parts = their sum
   int parts;
+  bool direct;                    // one part, whose rows are the output's
   int row_waves;                  // waves of a workgroup that hold query rows (matrix-core kernel)
   int tiles_s, tiles_p;           // row tiles of the shared region and of one continuation
   FastDiv d_group, d_block, d_kv, d_q, d_tiles_s, d_tiles_p, d_parts_u, d_parts_o;
@@ -362,8 +369,7 @@ __device__ __forceinline__ PrefixWork prefix_work(const PrefixArgs& a, int id) {
   w.part = c - w.b * (w.region == 1 ? a.parts_u : a.parts_o);
   return w;
 }
-// The keys of a region as a step's key axis: every row sees all of the shared and the
-// units region (n_q = 0 there).
+// The keys of a region as a step's key axis; n_q = 0 where every row sees all of them.
 __device__ __forceinline__ StepGeom prefix_geom(const PrefixArgs& a, const PrefixWork& w) {
   StepGeom g;
   g.n_units = a.n_units;
@@ -373,11 +379,11 @@ __device__ __forceinline__ StepGeom prefix_geom(const PrefixArgs& a, const Prefi
   g.n_init = w.region == 0 ? a.n_init : 0;
   g.n_sel = w.region == 1 ? a.n_sel : 0;
   g.local_begin = w.region == 0 ? a.local_begin : 0;
-  g.n_q = w.region == 2 ? a.n_q : 0;
+  g.n_q = w.region == 2 && a.x_k == nullptr ? a.n_q : 0;
   g.past_len = w.region == 2 ? a.own_len[w.b] : a.prefix_len;
   g.n_virtual = w.region == 1   ? a.n_sel * a.block_size
                 : w.region == 0 ? (int32_t)(a.n_init + (a.prefix_len - a.local_begin))
-                                : (int32_t)g.past_len + a.n_q;
+                                : (int32_t)g.past_len + g.n_q;
   return g;
 }
 // First part of a region among all parts, and the workgroups of the launch.
@@ -388,6 +394,7 @@ __host__ inline int prefix_workgroups(const PrefixArgs& a) {
   return a.n_kv_heads * (a.tiles_s * a.parts_s + a.batch * a.tiles_p * (a.parts_u + a.parts_o));
 }
 hipError_t launch_prefix(const PrefixArgs& a, hipStream_t s);
+hipError_t launch_prefix_merge(const PrefixArgs& a, hipStream_t s);
 
 // Copies of whole sequences between memories: the pairs are sorted by source, so that a
 // source's bytes are read once for all its copies.

@@ -187,6 +187,95 @@ __global__ void __launch_bounds__(256) prompt_merge_kernel(PromptArgs a, int row
                           a.lse != nullptr && c == 0 ? a.lse + h * a.lse_stride + pt.start + i : nullptr, M, tot, acc);
 }
 
+// The parts of the prefix attention, and its few current tokens.  A wave per row: its
+// 64 / tpr groups of lanes take every GR-th part (the loads of CH of them issued before
+// the first use) and every GR-th current token, and are joined by lane exchanges.  A wave
+// of a group's first head also writes its token's key and value to the own store.
+template <typename T, bool HALF, int D>
+__global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixArgs a) {
+  constexpr int DPT = HALF ? 8 : 4, TPR = D / DPT, GR = 64 / TPR, CH = 4;
+  const int row = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+  const int rows = a.batch * a.n_q_heads * a.n_q;
+  if (row >= rows) return;
+  const int lane = threadIdx.x & 63, c = lane % TPR, grp = lane / TPR;
+  const int bh = div_by(row, a.d_q), i = row - bh * a.n_q;
+  const int bg = div_by(bh, a.d_group);  // (sequence, kv head)
+  const MergeArgs m = {rows, D, a.parts, a.n_q, a.n_q_heads, a.out_head_stride, a.part_o, a.part_lse, a.part_exp, a.out, a.lse, HALF};
+  // the current tokens' rows, requested first
+  float q[DPT] = {};
+  float xk[CH][DPT], xv[CH][DPT];
+  auto load_row = [&](const void* p, int64_t at, float (&x)[DPT]) {
+    const T* r = (const T*)p + at + DPT * c;
+    if constexpr (HALF) {
+      const u32x4 w = *(const u32x4*)r;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        x[2 * j] = __uint_as_float(w[j] << 16);
+        x[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
+      }
+    } else {
+      const f32x4 w = *(const f32x4*)r;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = w[j];
+    }
+  };
+  const int64_t x0 = bg * a.x_head_stride;
+  if (a.x_k != nullptr) {
+    load_row(a.q, bh * a.q_head_stride + (int64_t)i * D, q);
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {  // (a token past the query's own is not looked at)
+      const int64_t at = x0 + (int64_t)min(grp + j * GR, i) * D;
+      if (j * GR < a.n_q) {
+        load_row(a.x_k, at, xk[j]);
+        load_row(a.x_v, at, xv[j]);
+      }
+    }
+  }
+  float M, tot, acc[DPT];
+  if (a.parts <= CH * GR) join_parts<HALF, CH, true>(m, row, c, grp, GR, M, tot, acc);
+  else join_parts<HALF, 2 * CH, false>(m, row, c, grp, GR, M, tot, acc);
+  if (a.x_k != nullptr) {
+    static_assert(kPrefixMergeTokens <= CH * GR, "every token has a place");
+    float z[CH];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      z[j] = -__builtin_inff();
+      if (j * GR >= a.n_q) continue;
+      float s = 0.f;
+#pragma unroll
+      for (int e = 0; e < DPT; ++e) s = __builtin_fmaf(q[e], xk[j][e], s);
+#pragma unroll
+      for (int o = 1; o < TPR; o <<= 1) s += __shfl_xor(s, o);
+      s *= a.sm_scale;
+      // (a NaN score as the attention's parts give it)
+      if (grp + j * GR <= i) z[j] = s == s ? s : __builtin_inff();
+    }
+    add_parts<DPT, CH>(z, xv, CH, true, M, tot, acc);
+  }
+  // the groups' shares
+#pragma unroll
+  for (int o = TPR; o < 64; o <<= 1) {
+    const float M2 = __shfl_xor(M, o), tot2 = __shfl_xor(tot, o), m_new = fmaxf(M, M2);
+    const float w1 = M == -__builtin_inff() ? 0.f : expf(M - m_new), w2 = M2 == -__builtin_inff() ? 0.f : expf(M2 - m_new);
+    tot = tot * w1 + tot2 * w2;
+#pragma unroll
+    for (int e = 0; e < DPT; ++e) {
+      const float x2 = __shfl_xor(acc[e], o);
+      acc[e] = (M == -__builtin_inff() ? 0.f : acc[e] * w1) + (M2 == -__builtin_inff() ? 0.f : x2 * w2);
+    }
+    M = m_new;
+  }
+  if (grp == 0) store_piece<T, DPT>(m, row, c, M, tot, acc);
+  if (a.x_k != nullptr && bh == bg * (int)a.d_group.d && grp < 2) {
+    const int b = bg / a.n_kv_heads;
+    const int64_t to = ((int64_t)bg * a.own_capacity + a.own_len[b] + i) * D + DPT * c;
+    const int64_t from = x0 + (int64_t)i * D + DPT * c;
+    const void* src = grp == 0 ? a.x_k : a.x_v;
+    void* dst = const_cast<void*>(grp == 0 ? a.own_k : a.own_v);
+    *(u32x4*)((T*)dst + to) = *(const u32x4*)((const T*)src + from);
+  }
+}
+
 constexpr int kManyRows = 1024;  // most rows whose many parts are split over threads
 
 template <typename T, bool HALF>
@@ -224,6 +313,16 @@ hipError_t launch_prompt_merge(const PromptArgs& a, hipStream_t s) {
     if (few) hipLaunchKernelGGL((prompt_merge_kernel<float, false, 4>), grid, block, 0, s, a, log2);
     else hipLaunchKernelGGL((prompt_merge_kernel<float, false, 8>), grid, block, 0, s, a, log2);
   }
+  return hipGetLastError();
+}
+
+hipError_t launch_prefix_merge(const PrefixArgs& a, hipStream_t s) {
+  const dim3 grid((a.batch * a.n_q_heads * a.n_q + 3) / 4), block(256);
+  const bool wide = a.head_dim == 128;
+  if (a.bf16 && wide) hipLaunchKernelGGL((prefix_merge_kernel<bf16_t, true, 128>), grid, block, 0, s, a);
+  else if (a.bf16) hipLaunchKernelGGL((prefix_merge_kernel<bf16_t, true, 64>), grid, block, 0, s, a);
+  else if (wide) hipLaunchKernelGGL((prefix_merge_kernel<float, false, 128>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((prefix_merge_kernel<float, false, 64>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
