@@ -97,7 +97,7 @@ struct Smem {
   uint32_t rows[ROWS];      // store position of each key group of a window of tiles (kNoRow: skipped entry)
   int32_t sidx[kSelLds];    // the lookup row (its first kSelLds entries)
   int32_t sel_ok;           // whether the first wave's select wrote it
-  uint8_t kvalid[NBUF][KB];
+  uint8_t kvalid[4][KB];    // by tile, also where there are two buffers
 };
 
 // Publish LDS tiles to the workgroup: wait until at most N of this wave's
@@ -158,6 +158,12 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
     asm volatile("" ::"s"(a.mem_len), "s"(a.parts_mem), "s"(a.rope.on), "s"(a.var.on), "s"(a.d_row_tiles.mul),
                  "s"(a.d_parts.mul), "s"(a.d_kv.mul), "s"(a.d_group.mul), "s"(a.d_block.mul), "s"(a.sel_scores),
                  "s"(a.sel_stride));
+  }
+  if constexpr (kPrompt) {
+    asm volatile("" ::"s"(a.n_seqs), "s"(a.n_kv_heads), "s"(a.q_tok), "s"(a.q_head), "s"(a.kv_tok), "s"(a.kv_head),
+                 "s"(a.q), "s"(a.k), "s"(a.v), "s"(a.parts), "s"(a.part_tiles), "s"(a.split_tiles));
+    asm volatile("" ::"s"(a.d_group.d), "s"(a.d_group.mul), "s"(a.d_kv.d), "s"(a.d_kv.mul), "s"(a.full_begin[0]),
+                 "s"(a.full_begin[1]), "s"(a.rest_begin[0]), "s"(a.full[0]), "s"(a.sm_scale));
   }
   const int G = (int)a.d_group.d;
   int R, rt, bg, part, b, g;
@@ -380,7 +386,17 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
     h -= wrap ? G : 0;
     i += wrap ? 1 : 0;
   };
-  if (active && t_begin < t_end) {
+  // Four waves take them into registers: the first tile's values are then requested with
+  // its keys, and not once the rows have left their buffers (a trip to memory of the two
+  // that a workgroup of few tiles waits for).
+  bf16x8 qreg[KSTEPS];
+  if constexpr (!kPairs) {
+    if (active && t_begin < t_end) {
+      const bf16_t* qp = (const bf16_t*)a.q + query_at(qi, qh - g * G) + 8 * gsel;
+#pragma unroll
+      for (int s = 0; s < KSTEPS; ++s) qreg[s] = *(const bf16x8*)(qp + 16 * s);
+    }
+  } else if (active && t_begin < t_end) {
     // within the kv head's query rows 32-bit byte offsets do, unless the heads lie
     // very far apart
     const bf16_t* qg = (const bf16_t*)a.q;
@@ -531,7 +547,11 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
   struct TileOff {
     uint32_t o[NI];
   };
+  // (With four waves a lane's rows, granules and table places of four loads, held through
+  // the loop, do not fit the registers: they are formed for each tile.)
+  auto first_lrow = [&]() { return kPairs || kPrompt ? lrow0 : (int)opaque_v((uint32_t)lrow0); };
   auto row_read = [&](int tile, uint32_t (&e)[NI]) {
+    const int lrow0 = first_lrow();
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       if constexpr (kPrompt) {  // the keys are one run: no table
@@ -543,6 +563,7 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
     }
   };
   auto row_off = [&](const uint32_t (&e)[NI], TileOff& f) {
+    const int lrow0 = first_lrow();
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       const uint32_t r = (uint32_t)(lrow0 + RPI * j);
@@ -612,7 +633,6 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
   // a lane takes one granule of one query and turns it for all of the query's heads,
   // so that each angle's sine and cosine are formed once (per row and lane they took
   // 4.5 us of a local part's prologue).
-  bf16x8 qreg[KSTEPS];
   auto read_q = [&]() {
     if (remap) {
       const int gr = lane % CH, r_end = min(row0 + 32, R);
@@ -849,6 +869,7 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
       off2 = off3;
       row_read(t + 3, e3);
       row_off(e3, off3);
+      note_valid((t - t_begin + 3) & 3, e3);
     }
   };
   // One tile's step: FIRST of the pair (issues the pair's loads) or second (forms
@@ -936,16 +957,18 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int j4 = 0; j4 < 4; ++j4)
-            kv[j4][kb] = *(const uint32_t*)&sm.kvalid[bn][32 * kb + 8 * j4 + 4 * gsel];
+            kv[j4][kb] = *(const uint32_t*)&sm.kvalid[kPairs ? bn : (t - t_begin + 1) & 3][32 * kb + 8 * j4 + 4 * gsel];
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         if constexpr (!kPairs) {
+          // (the flags of tile t+3 are noted at once: four places, two barriers before they are read)
           if (j == 0) {
             off2 = off3;
             row_read(t + 3, e3);
           } else if (j == 2) {
             row_off(e3, off3);
+            note_valid((t - t_begin + 3) & 3, e3);
           }
         } else if constexpr (!FIRST) {
           // the next pair's load offsets: V(t+3) .. of this pair's last K tile, then
@@ -1008,8 +1031,6 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
       if constexpr (kPairs) {
         note_valid((t - t_begin + 3) % NBUF, e3);
         note_valid((t - t_begin) % NBUF, e4);
-      } else {
-        note_valid((t - t_begin) % NBUF, e3);
       }
     }
     if constexpr (kPrompt) {
@@ -1049,6 +1070,10 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
     }
 #pragma unroll
     for (int j = 0; j < NI; ++j) load_k(0, off0, j);
+    if constexpr (!kPairs) {
+#pragma unroll
+      for (int j = 0; j < NI; ++j) load_v(0, off0, j);
+    }
     if constexpr (!kPrompt) {
       fill_rows(t_begin);
       lds_barrier();
@@ -1072,6 +1097,7 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
         off2 = off1;
         row_off(e3, off3);
         note_valid(1, e1);
+        note_valid(2, e3);
       }
     }
 #pragma unroll
@@ -1080,13 +1106,15 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
 #pragma unroll
       for (int j = 0; j < NI; ++j) load_k(2, off2, j);
     }
-    // the query rows and K(t0) have landed ("memory": the reads of the rows stay behind it)
-    asm volatile("s_waitcnt vmcnt(%0)" : : "n"((kPairs ? 2 : 1) * NI) : "memory");
-    if (active) read_q();
+    // the query rows and K(t0) have landed ("memory": the reads of the rows stay behind it);
+    // in flight: K(t0+1) and K(t0+2), or V(t0) and K(t0+1)
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * NI) : "memory");
+    if constexpr (kPairs)
+      if (active) read_q();
     lds_barrier();  // K(t0) published, the query rows read
-#pragma unroll
-    for (int j = 0; j < NI; ++j) load_v(0, off0, j);
     if constexpr (kPairs) {
+#pragma unroll
+      for (int j = 0; j < NI; ++j) load_v(0, off0, j);
 #pragma unroll
       for (int j = 0; j < NI; ++j) load_v(1, off1, j);
     }
@@ -1318,13 +1346,15 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
     return nullptr;
   };
   if constexpr (!kStep) {
-    if (row_ok && gsel == 0) {
-      int64_t at = partial_row(qi, qh - g * G);
+    // (the row's place is formed again rather than held through the loop)
+    const int r = (int)opaque_v((uint32_t)row), i = div_by(min(r, R - 1), a.d_group), h = r - i * G;
+    if (row0 < R && r < R && gsel == 0) {
+      int64_t at = partial_row(i, h);
       if (!one_part) {
         a.part_lse[at] = lse_v;
         a.part_exp[at] = ex;
       } else if (a.lse != nullptr) {
-        if constexpr (kPrompt) at = qh * a.lse_stride + seq_start + qi;
+        if constexpr (kPrompt) at = (g * G + h) * a.lse_stride + seq_start + i;
         a.lse[at] = lse_v;
       }
     }
@@ -1356,6 +1386,11 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
       hstride = one_part ? a.out_head_stride * 2 : (int64_t)geo.n_q * kRowBytes;
     }
     int i = li0, h = lh0;
+    if constexpr (!kStep) {
+      const int r = (int)opaque_v((uint32_t)(row0 + lane / CH));
+      i = div_by(r, a.d_group);
+      h = r - i * G;
+    }
 #pragma unroll
     for (int k = 0; k < 32 * CPR / 64; ++k) {
       const int r = RPI * k + lane / CH, ch = lane % CH;

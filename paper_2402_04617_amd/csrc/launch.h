@@ -287,19 +287,36 @@ __device__ __forceinline__ int prompt_part_count(const PromptArgs& a, int p) {
 __host__ inline int64_t prompt_partial_rows(const PromptArgs& a) {
   return a.parts > 1 ? (int64_t)a.rest_begin[a.parts - 1] * a.n_kv_heads * 32 * a.row_waves : 0;
 }
-// Row tile number t (uniform over the wave).
+// Row tile number t (uniform over the wave).  Every lane reads its sequences' entries at
+// once, so that one trip to memory serves the search and what it leads to.
 __device__ __forceinline__ PromptTile prompt_tile(const PromptArgs& a, int t, int rows_log2) {
-  int i = 1;
-  if (a.n_seqs > 1) {
-    i = 0;
-    const int lane = threadIdx.x & 63;
-    for (int j = 0; j < a.n_seqs; j += kWave)
-      i += __popcll(__ballot(j + lane < a.n_seqs && a.first[j + lane < kMaxPrompts ? j + lane : 0] <= t));
-    i = __builtin_amdgcn_readfirstlane(i);
+  constexpr int CH = kMaxPrompts / kWave;
+  const int lane = threadIdx.x & 63;
+  int first[CH], len[CH], start[CH];
+#pragma unroll
+  for (int j = 0; j < CH; ++j) {
+    if (j * kWave >= a.n_seqs) break;
+    first[j] = a.first[j * kWave + lane];
+    len[j] = a.len[j * kWave + lane];
+    start[j] = a.start[j * kWave + lane];
   }
-  const int u = t - a.first[i - 1], down = u / i, s = u - down * i;
-  const int rows = a.len[i - 1] * (int)a.d_group.d;
-  return PromptTile{a.start[s], a.len[s], ((rows - 1) >> rows_log2) - down};
+  int i = 0;  // sequences with tiles on the level of t
+#pragma unroll
+  for (int j = 0; j < CH; ++j) {
+    if (j * kWave >= a.n_seqs) break;
+    i += __popcll(__ballot(j * kWave + lane < a.n_seqs && first[j] <= t));
+  }
+  i = __builtin_amdgcn_readfirstlane(i);
+  auto pick = [&](const int (&x)[CH], int s) {
+    int v = __builtin_amdgcn_readlane(x[0], s & 63);
+#pragma unroll
+    for (int j = 1; j < CH; ++j)
+      if (s >> 6 == j) v = __builtin_amdgcn_readlane(x[j], s & 63);
+    return v;
+  };
+  const int u = t - pick(first, i - 1), down = u / i, s = u - down * i;
+  const int rows = pick(len, i - 1) * (int)a.d_group.d;
+  return PromptTile{pick(start, s), pick(len, s), ((rows - 1) >> rows_log2) - down};
 }
 hipError_t launch_prompt(const PromptArgs& a, hipStream_t s);
 hipError_t launch_prompt_merge(const PromptArgs& a, hipStream_t s);
