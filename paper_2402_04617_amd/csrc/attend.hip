@@ -54,6 +54,15 @@ constexpr int kF32Sel = 2048;  // lookup entries kept in LDS
 // With the positional remap (ROPE) a wave holds both forms of its query rows; a tile
 // of memory keys takes the one at distance l_L, a tile of local keys the other, and
 // the tile that holds both kinds takes both and picks per key.
+// e^x for x <= 0 (and NaN): 2^t (1 + r ln 2) with t = x log2(e) rounded and r what the
+// rounding lost, within 2 units in the last place; -inf is met as -150, which underflows.
+__device__ __forceinline__ float exp_of(float x) {
+  x = x < -150.f ? -150.f : x;
+  const float t = x * 1.44269502f;
+  const float r = __builtin_fmaf(x, 1.92596299e-8f, __builtin_fmaf(x, 1.44269502f, -t));
+  const float e = __builtin_amdgcn_exp2f(t);
+  return __builtin_fmaf(e, r * 0.693147182f, e);
+}
 // Waves of the kernel on a SIMD.  Prompts and the prefix attention at D = 64 run two, at
 // half the registers (222 to 230): one's softmax overlaps the other's products.
 constexpr int f32_waves_per_simd(int head_dim, int waves, bool step) { return head_dim == 64 && waves > 1 && !step ? 2 : 1; }
@@ -275,6 +284,22 @@ attend_f32_kernel(Args a) {
     return sum;
   };
 
+  // some row's maximum grows (the first visible tile included)
+  auto raise_max = [&](float mx) {
+    const float m_new = fmaxf(m, mx);
+    const float corr = m_new == -__builtin_inff() ? 1.f : expf(m - m_new);
+    m = m_new;
+    l *= corr;
+#pragma unroll
+    for (int db = 0; db < DBLK; ++db)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) o[db][j] *= corr;
+  };
+  // Last key that every row of the wave sees (none where unit entries may be skipped).
+  int seen_by_all = -1;
+  if constexpr (!kStep)
+    if (geo.n_sel == 0) seen_by_all = no_causal ? geo.n_virtual - 1 : v_x0 + min(R - 1, rt * RW + wave * 32) / G;
+
   if (t_begin < t_end) {
     __syncthreads();  // sidx
     find_keys(t_begin);
@@ -306,6 +331,40 @@ attend_f32_kernel(Args a) {
     } else {
       s = scores(ks[buf], qv);
     }
+    typedef float vfrag_t __attribute__((ext_vector_type(DBLK)));
+    auto value_row = [&](int r, int d0) {
+      return *(const vfrag_t*)(vs[buf] + r * D + 4 * ((d0 >> 2) ^ (r & 15)) + (d0 & 3));
+    };
+    auto values = [&](int j) { return value_row(8 * (j >> 2) + 4 * gsel + (j & 3), DBLK * n); };  // this lane's dims
+    // A tile that every row of the wave sees: no mask, the scale within the exponential's
+    // argument.  The float32 products and the vector ALU's instructions do not overlap on a
+    // SIMD (8,000 tokens: the matrix cores busy 60 % of the cycles, the vector ALU 32 %),
+    // so that each of the 540 of a tile's 64 products counts.
+    if constexpr (!kStep) {
+      if ((t + 1) * KT - 1 <= seen_by_all) {
+        float mx = s[0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) mx = fmaxf(mx, s[j]);
+        const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+        mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * a.sm_scale;
+        if (__ballot(mx > m)) raise_max(mx);
+        const float base = m == -__builtin_inff() ? 0.f : m;
+        float ls[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          s[j] = exp_of(__builtin_fmaf(s[j], a.sm_scale, -base));
+          ls[j & 1] += s[j];
+        }
+        l += ls[0] + ls[1];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const vfrag_t vf = values(j);
+#pragma unroll
+          for (int db = 0; db < DBLK; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[db], s[j], o[db], 0, 0, 0);
+        }
+        continue;
+      }
+    }
     // mask and the tile's maximum (both lane halves of a row)
     const int lim = vlim - t * KT - 4 * gsel;
     float mx = -__builtin_inff();
@@ -324,16 +383,7 @@ attend_f32_kernel(Args a) {
     }
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
     mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-    if (__ballot(mx > m)) {  // some row's maximum grows (the first visible tile included)
-      const float m_new = fmaxf(m, mx);
-      const float corr = m_new == -__builtin_inff() ? 1.f : expf(m - m_new);
-      m = m_new;
-      l *= corr;
-#pragma unroll
-      for (int db = 0; db < DBLK; ++db)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) o[db][j] *= corr;
-    }
+    if (__ballot(mx > m)) raise_max(mx);
     const float base = m == -__builtin_inff() ? 0.f : m;
     float ls[2] = {0.f, 0.f};
 #pragma unroll
@@ -342,15 +392,10 @@ attend_f32_kernel(Args a) {
       ls[j & 1] += s[j];
     }
     l += ls[0] + ls[1];
-    typedef float vfrag_t __attribute__((ext_vector_type(DBLK)));
-    auto value_row = [&](int r, int d0) {
-      return *(const vfrag_t*)(vs[buf] + r * D + 4 * ((d0 >> 2) ^ (r & 15)) + (d0 & 3));
-    };
     auto add_keys = [&](int j, const vfrag_t& vf) {
 #pragma unroll
       for (int db = 0; db < DBLK; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[db], s[j], o[db], 0, 0, 0);
     };
-    auto values = [&](int j) { return value_row(8 * (j >> 2) + 4 * gsel + (j & 3), DBLK * n); };  // this lane's dims
     if (__ballot(seen != 0xFFFFu) == 0) {
 #pragma unroll
       for (int j = 0; j < 16; ++j) add_keys(j, values(j));
