@@ -353,8 +353,8 @@ infllm_status infllm_step_varlen(const infllm_params* p, const infllm_memory* m,
  * tokens in all.  For token i of a sequence and query head h (kv head g = h / G):
  * one softmax of sm_scale * q_i . k_t over the tokens t <= i of the same sequence.
  * This is the step's attention for prompts that fit the window (nothing evicted),
- * for all of them in one launch (256 sequences that are not empty; more take one
- * launch for every 256).  Of the params only the heads, head_dim, dtype and
+ * for all of them in one launch, or two where the keys of the longest are split
+ * (more than 256 sequences that are not empty: for every 256).  Of the params only the heads, head_dim, dtype and
  * sm_scale matter.
  *  q, k, v, out: dtype rows of head_dim elements; the row of token t and head h
  *     starts at t * token_stride + h * head_stride elements (k and v share their
@@ -364,8 +364,9 @@ infllm_status infllm_step_varlen(const infllm_params* p, const infllm_memory* m,
  *  lse: optional [Hq][total] float32 natural log-sum-exp of the logits.
  *  workspace: infllm_prompt_workspace_bytes(p, n_seqs, seq_lens) bytes, which may
  *     be 0 (then NULL is allowed).
- * Rows past `total` are neither read nor written.  E_UNSUPPORTED where total * G
- * exceeds 2^31 - 1, or for bf16 a sequence's keys span more than 4 GiB. */
+ * Rows past `total` are neither read nor written.  E_UNSUPPORTED where the work
+ * exceeds 32-bit numbers (total * G past 2^31 - 1, or some 2^32 / 512 row tiles of all
+ * heads), or for bf16 a sequence's keys span more than 4 GiB. */
 size_t infllm_prompt_workspace_bytes(const infllm_params* p, int32_t n_seqs, const int32_t* seq_lens);
 infllm_status infllm_prompt_attend(const infllm_params* p, int32_t n_seqs, const int32_t* seq_lens, const void* q,
                                    int64_t q_token_stride, int64_t q_head_stride, const void* k, const void* v,
@@ -410,7 +411,8 @@ infllm_status infllm_prefix_score(const infllm_params* p, const infllm_memory* p
  *  out, lse: as in infllm_chunk_attend ([batch][Hq], n_q rows each).
  * The two stores must not overlap where X is written.  E_RANGE if prefix_len or an
  * own_lens[b] + n_q exceeds its capacity.  For bf16 a [capacity][D] slice of either
- * store spans at most 4 GiB (else E_UNSUPPORTED). */
+ * store spans at most 4 GiB (else E_UNSUPPORTED, as
+ * for more than some 67 million rows batch * Hq * n_q). */
 infllm_status infllm_prefix_attend(const infllm_params* p, const infllm_memory* prefix, int64_t prefix_len,
                                    const infllm_memory* own, const int64_t* own_lens, const void* q,
                                    int64_t q_head_stride, const void* k, const void* v, int64_t kv_head_stride,

@@ -25,6 +25,9 @@ infllm_status check_strided(const infllm_params* p, const void* ptr, int64_t tok
 
 int key_tile(bool bf16) { return bf16 ? 64 : 32; }
 
+// Whether a launch of so many workgroups stays within 2^32 threads.
+bool launchable(int64_t wgs, int threads) { return wgs < (int64_t)(0xFFFFFFFFull / (uint64_t)threads); }
+
 // Workgroups that run at a time: the bf16 kernel's by their LDS, the float32 kernel's by
 // their registers.
 int resident_wgs(const infllm_params* p, int row_waves) {
@@ -228,8 +231,10 @@ infllm_status infllm_prompt_attend(const infllm_params* p, int32_t n_seqs, const
   int launches = 0;
   int64_t at = 0;
   size_t need = 0;
-  for (int i = 0; prompt_next(p, n_seqs, seq_lens, &i, &at, &a); ++launches)
+  for (int i = 0; prompt_next(p, n_seqs, seq_lens, &i, &at, &a); ++launches) {
     need = std::max(need, (size_t)prompt_partial_rows(a) * part_row_bytes(p));
+    if (!launchable((int64_t)a.items * p->n_kv_heads, 64 * a.row_waves)) return INFLLM_E_UNSUPPORTED;
+  }
   if (need > 0) {
     if (workspace == nullptr || workspace_bytes < need) return INFLLM_E_WORKSPACE;
     if (!aligned16(workspace)) return INFLLM_E_SHAPE;
@@ -458,6 +463,10 @@ infllm_status infllm_prefix_attend(const infllm_params* p, const infllm_memory* 
   const bool merge_x = k != nullptr && n_q <= kPrefixMergeTokens;
   prefix_parts(p, B, n_q, own_lens, own_most + (merge_x ? 0 : n_q), &r);
   const int parts = r.parts_s + r.parts_u + r.parts_o;
+  if (!launchable((int64_t)p->n_kv_heads * ((int64_t)r.tiles_s * r.parts_s + (int64_t)B * r.tiles_p * (r.parts_u + r.parts_o)),
+                  64 * r.row_waves) ||
+      !launchable(((int64_t)B * p->n_q_heads * n_q + 3) / 4, 256))
+    return INFLLM_E_UNSUPPORTED;
   const bool direct = parts == 1 && !merge_x;
   if (parts > 0 && !direct) {
     if (workspace == nullptr || workspace_bytes < attend_ws_bytes(p, B, n_q, parts)) return INFLLM_E_WORKSPACE;

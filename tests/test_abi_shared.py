@@ -114,6 +114,8 @@ def test_prefix_attend_refusals(L):  # noqa: F811
     assert call(wb=2 * 3 * 32 * 2 * 264) == WORKSPACE     # two parts' rows: three regions need three
     assert call(ws=FAKE + 4) == SHAPE
     assert call(n_q=0) == 0
+    wide = mem(batch=3, capacity=1 << 24)                 # 3 * 32 * 2^23 rows in all
+    assert call(own=ctypes.byref(wide), n_q=1 << 23, qs=128 << 23, kvs=128 << 23, os=128 << 23) == UNSUPPORTED
     far = mem(capacity=1 << 25)
     assert call(m=ctypes.byref(far)) == UNSUPPORTED       # 2^25 rows of 256 bytes: past 4 GiB
     pr = P(rope_inv_freq=F.rope_frequencies(128))

@@ -125,6 +125,9 @@ def params(Hq, Hkv, D, dtype, local=256, init=16, block=64, topk=3):
     ("bf16", 32, 8, 128, dict(local=1024, init=128, block=128, topk=8), 16, 4, 8000, tuple(40 * i for i in range(16)), {}),
     ("bf16", 4, 4, 128, {}, 1, 1, 1, (0,), {}),
     ("bf16", 4, 2, 128, {}, 2, 3, 0, (0, 70), {}),                       # no document at all
+    ("bf16", 4, 2, 64, {}, 2, 2, 0, (0, 0), {}),                         # and nothing of their own: X alone
+    ("bf16", 4, 2, 128, {}, 3, 8, 900, (0, 0, 0), {}),                   # the most tokens that the merge meets
+    ("bf16", 4, 2, 128, {}, 3, 9, 900, (0, 5, 64), dict(q_pad=1)),       # one more
     ("bf16", 4, 2, 128, dict(topk=0), 2, 1, 2000, (5, 6), {}),            # I and L alone
     ("bf16", 4, 2, 128, {}, 3, 200, 1500, (0, 300, 17), dict(q_pad=1)),   # chunks
     ("bf16", 4, 2, 128, {}, 2, 2, 2000, (10, 20), dict(idx="none", given=False)),
@@ -132,6 +135,8 @@ def params(Hq, Hkv, D, dtype, local=256, init=16, block=64, topk=3):
     ("f32", 8, 2, 128, dict(block=37, init=5, local=100), 3, 5, 1111, (64, 0, 130), dict(idx="some", q_pad=1)),
     ("f32", 3, 1, 64, dict(topk=0, local=5000), 20, 2, 901, tuple(range(20)), dict(given=False)),
     ("f32", 4, 2, 64, {}, 2, 90, 0, (0, 70), {}),
+    ("f32", 4, 2, 128, {}, 2, 8, 500, (0, 0), {}),
+    ("f32", 2, 1, 64, {}, 1, 1, 0, (0,), {}),
 ])
 def test_prefix_parity(dtype, Hq, Hkv, D, kw, B, n_q, length, own, more):
     log(f"[prefix] {dtype} {Hq}/{Hkv} D={D} {kw} B={B} n_q={n_q} length={length} {more}")

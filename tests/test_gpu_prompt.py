@@ -102,6 +102,26 @@ def test_prompt_many_sequences(dtype):
     verify(lens, views, out, lse, 4, 2, "tokens", dtype, 0.125)
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,lens", [
+    ("bf16", 4, 1, 128, (4000,)), ("bf16", 2, 2, 64, (3000, 2999, 64, 1)), ("bf16", 8, 1, 128, (0, 1500, 1400, 7)),
+    ("f32", 4, 1, 128, (900, 33)), ("f32", 2, 1, 64, (2000, 1999)),
+])
+def test_prompt_split_keys(dtype, Hq, Hkv, D, lens):
+    """Prompts whose longest row tiles are split along the keys, without an lse as well."""
+    log(f"[prompt] {dtype} {Hq}/{Hkv} D={D} {lens} split")
+    p = F.params(Hq, Hkv, D, 0, 4096, 128, 4, 0, dtype, sm_scale=D ** -0.5)
+    assert F.infllm_prompt_workspace_bytes(p, lens) > 0
+    q, k, v, out, qs, ks, os, views = make(lens, Hq, Hkv, D, dtype, "tokens")
+    lse = attend(p, lens, q, k, v, out, qs, ks, os)
+    verify(lens, views, out, lse, Hq, Hkv, "tokens", dtype, D ** -0.5)
+    again = torch.full_like(out, 7.0)
+    ws = torch.empty(F.infllm_prompt_workspace_bytes(p, lens), dtype=torch.uint8, device="cuda")
+    F.infllm_prompt_attend(p, lens, q, qs, k, v, ks, again, os, None, ws)
+    assert torch.equal(again, out)
+    with pytest.raises(F.InfllmError):
+        F.infllm_prompt_attend(p, lens, q, qs, k, v, ks, again, os, None, ws, workspace_bytes=ws.numel() - 256)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_prompt_steep_scores(dtype):
     """Scores of some hundreds: one key takes nearly all of a row, and the running maximum moves by jumps."""
