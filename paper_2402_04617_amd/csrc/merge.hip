@@ -233,7 +233,8 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixArgs a) {
   }
   float M, tot, acc[DPT];
   if (a.parts <= CH * GR) join_parts<HALF, CH, true>(m, row, c, grp, GR, M, tot, acc);
-  else join_parts<HALF, 2 * CH, false>(m, row, c, grp, GR, M, tot, acc);
+  else if (a.parts <= 2 * CH * GR) join_parts<HALF, 2 * CH, true>(m, row, c, grp, GR, M, tot, acc);
+  else join_parts<HALF, 3 * CH, false>(m, row, c, grp, GR, M, tot, acc);
   if (a.x_k != nullptr) {
     static_assert(kPrefixMergeTokens <= CH * GR, "every token has a place");
     float z[CH];
