@@ -9,6 +9,7 @@
 #include <cstring>
 
 #include "abi_util.h"
+#include "shared.h"
 
 using namespace infllm;
 

@@ -6,7 +6,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "launch.h"
+#include "shared.h"
 
 namespace infllm {
 

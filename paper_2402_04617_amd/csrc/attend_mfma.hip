@@ -21,7 +21,7 @@
 //                  accumulator layout gives P^T.
 #include <type_traits>
 
-#include "launch.h"
+#include "shared.h"
 #include "topk_select.h"
 
 namespace infllm {

@@ -6,7 +6,7 @@
 // (2,048 pieces of 16 bytes, eight loads per thread in flight), and stores them to every
 // copy of it.  One launch for all arrays and pairs: the blocks of a source run through
 // its K, V (and rotated K) rows, then its rings, key sums and representatives.
-#include "launch.h"
+#include "shared.h"
 
 namespace infllm {
 namespace {

@@ -9,7 +9,7 @@
 // least half as many as a workgroup has groups: a workgroup per row, its threads split into groups that take every GR-th part and are
 // joined in LDS -- the parts are then the only parallelism (25 parts of 32 rows: 6.8 us
 // one thread per piece, 4.3 split; 16 parts of 2,048 rows: 3.7 and 6.5).
-#include "launch.h"
+#include "shared.h"
 
 namespace infllm {
 namespace {
