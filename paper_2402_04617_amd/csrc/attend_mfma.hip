@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
   // Whether a tile this workgroup loads (its own and those issued ahead, [t_begin,
   // t_end + 7)) may hold unit keys; only then does it need the lookup.
   const int u_t0 = geo.n_init / KB, u_t1 = (geo.n_init + geo.n_sel * geo.block_size + KB - 1) / KB;
-  const bool units_here = t_begin < t_end && t_begin < u_t1 && t_end + 7 > u_t0;
+  const bool units_here = t_begin < t_end && t_begin < u_t1 && t_end + 7 > u_t0 && (kStep || geo.n_sel > 0);
   // Lookup inside the attention: such a workgroup selects the units itself; the
   // workgroup of row tile 0 and part 0 always does, and writes the row out (also
   // without units: it is then all -1).  Every entry is valid.
@@ -525,7 +525,14 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
         pos = geo.local_begin + (w - sel_len);
       } else {
         const int u = div_by(w, a.d_block);
-        const int bu = u < kSelLds ? sm.sidx[u] : idx_row[u];
+        int bu;
+        if constexpr (kStep) {
+          bu = u < kSelLds ? sm.sidx[u] : idx_row[u];
+        } else if (geo.n_sel <= kSelLds) {  // (read through one pointer to both, it would wait for every load in flight)
+          bu = sm.sidx[u];
+        } else {
+          bu = idx_row[u];
+        }
         if (bu < 0 || bu >= geo.n_units) return kNoRow;
         pos = (int64_t)geo.unit_base + (int64_t)bu * geo.block_size + (w - u * geo.block_size);
       }
