@@ -559,6 +559,9 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
   auto first_lrow = [&]() { return kPairs || kPrompt ? lrow0 : (int)opaque_v((uint32_t)lrow0); };
   auto row_read = [&](int tile, uint32_t (&e)[NI]) {
     const int lrow0 = first_lrow();
+    // (what runs ahead of the part's end reads its last tile again, from the cache: parts of
+    // four tiles would otherwise read three from memory that they do not use)
+    if constexpr (!kStep) tile = min(tile, t_end - 1);
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       if constexpr (kPrompt) {  // the keys are one run: no table
@@ -1401,6 +1404,8 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
 #pragma unroll
     for (int k = 0; k < 32 * CPR / 64; ++k) {
       const int r = RPI * k + lane / CH, ch = lane % CH;
+      if constexpr (!kStep)
+        if (row0 + RPI * k >= R) break;  // (uniform)
       const u32x4 w = *(const INFLLM_LDS u32x4*)(stage + r * kStageRow + ch * 16);
       if (active && row0 + r < R) {
         if constexpr (kStep) *(u32x4*)(base + h * hstride + (int64_t)i * kRowBytes + ch * 16) = w;
