@@ -50,6 +50,13 @@ bool prompt_sizes(int32_t n_seqs, const int32_t* lens, PromptSizes* r) {
   return true;
 }
 
+// Whether every row tile, part and kv head of such prompts has its number in 32 bits.
+bool prompt_fits(const infllm_params* p, int32_t n_seqs, const PromptSizes& sizes) {
+  const int64_t G = p->n_q_heads / p->n_kv_heads;
+  return sizes.total <= INT32_MAX / G &&
+         (sizes.total * G / 32 + n_seqs) * kMaxPromptParts <= INT32_MAX / p->n_kv_heads;
+}
+
 // Microseconds of a workgroup of the attention kernels, for each tile of keys and beside
 // them (prologue, epilogue): with the whole chip at work, and of one that runs longer than
 // the others (alone on its compute unit, at a higher clock).
@@ -183,7 +190,7 @@ extern "C" {
 size_t infllm_prompt_workspace_bytes(const infllm_params* p, int32_t n_seqs, const int32_t* seq_lens) {
   PromptSizes sizes;
   if (check_params(p) != INFLLM_OK || n_seqs < 0 || (n_seqs > 0 && seq_lens == nullptr) ||
-      !prompt_sizes(n_seqs, seq_lens, &sizes))
+      !prompt_sizes(n_seqs, seq_lens, &sizes) || !prompt_fits(p, n_seqs, sizes))
     return 0;
   PromptArgs a;
   size_t most = 0;
@@ -210,18 +217,18 @@ infllm_status infllm_prompt_attend(const infllm_params* p, int32_t n_seqs, const
   if (!prompt_sizes(n_seqs, seq_lens, &sizes)) return INFLLM_E_SHAPE;
   const int64_t total = sizes.total, longest = sizes.longest;
   if (total == 0) return INFLLM_OK;
-  // (room for every row tile, part and kv head in 32-bit numbers)
-  if (total > INT32_MAX || total * G > INT32_MAX ||
-      (total * G / 32 + n_seqs) * p->n_kv_heads * kMaxPromptParts > INT32_MAX)
-    return INFLLM_E_UNSUPPORTED;
+  if (!prompt_fits(p, n_seqs, sizes)) return INFLLM_E_UNSUPPORTED;
   if ((st = check_strided(p, q, q_token_stride, q_head_stride)) != INFLLM_OK) return st;
   if ((st = check_strided(p, k, kv_token_stride, kv_head_stride)) != INFLLM_OK) return st;
   if ((st = check_strided(p, v, kv_token_stride, kv_head_stride)) != INFLLM_OK) return st;
   if ((st = check_strided(p, out, out_token_stride, out_head_stride)) != INFLLM_OK) return st;
   // two rows of the output never share an element: one stride steps over all of the other's rows
   const int64_t D = p->head_dim;
-  const bool by_head = out_token_stride >= D && (p->n_q_heads == 1 || out_head_stride >= (total - 1) * out_token_stride + D);
-  const bool by_token = out_head_stride >= D && (total == 1 || out_token_stride >= (p->n_q_heads - 1) * out_head_stride + D);
+  auto steps_over = [&](int64_t outer, int64_t inner, int64_t n) {  // outer >= (n - 1) * inner + D, in 64 bits
+    return outer >= D && (n == 1 || inner <= (outer - D) / (n - 1));
+  };
+  const bool by_head = out_token_stride >= D && (p->n_q_heads == 1 || steps_over(out_head_stride, out_token_stride, total));
+  const bool by_token = out_head_stride >= D && (total == 1 || steps_over(out_token_stride, out_head_stride, p->n_q_heads));
   if (!by_head && !by_token) return INFLLM_E_SHAPE;
   // the bf16 kernel addresses the keys of a sequence with 32-bit byte offsets
   if (bf16 && ((uint64_t)kv_token_stride > 0x7FFFFFFFull ||
@@ -286,7 +293,7 @@ struct PrefixPlan {
 
 int64_t key_tiles(const infllm_params* p, int64_t keys) {
   const int kt = key_tile(p->dtype == INFLLM_BF16);
-  return (keys + kt - 1) / kt;
+  return keys / kt + (keys % kt != 0);
 }
 
 // The part counts' bounds follow from the shape alone, so that the workspace does: no
@@ -438,7 +445,7 @@ infllm_status infllm_prefix_attend(const infllm_params* p, const infllm_memory* 
   int64_t own_most = 0;
   for (int b = 0; b < B; ++b) {
     if (own_lens[b] < 0) return INFLLM_E_SHAPE;
-    if (own_lens[b] + n_q > own->capacity) return INFLLM_E_RANGE;
+    if (own_lens[b] > own->capacity - n_q) return INFLLM_E_RANGE;
     own_most = std::max(own_most, own_lens[b]);
   }
   if ((st = check_rows(p, q, q_head_stride, n_q)) != INFLLM_OK) return st;
@@ -456,7 +463,8 @@ infllm_status infllm_prefix_attend(const infllm_params* p, const infllm_memory* 
   if (shared > INT32_MAX || units > INT32_MAX || own_most + n_q > INT32_MAX || G * n_q * B * p->n_kv_heads > INT32_MAX)
     return INFLLM_E_UNSUPPORTED;
   // the bf16 kernel addresses one (sequence, kv head) slice of a store with 32-bit byte offsets
-  if (bf16 && ((uint64_t)prefix->capacity * D * 2u > 0xFFFFFFFFull || (uint64_t)own->capacity * D * 2u > 0xFFFFFFFFull))
+  const int64_t most_rows = (int64_t)(0xFFFFFFFFull / (uint64_t)(2 * D));
+  if (bf16 && (prefix->capacity > most_rows || own->capacity > most_rows))
     return INFLLM_E_UNSUPPORTED;
   if (n_q == 0) return INFLLM_OK;
   PrefixPlan r = prefix_shape(p, B, n_q, shared, units, own->capacity);

@@ -167,6 +167,27 @@ def test_copy_refusals(L):  # noqa: F811
     assert call(p=ctypes.byref(pr)) == NULL                # the remap's rotated keys
 
 
+def test_numbers_past_64_bits(L):  # noqa: F811
+    """Arguments whose products do not fit 64 bits are refused like the ones that do."""
+    D, Hq, Hkv, huge = 128, 32, 8, 1 << 62
+    p, one = P(), P(n_q_heads=1, n_kv_heads=1)
+    prompt = lambda q, lens, ot, oh: L.infllm_prompt_attend(  # noqa: E731
+        ctypes.byref(q), len(lens), lens, FAKE, Hq * D, D, FAKE, FAKE, Hkv * D, D, FAKE, ot, oh, None, None, 0, None)
+    assert prompt(p, i32(1 << 20), huge, huge) == SHAPE       # rows of neither stride step over the other's
+    assert prompt(p, i32(1 << 20), huge >> 10, huge) == SHAPE
+    assert prompt(p, i32(1), huge, 0) == SHAPE                # one token, heads on top of each other
+    assert prompt(one, i32(300), 0, huge) == SHAPE            # one head, tokens on top of each other
+    size = lambda *lens: L.infllm_prompt_workspace_bytes(ctypes.byref(one), len(lens), i32(*lens))  # noqa: E731
+    assert size(*[(1 << 31) - 1] * 3) == 0                    # what the attention refuses has no workspace
+    assert size(4000) > 0                                     # (one head of 4,000 rows leaves most units idle: split)
+    own = mem(batch=1, capacity=(1 << 63) - 1)
+    attend = lambda m, o, n, lens: L.infllm_prefix_attend(  # noqa: E731
+        ctypes.byref(p), ctypes.byref(m), 5, ctypes.byref(o), lens, FAKE, 256, FAKE, FAKE, 256, n, FAKE, 0, FAKE, 256, None, FAKE, BIG, None)
+    assert attend(mem(), own, 2, i64((1 << 63) - 1)) == RANGE
+    assert attend(mem(), own, 2, i64(0)) == UNSUPPORTED       # (bf16: slices past 4 GiB)
+    assert attend(mem(capacity=1 << 56), mem(batch=1, capacity=100), 2, i64(0)) == UNSUPPORTED
+
+
 @pytest.mark.parametrize("lens", [(3,), (1, 2, 3, 4)])
 def test_binding_checks_lengths(L, lens):  # noqa: F811
     own = mem(batch=2, capacity=100)
