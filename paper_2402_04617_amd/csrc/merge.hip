@@ -158,7 +158,8 @@ __global__ void __launch_bounds__(256) merge_many_kernel(MergeArgs a) {
 }
 
 // The split row tiles of packed prompts: workgroups (row tile, kv head, rows of it); a
-// row's parts lie in the items of its row tile.
+// row's parts lie in the items of its row tile.  Bound by the partial rows' bytes and its
+// launch: 14 MB of 52,992 float32 rows of 64 dims 7.7 us.
 template <typename T, bool HALF, int CH>
 __global__ void __launch_bounds__(256) prompt_merge_kernel(PromptArgs a, int rows_log2) {
   constexpr int DPT = HALF ? 8 : 4;
@@ -190,7 +191,11 @@ __global__ void __launch_bounds__(256) prompt_merge_kernel(PromptArgs a, int row
 // The parts of the prefix attention, and its few current tokens.  A wave per row: its
 // 64 / tpr groups of lanes take every GR-th part (the loads of CH of them issued before
 // the first use) and every GR-th current token, and are joined by lane exchanges.  A wave
-// of a group's first head also writes its token's key and value to the own store.
+// of a group's first head also writes its token's key and value to the own store: a few
+// current tokens cost two 16-byte loads a lane here, and no launch of their own nor a part.
+// A row's parts are the only parallelism where rows are few, hence a wave per row.  Bound
+// by latency, the pieces' trip to memory and five exchanges: 128 rows of 26 parts and a
+// current token 5.7 us; 1,024 rows of 48 parts (13 MB) 8.6.
 template <typename T, bool HALF, int D>
 __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixArgs a) {
   constexpr int DPT = HALF ? 8 : 4, TPR = D / DPT, GR = 64 / TPR, CH = 4;
