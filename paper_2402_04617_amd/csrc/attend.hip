@@ -66,7 +66,8 @@ constexpr int f32_waves_per_simd(int head_dim, int waves, bool step) { return he
 // strided rows) or the prefix attention's (one of its regions), without the remap; the
 // mathematics of both stand at attend_mfma_kernel.  Bound by the vector ALU and the matrix
 // cores, whose float32 instructions take turns on a SIMD: 5 prompts up to 1,600 tokens, 8
-// / 2 heads of 64, 70 us with the merge (55 TFLOP/s; a product of 8,192^3 reaches 154).
+// / 2 heads of 64, 67 us with the merge (57 TFLOP/s; a product of 8,192^3 reaches 154):
+// few tiles a wave beside its prologue and epilogue.
 template <int D, int NW, bool ROPE, typename Args = AttendArgs>
 __global__ void __launch_bounds__(64 * NW, f32_waves_per_simd(D, NW, std::is_same_v<Args, AttendArgs>))
 attend_f32_kernel(Args a) {
