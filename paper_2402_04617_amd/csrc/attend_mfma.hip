@@ -1254,8 +1254,47 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
   constexpr int kRowBytes = D * 2;
   constexpr int kStageRow = kRowBytes + 16;  // padded: the 32 rows of a wave spread over the LDS banks
   static_assert(NWAVE * 32 * kStageRow <= (int)sizeof(sm.k) + (int)sizeof(sm.v), "staging fits the tile buffers");
+  // Query row i of head h of the group lies at row_at + i * row_di + h * row_dh (+ c * row_dc
+  // in the shared region, for its continuation c): of the output, in elements, or of the
+  // partial arrays, in rows.
+  int64_t row_at = 0, row_di = 0, row_dh = 0, row_dc = 0;
+  if constexpr (kPrompt) {
+    if (one_part) {
+      row_at = seq_start * a.out_tok + g * G * a.out_head;
+      row_di = a.out_tok;
+      row_dh = a.out_head;
+    } else {  // by the place in the row tile
+      row_at = ((int64_t)prompt_item_of(a, part, prompt_t) * a.n_kv_heads + g - rt) * rows_wg;
+      row_di = G;
+      row_dh = 1;
+    }
+  } else if constexpr (kPrefix) {
+    const int64_t head0 = b * a.n_q_heads + g * G;
+    if (one_part) {
+      row_at = head0 * a.out_head_stride;
+      row_di = D;
+      row_dh = a.out_head_stride;
+      row_dc = a.n_q_heads * a.out_head_stride - (int64_t)a.n_q * D;
+    } else {
+      const int64_t rows_total = (int64_t)a.batch * a.n_q_heads * a.n_q;
+      row_at = (part + prefix_first_part(a, pw.region)) * rows_total + head0 * a.n_q;
+      row_di = 1;
+      row_dh = a.n_q;
+      row_dc = (int64_t)(a.n_q_heads - 1) * a.n_q;
+    }
+  }
+  auto continuation_of = [&](int i) -> int {
+    if constexpr (kPrefix)
+      if (pw.region == 0) return div_by(i, a.d_q);
+    return 0;
+  };
   __syncthreads();  // every wave is done with the tile buffers
-  {
+  // (One branch for all of a wave's pieces.  A step has one for each: without it the compiler
+  // joins the product and its rounding to fp16 in one instruction, rounded once, and a step
+  // is to keep its bits.)
+  auto stage_rows = [&](auto whole_rows) {
+    bool whole = decltype(whole_rows)::value;
+    if constexpr (kStep) whole = one_part;
     INFLLM_LDS char* stage = (INFLLM_LDS char*)(INFLLM_LDS bf16_t*)sm.k[0] + wave * 32 * kStageRow;
 #pragma unroll
     for (int db = 0; db < DBLK; ++db) {
@@ -1265,7 +1304,7 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
         const float o0 = oacc[db][4 * jq] * sc, o1 = oacc[db][4 * jq + 1] * sc;
         const float o2 = oacc[db][4 * jq + 2] * sc, o3 = oacc[db][4 * jq + 3] * sc;
         u32x2 w;
-        if (one_part) {
+        if (whole) {
           w[0] = (uint32_t)f32_to_bf16(o0) | ((uint32_t)f32_to_bf16(o1) << 16);
           w[1] = (uint32_t)f32_to_bf16(o2) | ((uint32_t)f32_to_bf16(o3) << 16);
         } else {
@@ -1275,17 +1314,20 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
         *(INFLLM_LDS u32x2*)(stage + n * kStageRow + d * 2) = w;
       }
     }
-  }
+  };
+  if (kStep || one_part) stage_rows(std::true_type{});
+  else stage_rows(std::false_type{});
   // Values that are not finite must not reach rows that do not see their key: in a masked
   // tile such a value meets P = 0 and leaves a NaN.  A row that came out so is formed again
   // by the wave from the keys it sees, 64 at a time, against its maximum (the scores'
   // sums are right: masked scores never enter them).  Costs the others 64 multiply-adds.
   if constexpr (!kStep) {
-    float z = 0.f;
+    float z4[4] = {};
 #pragma unroll
     for (int db = 0; db < DBLK; ++db)
 #pragma unroll
-      for (int j = 0; j < 16; ++j) z = __builtin_fmaf(oacc[db][j], 0.f, z);
+      for (int j = 0; j < 16; ++j) z4[j & 3] = __builtin_fmaf(oacc[db][j], 0.f, z4[j & 3]);
+    const float z = (z4[0] + z4[1]) + (z4[2] + z4[3]);
     const uint64_t odd = __ballot(row_ok && !(z == 0.f) && l_tot == l_tot);
     uint32_t rows = (uint32_t)odd | (uint32_t)(odd >> 32);
     if (__builtin_expect(rows != 0, 0)) {
@@ -1344,40 +1386,18 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
       }
     }
   }
-  // Row of the partial arrays, and address, of query i of head h: see query_at.
-  int part_id = part;
-  if constexpr (kPrefix) part_id += prefix_first_part(a, pw.region);
-  auto partial_row = [&](int i, int h) -> int64_t {
-    if constexpr (kPrefix) {
-      const int c = pw.region == 0 ? div_by(i, a.d_q) : b;
-      const int64_t rows_total = (int64_t)a.batch * a.n_q_heads * a.n_q;
-      return part_id * rows_total + (int64_t)(c * a.n_q_heads + g * G + h) * a.n_q + (pw.region == 0 ? i - c * a.n_q : i);
-    } else if constexpr (kPrompt) {  // by the place in the row tile
-      return ((int64_t)prompt_item_of(a, part, prompt_t) * a.n_kv_heads + g) * rows_wg + (i * G + h - rt * rows_wg);
-    }
-    return 0;
-  };
-  auto out_row = [&](int i, int h) -> char* {
-    if constexpr (!kStep)
-      if (!one_part) return (char*)a.part_o + partial_row(i, h) * kRowBytes;
-    if constexpr (kPrompt) return (char*)a.out + ((seq_start + i) * a.out_tok + (g * G + h) * a.out_head) * 2;
-    if constexpr (kPrefix) {
-      const int c = pw.region == 0 ? div_by(i, a.d_q) : b;
-      return (char*)a.out + ((int64_t)(c * a.n_q_heads + g * G + h) * a.out_head_stride + (int64_t)(pw.region == 0 ? i - c * a.n_q : i) * D) * 2;
-    }
-    return nullptr;
-  };
   if constexpr (!kStep) {
     // (the row's place is formed again rather than held through the loop)
     const int r = (int)opaque_v((uint32_t)row), i = div_by(min(r, R - 1), a.d_group), h = r - i * G;
     if (row0 < R && r < R && gsel == 0) {
-      int64_t at = partial_row(i, h);
+      const int c = continuation_of(i);
       if (!one_part) {
+        const int64_t at = row_at + i * row_di + h * row_dh + c * row_dc;
         a.part_lse[at] = lse_v;
         a.part_exp[at] = ex;
       } else if (a.lse != nullptr) {
-        if constexpr (kPrompt) at = (g * G + h) * a.lse_stride + seq_start + i;
-        a.lse[at] = lse_v;
+        if constexpr (kPrompt) a.lse[(g * G + h) * a.lse_stride + seq_start + i] = lse_v;
+        else a.lse[(int64_t)((pw.region == 0 ? c : b) * a.n_q_heads + g * G + h) * a.n_q + i - c * a.n_q] = lse_v;
       }
     }
   } else if (row_ok && gsel == 0) {
@@ -1407,23 +1427,52 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
                       : (char*)a.part_o + ((int64_t)part * rows_total + head0 * geo.n_q) * kRowBytes;
       hstride = one_part ? a.out_head_stride * 2 : (int64_t)geo.n_q * kRowBytes;
     }
-    int i = li0, h = lh0;
-    if constexpr (!kStep) {
-      const int r = (int)opaque_v((uint32_t)(row0 + lane / CH));
-      i = div_by(r, a.d_group);
-      h = r - i * G;
-    }
+    constexpr int NP = 32 * CPR / 64;  // pieces of a lane
+    const int r0 = lane / CH, ch = lane % CH;
+    auto piece = [&](int k) { return *(const INFLLM_LDS u32x4*)(stage + (RPI * k + r0) * kStageRow + ch * 16); };
+    if constexpr (kStep) {
+      int i = li0, h = lh0;
 #pragma unroll
-    for (int k = 0; k < 32 * CPR / 64; ++k) {
-      const int r = RPI * k + lane / CH, ch = lane % CH;
-      if constexpr (!kStep)
-        if (row0 + RPI * k >= R) break;  // (uniform)
-      const u32x4 w = *(const INFLLM_LDS u32x4*)(stage + r * kStageRow + ch * 16);
-      if (active && row0 + r < R) {
-        if constexpr (kStep) *(u32x4*)(base + h * hstride + (int64_t)i * kRowBytes + ch * 16) = w;
-        else *(u32x4*)(out_row(i, h) + ch * 16) = w;
+      for (int k = 0; k < NP; ++k) {
+        const u32x4 w = piece(k);
+        if (active && row0 + RPI * k + r0 < R) *(u32x4*)(base + h * hstride + (int64_t)i * kRowBytes + ch * 16) = w;
+        next_row(i, h);
       }
-      next_row(i, h);
+    } else if (active) {
+      // the rows' places stepped in bytes, without a product for each
+      const int64_t unit = one_part ? 2 : kRowBytes, di = row_di * unit, dh = row_dh * unit, dc = row_dc * unit;
+      const int64_t step = step_i * di + step_h * dh, wrap = di - G * dh;
+      const int r = (int)opaque_v((uint32_t)(row0 + r0));
+      int i = div_by(r, a.d_group), h = r - i * G;
+      char* at = (one_part ? (char*)a.out : (char*)a.part_o) + row_at * unit + i * di + h * dh + ch * 16;
+      auto store = [&](const u32x4& w) {
+        if constexpr (kPrefix) *(u32x4*)(at + continuation_of(i) * dc) = w;
+        else *(u32x4*)at = w;
+      };
+      auto next = [&]() {
+        const bool over = h + step_h >= G;
+        at += step + (over ? wrap : 0);
+        i += step_i + (over ? 1 : 0);
+        h += step_h - (over ? G : 0);
+      };
+      if (row0 + 32 <= R) {
+        u32x4 w[NP];
+#pragma unroll
+        for (int k = 0; k < NP; ++k) w[k] = piece(k);
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+          store(w[k]);
+          next();
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+          if (row0 + RPI * k >= R) break;  // (uniform)
+          const u32x4 w = piece(k);
+          if (row0 + RPI * k + r0 < R) store(w);
+          next();
+        }
+      }
     }
   }
 }

@@ -35,8 +35,10 @@ __device__ __forceinline__ void load_piece(const Args& a, int64_t pr, int c, flo
     o[3] = w.w;
   }
 }
-// Adds the first `n` of CH pieces to a running maximum, weight sum and weighted row.
-template <int DPT, int CH>
+// Adds the first `n` of CH pieces to a running maximum, weight sum and weighted row.  ANY:
+// the pieces may hold values that are not finite, which no weight of 0 may meet: it would
+// leave a NaN (the piece of a thread past the last part is that part's again).
+template <int DPT, int CH, bool ANY>
 __device__ __forceinline__ void add_parts(const float (&l)[CH], const float (&o)[CH][DPT], int n, bool rescale, float& M,
                                           float& tot, float (&acc)[DPT]) {
   float m_new = M;
@@ -55,17 +57,15 @@ __device__ __forceinline__ void add_parts(const float (&l)[CH], const float (&o)
     const bool live = j < n && l[j] != -__builtin_inff();
     const float w = live ? expf(l[j] - m_new) : 0.f;
     tot += w;
-    // (no value times 0: one that is not finite would leave a NaN, and the piece of a
-    // thread past the last part is that part's again)
 #pragma unroll
-    for (int e = 0; e < DPT; ++e) acc[e] += w * (live ? o[j][e] : 0.f);
+    for (int e = 0; e < DPT; ++e) acc[e] += w * (!ANY || live ? o[j][e] : 0.f);
   }
   M = m_new;
 }
 // Joins parts first, first + step, ... (every load of CH of them issued before the
 // first use) into a running maximum, weight sum and weighted row.  ONCE: there are at
 // most CH of them.
-template <bool HALF, int CH, bool ONCE>
+template <bool HALF, int CH, bool ONCE, bool ANY = false>
 __device__ __forceinline__ void join_parts(const MergeArgs& a, int row, int c, int first, int step, float& M, float& tot,
                                            float (&acc)[HALF ? 8 : 4]) {
   constexpr int DPT = HALF ? 8 : 4;
@@ -78,7 +78,7 @@ __device__ __forceinline__ void join_parts(const MergeArgs& a, int row, int c, i
 #pragma unroll
     for (int j = 0; j < CH; ++j)
       load_piece<HALF>(a, (int64_t)min(p0 + j * step, a.parts - 1) * a.rows + row, c, o[j], l[j]);
-    add_parts<DPT, CH>(l, o, (a.parts - p0 + step - 1) / step, !ONCE, M, tot, acc);
+    add_parts<DPT, CH, ANY>(l, o, (a.parts - p0 + step - 1) / step, !ONCE, M, tot, acc);
     if (ONCE) break;
   }
 }
@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(256) prompt_merge_kernel(PromptArgs a, int row
       const int64_t pr = (((int64_t)prompt_item_of(a, min(p0 + j, parts - 1), t) * a.n_kv_heads + g) << rows_log2) + r;
       load_piece<HALF>(a, pr, c, o[j], l[j]);
     }
-    add_parts<DPT, CH>(l, o, parts - p0, p0 > 0, M, tot, acc);
+    add_parts<DPT, CH, true>(l, o, parts - p0, p0 > 0, M, tot, acc);
   }
   const int i = div_by(row, a.d_group), h = g * G + row - i * G;
   store_row_piece<T, DPT>((T*)a.out + (pt.start + i) * a.out_tok + h * a.out_head + DPT * c,
@@ -237,9 +237,9 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixArgs a) {
     }
   }
   float M, tot, acc[DPT];
-  if (a.parts <= CH * GR) join_parts<HALF, CH, true>(m, row, c, grp, GR, M, tot, acc);
-  else if (a.parts <= 2 * CH * GR) join_parts<HALF, 2 * CH, true>(m, row, c, grp, GR, M, tot, acc);
-  else join_parts<HALF, 3 * CH, false>(m, row, c, grp, GR, M, tot, acc);
+  if (a.parts <= CH * GR) join_parts<HALF, CH, true, true>(m, row, c, grp, GR, M, tot, acc);
+  else if (a.parts <= 2 * CH * GR) join_parts<HALF, 2 * CH, true, true>(m, row, c, grp, GR, M, tot, acc);
+  else join_parts<HALF, 3 * CH, false, true>(m, row, c, grp, GR, M, tot, acc);
   if (a.x_k != nullptr) {
     static_assert(kPrefixMergeTokens <= CH * GR, "every token has a place");
     float z[CH];
@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixArgs a) {
       // (a NaN score as the attention's parts give it)
       if (grp + j * GR <= i) z[j] = s == s ? s : __builtin_inff();
     }
-    add_parts<DPT, CH>(z, xv, CH, true, M, tot, acc);
+    add_parts<DPT, CH, true>(z, xv, CH, true, M, tot, acc);
   }
   // the groups' shares
 #pragma unroll
