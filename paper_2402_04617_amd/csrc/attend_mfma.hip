@@ -125,12 +125,13 @@ __device__ __forceinline__ void publish_barrier() {
 //    cores bound it.  Measured with the tiles numbered by falling work (D = 128, 32 / 8
 //    heads): 16,000 tokens 1,705 to 1,780 us by card, 1.18 to 1.23 PFLOP/s, where a
 //    product of 8,192^3 reaches 1.25; 20 prompts of 1 to 2,999 tokens 262 us, 0.91
-//    PFLOP/s: 7 to 10 us of each workgroup's prologue and epilogue, and the launch's end.
+//    PFLOP/s: 8 of a workgroup's 24 us on average are prologue (3 its first rows and keys)
+//    and epilogue.
 //  PrefixArgs: the prefix attention: a workgroup has a row tile and a part of one of its
 //    three regions.  The rows of all continuations share the row tiles of I and L, so
 //    that those keys are read once; what looks at a continuation's own units or tokens
 //    reads them at the memory's rate.  32 continuations of one token over 64K tokens, all
-//    of them attended: 62 us, 5.1 TB/s; 4 over 32K with 16 units each 15 us, a chain of
+//    of them attended: 61 us, 5.2 TB/s; 4 over 32K with 16 units each 15 us, a chain of
 //    loads (arguments 1.5, lookup 1.2, first keys 2.3), four tiles (4.8) and the epilogue.
 // NWAVE: 8 waves, one workgroup per compute unit and a barrier per pair of tiles: least
 // LDS traffic per product, for long parts; or 4, two workgroups per compute unit with two
@@ -1439,7 +1440,9 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
         next_row(i, h);
       }
     } else if (active) {
-      // the rows' places stepped in bytes, without a product for each
+      // the rows' places stepped in bytes, without a product for each; whole row tiles
+      // without a branch for each (with both, and a branch for each staged piece, 4 us of a
+      // packed prompt's workgroup: 266 us where it takes 262)
       const int64_t unit = one_part ? 2 : kRowBytes, di = row_di * unit, dh = row_dh * unit, dc = row_dc * unit;
       const int64_t step = step_i * di + step_h * dh, wrap = di - G * dh;
       const int r = (int)opaque_v((uint32_t)(row0 + r0));
