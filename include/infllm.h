@@ -346,7 +346,9 @@ infllm_status infllm_step_varlen(const infllm_params* p, const infllm_memory* m,
  * (E_UNSUPPORTED with params.rope_inv_freq, except infllm_copy_sequences).
  * Values that are not finite stay with the rows that see them: a NaN or infinity
  * in a key, a value or behind a sequence's end changes no row that does not
- * attend it; a NaN among a row's scores makes its output and lse NaN. */
+ * attend it; a NaN among a row's scores makes its output and lse NaN.  Outputs
+ * (out, lse, scores) and workspaces overlap no input and no other call's that may
+ * run at the same time; calls with workspaces of their own may. */
 
 /* Causal attention of whole prompts, packed: n_seqs sequences of seq_lens[i] >= 0
  * tokens (a HOST array, read during the call) lie one after another, `total`
@@ -354,8 +356,8 @@ infllm_status infllm_step_varlen(const infllm_params* p, const infllm_memory* m,
  * one softmax of sm_scale * q_i . k_t over the tokens t <= i of the same sequence.
  * This is the step's attention for prompts that fit the window (nothing evicted),
  * for all of them in one launch, or two where the keys of the longest are split
- * (more than 256 sequences that are not empty: for every 256).  Of the params only the heads, head_dim, dtype and
- * sm_scale matter.
+ * (more than 256 sequences that are not empty: for every 256).  Of the params only
+ * the heads, head_dim, dtype and sm_scale matter.
  *  q, k, v, out: dtype rows of head_dim elements; the row of token t and head h
  *     starts at t * token_stride + h * head_stride elements (k and v share their
  *     strides; strides are multiples of 16 bytes and not negative; the output's
@@ -411,8 +413,8 @@ infllm_status infllm_prefix_score(const infllm_params* p, const infllm_memory* p
  *  out, lse: as in infllm_chunk_attend ([batch][Hq], n_q rows each).
  * The two stores must not overlap where X is written.  E_RANGE if prefix_len or an
  * own_lens[b] + n_q exceeds its capacity.  For bf16 a [capacity][D] slice of either
- * store spans at most 4 GiB (else E_UNSUPPORTED, as
- * for more than some 67 million rows batch * Hq * n_q). */
+ * store spans at most 4 GiB (else E_UNSUPPORTED, as for more than some 67 million
+ * rows batch * Hq * n_q). */
 infllm_status infllm_prefix_attend(const infllm_params* p, const infllm_memory* prefix, int64_t prefix_len,
                                    const infllm_memory* own, const int64_t* own_lens, const void* q,
                                    int64_t q_head_stride, const void* k, const void* v, int64_t kv_head_stride,
