@@ -768,15 +768,22 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
   // (2^16: P stays far inside the float and bf16 range) has met keys well above
   // m_run, and only then is the tile's maximum taken and the row rescaled (a rare
   // path; the decision is wave-uniform, and both lane halves of a row share
-  // m_run).  While a row has seen no visible key (m_run = -inf) any nonzero P
-  // takes that path, so the first visible tile sets m_run.
+  // m_run).  While m_run = -inf (the part began with lookup entries to skip) there is
+  // nothing to form P against, and the weights of a row of low scores would all
+  // underflow: every sum of P is above such a row's bound, so that the maximum of each
+  // tile is looked at until one is finite.  A row that the part's keys are all hidden
+  // from (a later part of X) keeps its -inf, its P are 0.
   constexpr float kLazy = 65536.f;
-  float lazy_bound = 0.f;  // 0 while m_run = -inf
+  auto bound_of = [&](float mx) {  // (formed where it is needed rather than held through the loop)
+    const int last = (int)opaque_v((uint32_t)vlim);
+    return mx != -__builtin_inff() ? kLazy : last < t_begin * KB ? 0.f : -1.f;
+  };
+  float lazy_bound = 0.f;
   float neg_m = 0.f;       // -m_run, 0 while m_run = -inf
   auto first_max = [&](float mx) {  // nothing accumulated yet
     m_run = mx;
     neg_m = (mx == -__builtin_inff()) ? 0.f : -mx;
-    lazy_bound = (mx == -__builtin_inff()) ? 0.f : kLazy;
+    lazy_bound = bound_of(mx);
   };
   auto force_max = [&](float mx) {
     const float m_new = fmaxf(m_run, mx);
@@ -788,7 +795,15 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
       for (int j = 0; j < 16; ++j) oacc[db][j] *= alpha;
     m_run = m_new;
     neg_m = (m_new == -__builtin_inff()) ? 0.f : -m_new;
-    lazy_bound = (m_new == -__builtin_inff()) ? 0.f : kLazy;
+    lazy_bound = bound_of(m_new);
+  };
+  // Whether a row of the wave needs tile `sacc`'s maximum, given its sums of P; takes it then.
+  auto outgrown = [&](float l_tile, const f32x16 (&sacc)[2]) -> bool {
+    if (__ballot(l_tile > lazy_bound) == 0) return false;
+    const float mx = tile_max(sacc);
+    if (__ballot(lazy_bound < 0.f ? mx != -__builtin_inff() : l_tile > lazy_bound) == 0) return false;
+    force_max(mx);
+    return true;
   };
   // Tile t's contribution to the unit masses (MASS): for a tile of the looked-up
   // units (whole tiles: l_I and l_bs are multiples of the tile), the row's sum of
@@ -959,8 +974,7 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
     float l_tile = l_pend + (ps1[0] + ps1[1]);
     // lazy-max check before the tile reaches the matrix cores: on the rare row that
     // exceeds the bound, rescale to the tile's maximum and redo both halves
-    if (__ballot(l_tile > lazy_bound)) {
-      force_max(tile_max(cur));
+    if (outgrown(l_tile, cur)) {
       l_tile = half_p(cur[0], p0);
       l_tile += half_p(cur[1], w1);
     }
@@ -1204,8 +1218,7 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
     // drain: P and PV of the last tile
     u32x4 w1[2];
     float l_tile = l_pend + half_p(sA[1], w1);
-    if (__ballot(l_tile > lazy_bound)) {
-      force_max(tile_max(sA));
+    if (outgrown(l_tile, sA)) {
       l_tile = half_p(sA[0], p0);
       l_tile += half_p(sA[1], w1);
     }
