@@ -21,6 +21,7 @@
 //                  accumulator layout gives P^T.
 #include <type_traits>
 
+#include "row_window.h"
 #include "shared.h"
 #include "topk_select.h"
 
@@ -572,9 +573,7 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
   auto first_lrow = [&]() { return kPairs || kPrompt ? lrow0 : (int)opaque_v((uint32_t)lrow0); };
   auto row_read = [&](int tile, uint32_t (&e)[NI]) {
     const int lrow0 = first_lrow();
-    // (what runs ahead of the part's end reads its last tile again, from the cache: parts of
-    // four tiles would otherwise read three from memory that they do not use)
-    if constexpr (!kStep) tile = min(tile, t_end - 1);
+    if constexpr (!kStep) tile = offsets_tile(tile, t_end);
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       if constexpr (kPrompt) {  // the keys are one run: no table
@@ -905,7 +904,7 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
       row_off(e4, off4);
     } else {
       off2 = off3;
-      row_read(t + 3, e3);
+      row_read(t + kRowsAhead, e3);
       row_off(e3, off3);
       note_valid((t - t_begin + 3) & 3, e3);
     }
@@ -1002,7 +1001,7 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
           // (the flags of tile t+3 are noted at once: four places, two barriers before they are read)
           if (j == 0) {
             off2 = off3;
-            row_read(t + 3, e3);
+            row_read(t + kRowsAhead, e3);
           } else if (j == 2) {
             row_off(e3, off3);
             note_valid((t - t_begin + 3) & 3, e3);
@@ -1078,8 +1077,8 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
         fill_rows(t + 5);
         publish_barrier<0>();
       }
-    } else if (t + 3 >= w0 + window) {
-      fill_rows(t + 3);
+    } else if (window_moves(t, t_end, w0, window)) {
+      fill_rows(t + kRowsAhead);  // (the table's readers are past the barrier)
       publish_barrier<0>();
     }
     // The matrix phases run at raised wave priority: a wave in its MFMA phases
