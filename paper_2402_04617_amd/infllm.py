@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
+from array import array
 from typing import Optional, Tuple
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libinfllm.so")
@@ -250,11 +251,12 @@ def infllm_step_varlen(p, m, q, q_head_stride, k, v, kv_head_stride, n_q, past_l
 
 
 def _i32s(xs):
-    return (ctypes.c_int32 * len(xs))(*xs)
+    """Host integers as a C array; OverflowError where one does not fit (ctypes alone would wrap it)."""
+    return (ctypes.c_int32 * len(xs)).from_buffer(array("i", xs))
 
 
 def _i64s(xs):
-    return (ctypes.c_int64 * len(xs))(*xs)
+    return (ctypes.c_int64 * len(xs)).from_buffer(array("q", xs))
 
 
 def _wb(workspace, workspace_bytes) -> int:
