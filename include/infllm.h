@@ -220,7 +220,8 @@ infllm_status infllm_chunk_attend(const infllm_params* p, const infllm_memory* m
 /* The two halves of infllm_chunk_attend, for callers that time or schedule them
  * apart.  infllm_attend_partial writes per-part normalised outputs and lse into the
  * workspace and reports the part count; infllm_lse_merge combines them
- * (LSE = log sum_s exp(lse_s), O = sum_s exp(lse_s - LSE) O_s) into out / lse.
+ * (LSE = log sum_s exp(lse_s), O = sum_s exp(lse_s - LSE) O_s; a NaN among a row's
+ * lse_s makes both NaN) into out / lse.
  * With one part, infllm_attend_partial writes out and lse directly and
  * infllm_lse_merge must not be called.  Arguments as in infllm_chunk_attend.
  * Workspace layout of the partials (rows = batch*Hq*n_q): [n_parts][rows][D]
@@ -346,7 +347,12 @@ infllm_status infllm_step_varlen(const infllm_params* p, const infllm_memory* m,
  * (E_UNSUPPORTED with params.rope_inv_freq, except infllm_copy_sequences).
  * Values that are not finite stay with the rows that see them: a NaN or infinity
  * in a key, a value or behind a sequence's end changes no row that does not
- * attend it; a NaN among a row's scores makes its output and lse NaN.  Outputs
+ * attend it (beyond its roundings, where the kernel takes both at once); a NaN among
+ * a row's scores makes its output and lse NaN.  Scores, softmax statistics and sums
+ * are float32.  As in the step, the bf16 attentions round each softmax weight to bf16
+ * before it meets the values (by at most 2^-8 of it; the normaliser sums the unrounded
+ * ones) and, where a row's keys are split, each part's row to fp16 relative to its
+ * largest value (2^-11); out is rounded once more.  Outputs
  * (out, lse, scores) and workspaces overlap no input and no other call's that may
  * run at the same time; calls with workspaces of their own may. */
 
@@ -388,7 +394,8 @@ size_t infllm_prefix_workspace_bytes(const infllm_params* p, int32_t batch, int3
  * of a larger memory is a view with its pointers moved), whose key sums are read
  * once for all.  q: [batch][Hq] heads of n_q x D dtype rows; scores:
  * [batch][Hkv][n_units] float32, which infllm_select_topk takes with
- * rows = batch * Hkv.  Uses only unit_ksum and max_units of the memory. */
+ * rows = batch * Hkv.  Uses only unit_ksum and max_units of the memory.
+ * E_UNSUPPORTED for batch * Hkv past 65,535. */
 infllm_status infllm_prefix_score(const infllm_params* p, const infllm_memory* prefix, int32_t batch, const void* q,
                                   int64_t q_head_stride, int32_t n_q, int32_t n_units, float* scores, void* workspace,
                                   size_t workspace_bytes, void* stream);
@@ -399,15 +406,16 @@ infllm_status infllm_prefix_score(const infllm_params* p, const infllm_memory* p
  * tokens of its own (a HOST array) in slot b of `own`, followed by its n_q current
  * tokens X.  For query i of continuation b, head h (kv head g): one softmax of
  * sm_scale * q . k over I, the units idx[b][g][0 .. min(n_idx, n_units)) of the
- * document (entries that are negative or >= n_units are skipped), L, the own tokens,
- * and X up to i.  The keys of I and L are read once for all continuations.  The
+ * document (entries that are negative or >= n_units are skipped, one given twice
+ * counts twice), L, the own tokens, and X up to i.  The keys of I and L are read once for all continuations.  The
  * partition stays that of the document: with n_local >= prefix_len the whole
  * document is attended (n_idx = 0), and tokens of a continuation are not evicted
  * (one that grows past the window is moved to a memory of its own with
  * infllm_copy_sequences).  Of the memories only batch, capacity, k and v are used.
  *  k, v: the current tokens' keys and values, [batch][Hkv] heads of n_q x D rows
- *     with kv_head_stride, written to positions own_lens[b] .. + n_q of `own`
- *     before the attention; both NULL when they are there already.
+ *     with kv_head_stride, which the call also writes to positions own_lens[b] ..
+ *     + n_q of `own` (they are there when it has run, in no order against its own
+ *     reads); both NULL when they are there already.
  *  idx: [batch][Hkv][n_idx] int32 (NULL allowed when nothing is looked up);
  *     n_idx <= params.topk for the workspace of infllm_prefix_workspace_bytes.
  *  out, lse: as in infllm_chunk_attend ([batch][Hq], n_q rows each).
@@ -430,6 +438,8 @@ infllm_status infllm_prefix_attend(const infllm_params* p, const infllm_memory* 
  * to the next infllm_step), and the query rings' slots of the last
  * min(lens[i], src ring, dst ring) positions, so that the copy is continued like its
  * source (a ring smaller than the source's must still be one the next append accepts).
+ * A copy that is to be continued takes the source's whole length: at a shorter one its
+ * K, V and units are right, but the source's rings hold later positions by now.
  * Everything else of the destination is left as it was.  The arrays are HOST arrays.
  * With INFLLM_REPR_MEAN there are no rings and no representatives.
  * E_RANGE: a slot outside its memory, a length beyond a capacity, units beyond a

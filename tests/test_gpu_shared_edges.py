@@ -91,3 +91,42 @@ def test_prompt_bits_beside_bad_values(dtype, what):
     for x, y in ((out, again), (lse, bad)):
         x[group, 100:1600] = y[group, 100:1600] = 0  # (NaN in part, and not equal to itself)
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_units_given_twice(dtype):
+    """An entry that stands in a row twice counts twice."""
+    c = Case(params(4, 2, 64, dtype, topk=6), 3, 2, 1500, (7, 0, 60))
+    c.idx[:, :, 3] = c.idx[:, :, 0]
+    c.idx[1, 0, :] = c.idx[1, 0, 2].clone()
+    log(f"[prefix] {dtype} entries given twice")
+    c.run()
+    c.verify()
+
+
+@pytest.mark.parametrize("dtype,parts,rows", [("bf16", 2, 40), ("bf16", 12, 40), ("f32", 3, 40), ("f32", 20, 2000), ("bf16", 20, 2000)])
+def test_merge_of_nan_parts(dtype, parts, rows):
+    """A part whose lse is NaN makes its row NaN, lse and all; one of -inf is left out."""
+    D, bad, empty = 64, rows // 3, rows // 2
+    p = F.params(1, 1, D, 0, 64, 8, 2, 0, dtype)
+    g = torch.Generator().manual_seed(parts)
+    o = (torch.randn((parts, rows, D), generator=g) * 100).to(torch.float16 if dtype == "bf16" else torch.float32)
+    l = torch.randn((parts, rows), generator=g)
+    l[1, bad] = math.nan
+    l[0, empty] = -math.inf
+    pieces = [o, l] + ([torch.zeros((parts, rows), dtype=torch.int32)] if dtype == "bf16" else [])
+    ws = torch.cat([x.contiguous().view(torch.uint8).flatten() for x in pieces]).cuda()
+    out = torch.empty((1, 1, rows, D), dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, device="cuda")
+    lse = torch.empty((1, 1, rows), device="cuda")
+    log(f"[merge] {dtype} {parts} parts of {rows} rows, a NaN")
+    F.infllm_lse_merge(p, 1, rows, parts, ws, out, rows * D, lse)
+    want = torch.logsumexp(l.double(), 0)
+    w = torch.exp(l.double() - want)
+    ref = (w[:, :, None] * o.double()).sum(0)
+    ref[bad] = want[bad] = math.nan
+    # parts + 8 float32 roundings of sums of weights, exponentials of scores up to 8
+    a = (w[:, :, None] * o.double().abs()).sum(0)
+    half = torch.finfo(out.dtype).eps / 2
+    tol = 2 * (parts + 32) * 2.0 ** -24 * a + half * ref.abs()
+    check("out", out[0, 0], ref, tol.nan_to_num())
+    check("lse", lse[0, 0], want, torch.full((rows,), (parts + 64) * 2.0 ** -24))
