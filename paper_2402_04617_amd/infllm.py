@@ -95,13 +95,12 @@ def lib() -> ctypes.CDLL:
         "infllm_step_varlen": [P, M, vp, i64, vp, vp, i64, i32, ctypes.POINTER(i64), ctypes.POINTER(i32), vp, vp,
                                vp, i64, vp, vp, sz, vp],
         "infllm_unit_mass": [P, M, vp, i64, i32, i64, vp, i32, vp, ctypes.c_float, vp, vp, vp],
-        "infllm_prompt_attend": [P, i32, ctypes.POINTER(i32), vp, i64, i64, vp, vp, i64, i64, vp, i64, i64, vp, vp, sz,
+        "infllm_prompt_attend": [P, i32, vp, vp, i64, i64, vp, vp, i64, i64, vp, i64, i64, vp, vp, sz,
                                  vp],
         "infllm_prefix_score": [P, M, i32, vp, i64, i32, i32, vp, vp, sz, vp],
-        "infllm_prefix_attend": [P, M, i64, M, ctypes.POINTER(i64), vp, i64, vp, vp, i64, i32, vp, i32, vp, i64, vp, vp,
+        "infllm_prefix_attend": [P, M, i64, M, vp, vp, i64, vp, vp, i64, i32, vp, i32, vp, i64, vp, vp,
                                  sz, vp],
-        "infllm_copy_sequences": [P, M, M, i32, ctypes.POINTER(i32), ctypes.POINTER(i32), ctypes.POINTER(i64),
-                                  ctypes.POINTER(i32), vp],
+        "infllm_copy_sequences": [P, M, M, i32, vp, vp, vp, vp, vp],
     }
     for name, args in sig.items():
         f = getattr(L, name)
@@ -111,7 +110,7 @@ def lib() -> ctypes.CDLL:
     L.infllm_workspace_bytes.restype = ctypes.c_size_t
     L.infllm_attend_workspace_bytes.argtypes = [P, i32, i32]
     L.infllm_attend_workspace_bytes.restype = ctypes.c_size_t
-    L.infllm_prompt_workspace_bytes.argtypes = [P, i32, ctypes.POINTER(i32)]
+    L.infllm_prompt_workspace_bytes.argtypes = [P, i32, vp]
     L.infllm_prompt_workspace_bytes.restype = ctypes.c_size_t
     L.infllm_prefix_workspace_bytes.argtypes = [P, i32, i32, i64, i64]
     L.infllm_prefix_workspace_bytes.restype = ctypes.c_size_t
@@ -139,6 +138,8 @@ def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
     import torch
+    # (the raw handle: torch.cuda.current_stream() builds an object around it, 2.7 us a call against 0.3, where the
+    # smallest calls take 7 to 10)
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
@@ -250,13 +251,19 @@ def infllm_step_varlen(p, m, q, q_head_stride, k, v, kv_head_stride, n_q, past_l
         _ptr(scores), _ptr(idx), _ptr(out), out_head_stride, _ptr(lse), _ptr(workspace), wb, _stream(stream)))
 
 
-def _i32s(xs):
-    """Host integers as a C array; OverflowError where one does not fit (ctypes alone would wrap it)."""
-    return (ctypes.c_int32 * len(xs)).from_buffer(array("i", xs))
+def _i32s(xs) -> array:
+    """Host integers for a C array argument (_at gives its address); OverflowError where one does not fit, which
+    ctypes' own arrays would wrap."""
+    return array("i", xs)
 
 
-def _i64s(xs):
-    return (ctypes.c_int64 * len(xs)).from_buffer(array("q", xs))
+def _i64s(xs) -> array:
+    return array("q", xs)
+
+
+def _at(xs: array) -> int:
+    """Address of the numbers; the caller holds the array through the call."""
+    return xs.buffer_info()[0]
 
 
 def _wb(workspace, workspace_bytes) -> int:
@@ -266,14 +273,16 @@ def _wb(workspace, workspace_bytes) -> int:
 
 
 def infllm_prompt_workspace_bytes(p: Params, seq_lens) -> int:
-    return int(lib().infllm_prompt_workspace_bytes(ctypes.byref(p), len(seq_lens), _i32s(seq_lens)))
+    lens = _i32s(seq_lens)
+    return int(lib().infllm_prompt_workspace_bytes(ctypes.byref(p), len(lens), _at(lens)))
 
 
 def infllm_prompt_attend(p, seq_lens, q, q_strides, k, v, kv_strides, out, out_strides, lse=None, workspace=None,
                          workspace_bytes=None, stream=None):
     """seq_lens: lengths (host ints); strides: (token, head) in elements."""
+    lens = _i32s(seq_lens)
     _check("infllm_prompt_attend", lib().infllm_prompt_attend(
-        ctypes.byref(p), len(seq_lens), _i32s(seq_lens), _ptr(q), q_strides[0], q_strides[1], _ptr(k), _ptr(v),
+        ctypes.byref(p), len(lens), _at(lens), _ptr(q), q_strides[0], q_strides[1], _ptr(k), _ptr(v),
         kv_strides[0], kv_strides[1], _ptr(out), out_strides[0], out_strides[1], _ptr(lse), _ptr(workspace),
         _wb(workspace, workspace_bytes), _stream(stream)))
 
@@ -292,22 +301,24 @@ def infllm_prefix_score(p, prefix, batch, q, q_head_stride, n_q, n_units, scores
 def infllm_prefix_attend(p, prefix, prefix_len, own, own_lens, q, q_head_stride, k, v, kv_head_stride, n_q, idx, n_idx,
                          out, out_head_stride, lse=None, workspace=None, workspace_bytes=None, stream=None):
     """own_lens: own.batch host ints."""
-    if len(own_lens) != own.batch:
-        raise ValueError(f"own_lens needs {own.batch} entries, got {len(own_lens)}")
+    lens = _i64s(own_lens)
+    if len(lens) != own.batch:
+        raise ValueError(f"own_lens needs {own.batch} entries, got {len(lens)}")
     _check("infllm_prefix_attend", lib().infllm_prefix_attend(
-        ctypes.byref(p), ctypes.byref(prefix), prefix_len, ctypes.byref(own), _i64s(own_lens), _ptr(q), q_head_stride,
+        ctypes.byref(p), ctypes.byref(prefix), prefix_len, ctypes.byref(own), _at(lens), _ptr(q), q_head_stride,
         _ptr(k), _ptr(v), kv_head_stride, n_q, _ptr(idx), n_idx, _ptr(out), out_head_stride, _ptr(lse),
         _ptr(workspace), _wb(workspace, workspace_bytes), _stream(stream)))
 
 
 def infllm_copy_sequences(p, dst, src, dst_seq, src_seq, lens, units_built, stream=None):
     """dst_seq, src_seq, lens, units_built: host ints, one of each per copy."""
-    n = len(dst_seq)
-    if not n == len(src_seq) == len(lens) == len(units_built):
+    to, start, length, built = _i32s(dst_seq), _i32s(src_seq), _i64s(lens), _i32s(units_built)
+    n = len(to)
+    if not n == len(start) == len(length) == len(built):
         raise ValueError("one destination, source, length and unit count per copy")
     _check("infllm_copy_sequences", lib().infllm_copy_sequences(
-        ctypes.byref(p), ctypes.byref(dst), ctypes.byref(src), n, _i32s(dst_seq), _i32s(src_seq), _i64s(lens),
-        _i32s(units_built), _stream(stream)))
+        ctypes.byref(p), ctypes.byref(dst), ctypes.byref(src), n, _at(to), _at(start), _at(length), _at(built),
+        _stream(stream)))
 
 
 # ------------------------------------------------------------------ allocation plumbing
