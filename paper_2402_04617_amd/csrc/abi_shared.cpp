@@ -296,8 +296,9 @@ int64_t key_tiles(const infllm_params* p, int64_t keys) {
   return keys / kt + (keys % kt != 0);
 }
 
-// The part counts' bounds follow from the shape alone, so that the workspace does: no
-// region takes more than one round of workgroups.
+// The part counts' bounds follow from the shape alone, so that the workspace does: a
+// region takes at most one part more than fits a round of workgroups (300 row tiles on 512
+// places: two; more row tiles than places: one).
 PrefixPlan prefix_shape(const infllm_params* p, int batch, int n_q, int64_t shared_keys, int64_t unit_keys,
                         int64_t own_keys) {
   PrefixPlan r;

@@ -134,6 +134,7 @@ __device__ __forceinline__ void publish_barrier() {
 //    reads them at the memory's rate.  32 continuations of one token over 64K tokens, all
 //    of them attended: 61 us, 5.2 TB/s; 4 over 32K with 16 units each 15 us, a chain of
 //    loads (arguments 1.5, lookup 1.2, first keys 2.3), four tiles (4.8) and the epilogue.
+//    At D = 128 it takes all 256 registers that two waves a SIMD leave it.
 // NWAVE: 8 waves, one workgroup per compute unit and a barrier per pair of tiles: least
 // LDS traffic per product, for long parts; or 4, two workgroups per compute unit with two
 // buffers each and a barrier per tile, whose prologues and epilogues run beside the
@@ -355,7 +356,7 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
   // without units: it is then all -1).  Every entry is valid.
   static_assert(SEL == 0 || SEL == 2 || SEL == tk::kMaxPer, "select variants");
   static_assert(SEL == 0 || tk::kThreads == 64 * NWAVE);
-  static_assert( tk::kMaxPer * tk::kThreads >= kFusedSelectMax, "select layout");
+  static_assert(tk::kMaxPer * tk::kThreads >= kFusedSelectMax, "select layout");
   const bool sel_writer = SEL > 0 && rt == 0 && part == 0;
   const bool sel_here = SEL > 0 && (sel_writer || units_here);
   const bool sel_all = geo.n_sel == 0 || geo.n_sel == geo.n_units;  // every unit (or none) is looked up
@@ -508,7 +509,7 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
   // Direct loads: instruction j of wave w fills LDS granules [(NI*w + j)*64, +64)
   // of the tile, lane l writing granule slot l; that slot belongs to tile row
   // r_j = r_0 + RPI*j, r_0 = KB/NWAVE*w + l / CH, and holds its global granule
-  // (l % CH) ^ swz(r_j); a wave's loads cover the eight rows [8w, 8w + 8).
+  // (l % CH) ^ swz(r_j); a wave's loads cover KB / NWAVE rows in a run (8 or 16).
   const int lrow0 = KB / NWAVE * wave + lane / CH;
 
   // Store positions of the keys.  The virtual axis is cut into groups of 8 keys
@@ -821,8 +822,10 @@ __global__ void __launch_bounds__(64 * NWAVE, NWAVE == kMfmaWaves ? 1 : 2) atten
       a.mass_part[((int64_t)bg * a.mass_tiles + ut) * R + row] = make_float2(tsum, m_run);
   };
   // Two P values as a bf16 pair (one v_cvt_pk_bf16_f32), added unrounded to the
-  // two running row sums (the normaliser keeps float32 precision; rounding only
-  // the PV operand moves O by at most 2^-9 relative).
+  // two running row sums (the normaliser keeps float32 precision).  The rounding of
+  // the PV operand, half a step of bf16, moves each weight by at most 2^-8 of itself and
+  // so O by at most 2^-8 of the weighted sum of |v|: the instruction takes bf16 values
+  // with bf16 weights, and a weight in two pieces would take it twice.
   auto p_pair = [&](float z0, float z1, float nm, float (&acc)[2], bool first) -> uint32_t {
     const float e0 = fast_exp2(__builtin_fmaf(z0, c2, nm));
     const float e1 = fast_exp2(__builtin_fmaf(z1, c2, nm));
