@@ -354,7 +354,8 @@ infllm_status infllm_step_varlen(const infllm_params* p, const infllm_memory* m,
  * ones) and, where a row's keys are split, each part's row to fp16 relative to its
  * largest value (2^-11); out is rounded once more.  Outputs
  * (out, lse, scores) and workspaces overlap no input and no other call's that may
- * run at the same time; calls with workspaces of their own may. */
+ * run at the same time; calls with workspaces of their own may.  Strides and
+ * capacities that reach past 2^62 bytes are E_UNSUPPORTED. */
 
 /* Causal attention of whole prompts, packed: n_seqs sequences of seq_lens[i] >= 0
  * tokens (a HOST array, read during the call) lie one after another, `total`
@@ -385,7 +386,8 @@ infllm_status infllm_prompt_attend(const infllm_params* p, int32_t n_seqs, const
 /* Bytes of workspace that infllm_prefix_score and infllm_prefix_attend need for
  * `batch` continuations of n_q current tokens each, a document of prefix_len
  * tokens and own stores of own_capacity tokens (up to params.topk looked-up
- * units).  Depends only on these arguments; 0 where they are invalid. */
+ * units).  Depends only on these arguments; 0 where they are invalid or batch * Hq *
+ * n_q passes 2^31 - 1, which both refuse. */
 size_t infllm_prefix_workspace_bytes(const infllm_params* p, int32_t batch, int32_t n_q, int64_t prefix_len,
                                      int64_t own_capacity);
 
@@ -395,7 +397,7 @@ size_t infllm_prefix_workspace_bytes(const infllm_params* p, int32_t batch, int3
  * once for all.  q: [batch][Hq] heads of n_q x D dtype rows; scores:
  * [batch][Hkv][n_units] float32, which infllm_select_topk takes with
  * rows = batch * Hkv.  Uses only unit_ksum and max_units of the memory.
- * E_UNSUPPORTED for batch * Hkv past 65,535. */
+ * E_UNSUPPORTED for batch * Hkv past 65,535 or batch * Hq * n_q past 2^31 - 1. */
 infllm_status infllm_prefix_score(const infllm_params* p, const infllm_memory* prefix, int32_t batch, const void* q,
                                   int64_t q_head_stride, int32_t n_q, int32_t n_units, float* scores, void* workspace,
                                   size_t workspace_bytes, void* stream);

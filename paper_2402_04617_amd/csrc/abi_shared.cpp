@@ -19,10 +19,21 @@ namespace {
 // the strides in elements.
 infllm_status check_strided(const infllm_params* p, const void* ptr, int64_t tok, int64_t head) {
   if (ptr == nullptr) return INFLLM_E_NULL;
-  if (tok < 0 || head < 0 || ((tok * esize(p)) & 15) != 0 || ((head * esize(p)) & 15) != 0 || !aligned16(ptr))
-    return INFLLM_E_SHAPE;
+  const int64_t piece = 16 / esize(p);
+  if (tok < 0 || head < 0 || tok % piece != 0 || head % piece != 0 || !aligned16(ptr)) return INFLLM_E_SHAPE;
   return INFLLM_OK;
 }
+
+// Whether offsets into rows of head_dim elements, n1 by n2 of them with strides s1 and s2,
+// stay within 62 bits: kernels and checks multiply them in 64.
+bool span_fits(const infllm_params* p, int64_t n1, int64_t s1, int64_t n2 = 1, int64_t s2 = 0) {
+  return ((__int128)(n1 - 1) * s1 + (__int128)(n2 - 1) * s2 + p->head_dim) * esize(p) <= (__int128)1 << 62;
+}
+bool store_fits(const infllm_params* p, const infllm_memory* m) {
+  return (__int128)m->batch * p->n_kv_heads * m->capacity <= ((__int128)1 << 62) / (p->head_dim * esize(p));
+}
+// Whether the product of three numbers that are not negative fits 31 bits.
+bool fits31(int64_t a, int64_t b, int64_t c) { return (__int128)a * b * c <= INT32_MAX; }
 
 int key_tile(bool bf16) { return bf16 ? 64 : 32; }
 
@@ -230,6 +241,10 @@ infllm_status infllm_prompt_attend(const infllm_params* p, int32_t n_seqs, const
   const bool by_head = out_token_stride >= D && (p->n_q_heads == 1 || steps_over(out_head_stride, out_token_stride, total));
   const bool by_token = out_head_stride >= D && (total == 1 || steps_over(out_token_stride, out_head_stride, p->n_q_heads));
   if (!by_head && !by_token) return INFLLM_E_SHAPE;
+  if (!span_fits(p, total, q_token_stride, p->n_q_heads, q_head_stride) ||
+      !span_fits(p, total, kv_token_stride, p->n_kv_heads, kv_head_stride) ||
+      !span_fits(p, total, out_token_stride, p->n_q_heads, out_head_stride))
+    return INFLLM_E_UNSUPPORTED;
   // the bf16 kernel addresses the keys of a sequence with 32-bit byte offsets
   if (bf16 && ((uint64_t)kv_token_stride > 0x7FFFFFFFull ||
                (uint64_t)(longest - 1) * (uint64_t)kv_token_stride * 2u + (uint64_t)D * 2u > 0xFFFFFFFFull))
@@ -384,6 +399,7 @@ extern "C" {
 size_t infllm_prefix_workspace_bytes(const infllm_params* p, int32_t batch, int32_t n_q, int64_t prefix_len,
                                      int64_t own_capacity) {
   if (check_params(p) != INFLLM_OK || batch < 1 || n_q < 0 || prefix_len < 0 || own_capacity < 0) return 0;
+  if (!fits31(batch, p->n_q_heads, n_q)) return 0;
   Part part;
   int64_t shared, units;
   prefix_keys(p, prefix_len, p->topk, &part, &shared, &units);
@@ -405,7 +421,8 @@ infllm_status infllm_prefix_score(const infllm_params* p, const infllm_memory* p
   if (prefix->unit_ksum == nullptr || scores == nullptr) return INFLLM_E_NULL;
   if (!aligned16(prefix->unit_ksum)) return INFLLM_E_SHAPE;
   if ((st = check_rows(p, q, q_head_stride, n_q)) != INFLLM_OK) return st;
-  if ((int64_t)batch * p->n_kv_heads > 65535 || (int64_t)(p->n_q_heads / p->n_kv_heads) * n_q > INT32_MAX)
+  if ((int64_t)batch * p->n_kv_heads > 65535 || !fits31(batch, p->n_q_heads, n_q) ||
+      !span_fits(p, (int64_t)batch * p->n_q_heads, q_head_stride))
     return INFLLM_E_UNSUPPORTED;
   if (workspace == nullptr) return INFLLM_E_NULL;
   if (workspace_bytes < qbar_ws_bytes(p, batch, n_q)) return INFLLM_E_WORKSPACE;
@@ -461,7 +478,11 @@ infllm_status infllm_prefix_attend(const infllm_params* p, const infllm_memory* 
   if (units > 0 && idx == nullptr) return INFLLM_E_NULL;
   const bool bf16 = p->dtype == INFLLM_BF16;
   const int64_t G = p->n_q_heads / p->n_kv_heads, D = p->head_dim;
-  if (shared > INT32_MAX || units > INT32_MAX || own_most + n_q > INT32_MAX || G * n_q * B * p->n_kv_heads > INT32_MAX)
+  if (shared > INT32_MAX || units > INT32_MAX || own_most + n_q > INT32_MAX || !fits31(B, p->n_q_heads, n_q))
+    return INFLLM_E_UNSUPPORTED;
+  if (!store_fits(p, prefix) || !store_fits(p, own) || !span_fits(p, (int64_t)B * p->n_q_heads, q_head_stride) ||
+      !span_fits(p, (int64_t)B * p->n_q_heads, out_head_stride) ||
+      (k != nullptr && !span_fits(p, (int64_t)B * p->n_kv_heads, kv_head_stride)))
     return INFLLM_E_UNSUPPORTED;
   // the bf16 kernel addresses one (sequence, kv head) slice of a store with 32-bit byte offsets
   const int64_t most_rows = (int64_t)(0xFFFFFFFFull / (uint64_t)(2 * D));
@@ -589,9 +610,9 @@ infllm_status infllm_copy_sequences(const infllm_params* p, const infllm_memory*
     if (rings) {
       if (m->qprefix == nullptr || m->rpart == nullptr) return INFLLM_E_NULL;
       if (!aligned16(m->qprefix) || m->ring < 1) return INFLLM_E_SHAPE;
-      if ((int64_t)p->n_kv_heads * m->ring * p->head_dim / 2 > INT32_MAX) return INFLLM_E_UNSUPPORTED;
+      if (!fits31(p->n_kv_heads, m->ring, p->head_dim / 2)) return INFLLM_E_UNSUPPORTED;
     }
-    if ((int64_t)p->n_kv_heads * units * std::max(p->head_dim / 4, p->n_repr) > INT32_MAX) return INFLLM_E_UNSUPPORTED;
+    if (!fits31(p->n_kv_heads, units, std::max(p->head_dim / 4, p->n_repr)) || !store_fits(p, m)) return INFLLM_E_UNSUPPORTED;
   }
   // a copy goes to a slot of its own, which no pair reads
   const int64_t row = (int64_t)p->head_dim * esize(p);
