@@ -439,7 +439,9 @@ infllm_status infllm_prefix_attend(const infllm_params* p, const infllm_memory* 
  * sums of units_built[i] units (<= n_units(lens[i]), as the caller passes units_built
  * to the next infllm_step), and the query rings' slots of the last
  * min(lens[i], src ring, dst ring) positions, so that the copy is continued like its
- * source (a ring smaller than the source's must still be one the next append accepts).
+ * source (a ring smaller than the source's must still be one the next append accepts;
+ * a larger one holds no more than the source's did, so that the next append and unit
+ * construction must be ones that the source's ring would accept).
  * A copy that is to be continued takes the source's whole length: at a shorter one its
  * K, V and units are right, but the source's rings hold later positions by now.
  * Everything else of the destination is left as it was.  The arrays are HOST arrays.
