@@ -132,7 +132,7 @@ __device__ __forceinline__ void publish_barrier() {
 //    three regions.  The rows of all continuations share the row tiles of I and L, so
 //    that those keys are read once; what looks at a continuation's own units or tokens
 //    reads them at the memory's rate.  32 continuations of one token over 64K tokens, all
-//    of them attended: 61 us, 5.2 TB/s; 4 over 32K with 16 units each 15 us, a chain of
+//    of them attended: 58 us, 5.4 TB/s; 4 over 32K with 16 units each 15 us, a chain of
 //    loads (arguments 1.5, lookup 1.2, first keys 2.3), four tiles (4.8) and the epilogue.
 //    At D = 128 it takes all 256 registers that two waves a SIMD leave it.
 // NWAVE: 8 waves, one workgroup per compute unit and a barrier per pair of tiles: least
