@@ -26,7 +26,8 @@
  *  - Calls on different streams that write the same buffers race; calls are
  *    otherwise re-entrant.
  *  - All sequences of a batch share one past length, except in
- *    infllm_step_varlen, infllm_prompt_attend and infllm_prefix_attend.
+ *    infllm_step_varlen, infllm_prompt_attend, infllm_prefix_attend and the calls on
+ *    paged caches.
  */
 #ifndef INFLLM_H
 #define INFLLM_H
@@ -452,6 +453,135 @@ infllm_status infllm_prefix_attend(const infllm_params* p, const infllm_memory* 
 infllm_status infllm_copy_sequences(const infllm_params* p, const infllm_memory* dst, const infllm_memory* src, int32_t n,
                                     const int32_t* dst_seq, const int32_t* src_seq, const int64_t* lens,
                                     const int32_t* units_built, void* stream);
+
+/* ---- paged caches ------------------------------------------------------------
+ * What a program that serves many requests uses for those whose keys and values it
+ * keeps in pages rather than in a memory's dense store (questions and passages that fit
+ * the window, until they need a memory): rotation of the projections to their positions,
+ * with the norms of models that have them; the new tokens' keys and values into their
+ * pages; and causal attention of the new tokens over them.  All take the positions of
+ * infllm_rotary, not the remap (E_UNSUPPORTED with params.rope_inv_freq); of the params
+ * only the heads, head_dim, dtype and (in the attention) sm_scale matter.  What
+ * the shared documents' calls above say of values that are not finite, of roundings, of
+ * outputs and workspaces and of strides holds here as well.  Every call is forward only
+ * and repeats itself bit for bit. */
+
+/* Rotation and norms of a layer's query and key rows.  For row x of head_dim elements at
+ * position p, in float32 and rounded once:
+ *   norm != 0:  x <- x / sqrt(mean_d x_d^2 + norm_eps) * weight
+ *   pair i < rotary_dim / 2, (a, b) = (x_2i, x_2i+1) if interleaved, else
+ *   (x_i, x_{i + rotary_dim/2}), turns by the angle f = p * inv_freq[i]:
+ *     a' = magnitude (a cos f - b sin f),  b' = magnitude (a sin f + b cos f)
+ * Dimensions from rotary_dim on are not turned (nor scaled by magnitude).  Angles are
+ * formed in float64. */
+typedef struct {
+  int32_t rotary_dim;     /* even, 0 (nothing turns) .. head_dim */
+  int32_t interleaved;    /* pairs (2i, 2i+1); 0: (i, i + rotary_dim/2) */
+  const double* inv_freq; /* HOST array of rotary_dim/2 finite frequencies >= 0 (radians per position) */
+  float magnitude;        /* finite; 1 unless the model's scaling says otherwise */
+  int32_t norm;           /* 0: rows are taken as they are */
+  float norm_eps;         /* finite, >= 0 */
+  const void* q_weight;   /* DEVICE [head_dim] dtype, or NULL for ones; used where norm != 0 */
+  const void* k_weight;
+} infllm_rotary;
+
+/* How inv_freq follows from theta_i = base^(-2i/rotary_dim) for contexts `factor` times
+ * the trained ones. */
+typedef enum {
+  INFLLM_ROPE_PLAIN = 0,  /* theta_i */
+  INFLLM_ROPE_LINEAR = 1, /* theta_i / factor (interpolated positions) */
+  INFLLM_ROPE_BASE = 2,   /* theta_i of base * factor^(r / (r - 2)), r = rotary_dim > 2: the fastest pair as it was, the slowest / factor */
+  INFLLM_ROPE_PARTS = 3   /* by the turns n_i = original_len * theta_i / (2 pi) that a pair makes in the trained
+                             context: theta_i (g + (1 - g) / factor), g = (n_i - slow) / (fast - slow) within [0, 1] */
+} infllm_rope_scaling;
+/* inv_freq: HOST output of rotary_dim/2.  slow < fast and original_len >= 1 are used by
+ * INFLLM_ROPE_PARTS alone.  Host only.  E_SHAPE: an odd or negative rotary_dim, a base
+ * or factor that is not finite and > 0, or an unknown scaling. */
+infllm_status infllm_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor,
+                                      int64_t original_len, double slow, double fast, double* inv_freq);
+
+/* Norms and rotation of n_tokens tokens' query and key rows.  The row of token t and
+ * head h starts at t * token_stride + h * head_stride elements, as in
+ * infllm_prompt_attend; outputs may be the inputs (same pointer and strides) and must not
+ * overlap them otherwise.  positions: DEVICE int64 [n_tokens] (any sign), or NULL for
+ * first_position + t.  q and q_out may both be NULL, and so may k and k_out. */
+infllm_status infllm_rotate(const infllm_params* p, const infllm_rotary* rot, int32_t n_tokens,
+                            const int64_t* positions, int64_t first_position, const void* q, int64_t q_token_stride,
+                            int64_t q_head_stride, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                            const void* k, int64_t k_token_stride, int64_t k_head_stride, void* k_out,
+                            int64_t k_out_token_stride, int64_t k_out_head_stride, void* stream);
+
+/* A layer's pages: the key row of page x, slot s < page_size and kv head h starts at
+ * x * page_stride + s * token_stride + h * head_stride elements of k, the value row at
+ * the same place of v.  So [n_pages][Hkv][page_size][D] and [n_pages][page_size][Hkv][D]
+ * do, and pages that lie apart (k and v, or layers, side by side).  Any page_size; with
+ * a multiple of 8 fewer positions are looked up.  Strides are multiples of 16 bytes, and
+ * no two rows share an element (E_SHAPE).
+ * Token t of sequence i lies in page page_table[i * table_stride + t / page_size], slot
+ * t % page_size (page_table: DEVICE int32).  Sequences may share pages that no call
+ * writes.  Entries that are negative or >= n_pages are not followed: their tokens are
+ * not written, and not seen by any query. */
+typedef struct {
+  int32_t n_pages;
+  int32_t page_size;
+  void* k;
+  void* v;
+  int64_t page_stride, token_stride, head_stride;
+} infllm_pages;
+
+/* The new tokens of n_seqs sequences into their pages: sequence i has past_lens[i] >= 0
+ * tokens and gets seq_lens[i] >= 0 more (HOST arrays, read during the call), which lie
+ * packed one after another in q, k and v.  k is normed and rotated to positions
+ * past_lens[i] + j on the way (rot; NULL: taken as it is), v copied, and q normed and
+ * rotated into q_out (which may be q) in the same launch; q and q_out both NULL leave the
+ * queries alone.  Slots that no new token takes are left as they are, as are q_out's
+ * rows past the last token.  Two new tokens must not share a slot.  E_RANGE where
+ * past_lens[i] + seq_lens[i] tokens need more than table_stride pages; E_UNSUPPORTED
+ * where they pass 2^31 - 1. */
+infllm_status infllm_paged_append(const infllm_params* p, const infllm_rotary* rot, const infllm_pages* pages,
+                                  int32_t n_seqs, const int32_t* seq_lens, const int64_t* past_lens,
+                                  const int32_t* page_table, int64_t table_stride, const void* q,
+                                  int64_t q_token_stride, int64_t q_head_stride, void* q_out,
+                                  int64_t q_out_token_stride, int64_t q_out_head_stride, const void* k, const void* v,
+                                  int64_t kv_token_stride, int64_t kv_head_stride, void* stream);
+
+/* Which keys a query sees and what its scores become.  For the query at position p and
+ * the key at t <= p: z = sm_scale q . k_t;
+ *   softcap > 0:  z <- softcap * tanh(z / softcap)
+ *   slopes:       z <- z - slopes[h] * (p - t)   (DEVICE float32 [Hq], any finite values)
+ *   window > 0:   seen only where t > p - window or t < n_init
+ * (with a window of l_L and n_init = l_I this is the step's attention without looked-up
+ * units).  NULL in place of the struct, or zeros, change nothing. */
+typedef struct {
+  float softcap;
+  int32_t window;
+  int32_t n_init;
+  const float* slopes;
+} infllm_score_form;
+
+/* Bytes of workspace of infllm_paged_attend for these arguments (0 where they are
+ * invalid); NULL is allowed where it is 0. */
+size_t infllm_paged_workspace_bytes(const infllm_params* p, const infllm_pages* pages, int32_t n_seqs,
+                                    const int32_t* seq_lens, const int64_t* past_lens, const infllm_score_form* score);
+
+/* Causal attention of the new tokens over their sequences' pages, where their own keys
+ * and values already lie (infllm_paged_append): the query of new token j of sequence i,
+ * at position past_lens[i] + j, and head h (kv head h / G) takes one softmax over the
+ * tokens t <= past_lens[i] + j that `score` lets it see.  Single tokens (a decoding
+ * batch), chunks of prompts and both together are one call: one launch and, where keys
+ * are split, a merge (more than 256 sequences: for every 256).
+ *  q, out: packed rows with token and head strides as in infllm_prompt_attend; lse:
+ *     optional [Hq][total] float32, total the sum of seq_lens.
+ * A query that sees nothing (its pages not followed) gets zeros and lse -inf.
+ * E_RANGE as in infllm_paged_append.  E_UNSUPPORTED where the rows of k span more than
+ * 64 GiB, or the work exceeds 32-bit numbers (total * G past 2^31 - 1, positions past
+ * 2^31 - 256, or some 2^32 / 256 workgroups). */
+infllm_status infllm_paged_attend(const infllm_params* p, const infllm_pages* pages, int32_t n_seqs,
+                                  const int32_t* seq_lens, const int64_t* past_lens, const int32_t* page_table,
+                                  int64_t table_stride, const infllm_score_form* score, const void* q,
+                                  int64_t q_token_stride, int64_t q_head_stride, void* out, int64_t out_token_stride,
+                                  int64_t out_head_stride, float* lse, void* workspace, size_t workspace_bytes,
+                                  void* stream);
 
 /* Static description of a status code. */
 const char* infllm_status_string(infllm_status s);

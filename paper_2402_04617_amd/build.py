@@ -18,8 +18,9 @@ LIB = os.path.join(PKG, "libinfllm.so")
 PEAKS = os.path.join(PKG, "infllm_peaks")
 TOPK_CMP = os.path.join(PKG, "infllm_topk_compare")
 
-SOURCES = ["abi.cpp", "abi_shared.cpp", "append.hip", "copy.hip", "build_units.hip", "score.hip", "topk.hip", "attend_mfma.hip",
-           "attend.hip", "attend_decode.hip", "merge.hip", "mass.hip", "prefix_score.hip"]
+SOURCES = ["abi.cpp", "abi_shared.cpp", "abi_paged.cpp", "append.hip", "copy.hip", "build_units.hip", "score.hip", "topk.hip", "attend_mfma.hip",
+           "attend.hip", "attend_decode.hip", "merge.hip", "mass.hip", "prefix_score.hip",
+           "rotate.hip", "paged_attend.hip"]
 
 # Packed fp32 ops are disabled for all device code (the host pass warns that it
 # does not know the feature; that is harmless).

@@ -1,0 +1,343 @@
+// C ABI of the calls on paged caches (declared in include/infllm.h): rotary frequencies,
+// norms and rotation, the append to pages, attention over them.  As in abi.cpp every check
+// runs before the first HIP call.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "abi_util.h"
+#include "paged.h"
+
+using namespace infllm;
+
+namespace {
+
+constexpr double kTwoPi = 6.283185307179586476925286766559;
+constexpr int64_t kMostTokens = INT32_MAX - 255;  // of a sequence: tile ends past them stay in 31 bits
+
+infllm_status check_rotary(const infllm_params* p, const infllm_rotary* r) {
+  if (r == nullptr) return INFLLM_E_NULL;
+  if (r->rotary_dim < 0 || r->rotary_dim > p->head_dim || r->rotary_dim % 2 != 0) return INFLLM_E_SHAPE;
+  if (r->rotary_dim > 0) {
+    if (r->inv_freq == nullptr) return INFLLM_E_NULL;
+    if (!std::isfinite(r->magnitude)) return INFLLM_E_SHAPE;
+    for (int i = 0; i < r->rotary_dim / 2; ++i)
+      if (!std::isfinite(r->inv_freq[i]) || r->inv_freq[i] < 0.0) return INFLLM_E_SHAPE;
+  }
+  if (r->norm != 0) {
+    if (!std::isfinite(r->norm_eps) || r->norm_eps < 0.f) return INFLLM_E_SHAPE;
+    if (!aligned16(r->q_weight) || !aligned16(r->k_weight)) return INFLLM_E_SHAPE;
+  }
+  return INFLLM_OK;
+}
+
+// Rows (i, j), i < n1, j < n2, with strides s1 and s2: whether no two share an element.
+bool apart(int64_t D, int64_t n1, int64_t s1, int64_t n2, int64_t s2) {
+  auto over = [&](int64_t outer, int64_t inner, int64_t n) {  // outer steps over n inner rows, in 64 bits
+    return outer >= D && (n == 1 || inner <= (outer - D) / (n - 1));
+  };
+  const bool i_outer = (n2 == 1 || s2 >= D) && (n1 == 1 || over(s1, s2, n2));
+  const bool j_outer = (n1 == 1 || s1 >= D) && (n2 == 1 || over(s2, s1, n1));
+  return i_outer || j_outer;
+}
+
+infllm_status check_out(const infllm_params* p, const void* ptr, int64_t n_tokens, int64_t tok, int64_t n_heads, int64_t head) {
+  infllm_status st = check_strided(p, ptr, tok, head);
+  if (st != INFLLM_OK) return st;
+  return apart(p->head_dim, n_tokens, tok, n_heads, head) ? INFLLM_OK : INFLLM_E_SHAPE;
+}
+
+// The pages: three strides, each of which steps over all rows of the smaller ones.
+infllm_status check_pages(const infllm_params* p, const infllm_pages* g) {
+  if (g == nullptr || g->k == nullptr || g->v == nullptr) return INFLLM_E_NULL;
+  if (g->n_pages < 1 || g->page_size < 1) return INFLLM_E_SHAPE;
+  infllm_status st;
+  if ((st = check_strided(p, g->k, g->page_stride, g->token_stride)) != INFLLM_OK) return st;
+  if ((st = check_strided(p, g->v, g->head_stride, 0)) != INFLLM_OK) return st;
+  struct Axis {
+    int64_t n, s;
+  } ax[3] = {{g->n_pages, g->page_stride}, {g->page_size, g->token_stride}, {p->n_kv_heads, g->head_stride}};
+  std::sort(ax, ax + 3, [](const Axis& x, const Axis& y) { return x.s < y.s; });
+  __int128 extent = p->head_dim;  // elements that the axes so far span
+  for (const Axis& x : ax) {
+    if (x.n == 1) continue;
+    if (x.s < extent) return INFLLM_E_SHAPE;
+    extent += (__int128)(x.n - 1) * x.s;
+  }
+  return extent * esize(p) <= (__int128)1 << 62 ? INFLLM_OK : INFLLM_E_UNSUPPORTED;
+}
+
+// The sequences' lengths: their sum, and whether they fit the table.
+infllm_status check_seqs(const infllm_pages* g, int32_t n_seqs, const int32_t* lens, const int64_t* pasts,
+                         int64_t table_stride, int64_t* total) {
+  *total = 0;
+  if (n_seqs < 0) return INFLLM_E_SHAPE;
+  if (n_seqs == 0) return INFLLM_OK;
+  if (lens == nullptr || pasts == nullptr) return INFLLM_E_NULL;
+  if (table_stride < 0) return INFLLM_E_SHAPE;
+  infllm_status st = INFLLM_OK;
+  for (int i = 0; i < n_seqs; ++i) {
+    if (lens[i] < 0 || pasts[i] < 0) return INFLLM_E_SHAPE;
+    *total += lens[i];
+    if (lens[i] == 0) continue;
+    if (pasts[i] > kMostTokens - lens[i]) st = INFLLM_E_UNSUPPORTED;
+    else if (st == INFLLM_OK && (pasts[i] + lens[i] - 1) / g->page_size >= table_stride) st = INFLLM_E_RANGE;
+  }
+  if (st == INFLLM_OK && (*total > INT32_MAX || (__int128)n_seqs * table_stride > (__int128)1 << 59)) st = INFLLM_E_UNSUPPORTED;
+  return st;
+}
+
+// The sequences [i, i + kMaxPaged) of the call, the first of which starts at token `at`.
+void fill_seqs(const infllm_pages* g, int32_t n_seqs, const int32_t* lens, const int64_t* pasts, const int32_t* table,
+               int64_t table_stride, int i, int64_t at, PagedSeqs* s) {
+  s->n_seqs = std::min(n_seqs - i, kMaxPaged);
+  s->n_pages = g->n_pages;
+  s->page_size = g->page_size;
+  s->d_page = fast_div(g->page_size);
+  s->table = table + i * table_stride;
+  s->table_stride = table_stride;
+  for (int j = 0; j < s->n_seqs; ++j) {
+    s->start[j] = (int32_t)at;
+    s->past[j] = lens[i + j] > 0 ? (int32_t)pasts[i + j] : 0;
+    at += lens[i + j];
+  }
+  s->start[s->n_seqs] = (int32_t)at;
+}
+
+void set_rotary(const infllm_params* p, const infllm_rotary* r, RotateArgs* a) {
+  a->head_dim = p->head_dim;
+  a->bf16 = p->dtype == INFLLM_BF16;
+  if (r == nullptr) return;
+  a->rotary_dim = r->rotary_dim;
+  a->interleaved = r->interleaved != 0;
+  a->magnitude = r->magnitude;
+  for (int i = 0; i < r->rotary_dim / 2; ++i) a->rev[i] = r->inv_freq[i] / kTwoPi;
+  a->norm = r->norm != 0;
+  a->eps = r->norm_eps;
+  a->q_weight = r->q_weight;
+  a->k_weight = r->k_weight;
+}
+
+// Whether a rotation's launch, at most a wave per row of a token, stays within 2^31 waves.
+bool rotate_fits(int64_t tokens, int64_t rows) { return (__int128)tokens * rows < INT32_MAX / 64; }
+
+infllm_status check_score(const infllm_score_form* s) {
+  if (s == nullptr) return INFLLM_OK;
+  if (!std::isfinite(s->softcap) || s->softcap < 0.f || s->window < 0 || s->n_init < 0) return INFLLM_E_SHAPE;
+  return (reinterpret_cast<uintptr_t>(s->slopes) & 3u) == 0 ? INFLLM_OK : INFLLM_E_SHAPE;
+}
+
+}  // namespace
+
+extern "C" {
+
+infllm_status infllm_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor,
+                                      int64_t original_len, double slow, double fast, double* inv_freq) {
+  if (rotary_dim < 0 || rotary_dim % 2 != 0) return INFLLM_E_SHAPE;
+  if (!std::isfinite(base) || !(base > 0.0)) return INFLLM_E_SHAPE;
+  if (scaling < INFLLM_ROPE_PLAIN || scaling > INFLLM_ROPE_PARTS) return INFLLM_E_SHAPE;
+  if (scaling != INFLLM_ROPE_PLAIN && (!std::isfinite(factor) || !(factor > 0.0))) return INFLLM_E_SHAPE;
+  if (scaling == INFLLM_ROPE_BASE && rotary_dim <= 2) return INFLLM_E_SHAPE;
+  if (scaling == INFLLM_ROPE_PARTS && (original_len < 1 || !std::isfinite(slow) || !std::isfinite(fast) || !(slow < fast)))
+    return INFLLM_E_SHAPE;
+  if (rotary_dim == 0) return INFLLM_OK;
+  if (inv_freq == nullptr) return INFLLM_E_NULL;
+  const double r = rotary_dim, b = scaling == INFLLM_ROPE_BASE ? base * std::pow(factor, r / (r - 2.0)) : base;
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    double theta = std::pow(b, -2.0 * i / r);
+    if (scaling == INFLLM_ROPE_LINEAR) theta /= factor;
+    if (scaling == INFLLM_ROPE_PARTS) {
+      const double g = std::min(1.0, std::max(0.0, ((double)original_len * theta / kTwoPi - slow) / (fast - slow)));
+      theta *= g + (1.0 - g) / factor;
+    }
+    inv_freq[i] = theta;
+  }
+  return INFLLM_OK;
+}
+
+infllm_status infllm_rotate(const infllm_params* p, const infllm_rotary* rot, int32_t n_tokens,
+                            const int64_t* positions, int64_t first_position, const void* q, int64_t q_token_stride,
+                            int64_t q_head_stride, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                            const void* k, int64_t k_token_stride, int64_t k_head_stride, void* k_out,
+                            int64_t k_out_token_stride, int64_t k_out_head_stride, void* stream) {
+  infllm_status st;
+  if ((st = check_params(p)) != INFLLM_OK) return st;
+  if (remap(p)) return INFLLM_E_UNSUPPORTED;
+  if ((st = check_rotary(p, rot)) != INFLLM_OK) return st;
+  if (n_tokens < 0) return INFLLM_E_SHAPE;
+  if ((q == nullptr) != (q_out == nullptr) || (k == nullptr) != (k_out == nullptr)) return INFLLM_E_NULL;
+  if (n_tokens == 0 || (q == nullptr && k == nullptr)) return INFLLM_OK;
+  if ((reinterpret_cast<uintptr_t>(positions) & 7u) != 0) return INFLLM_E_SHAPE;
+  if (q != nullptr) {
+    if ((st = check_strided(p, q, q_token_stride, q_head_stride)) != INFLLM_OK) return st;
+    if ((st = check_out(p, q_out, n_tokens, q_out_token_stride, p->n_q_heads, q_out_head_stride)) != INFLLM_OK) return st;
+    if (!span_fits(p, n_tokens, q_token_stride, p->n_q_heads, q_head_stride) ||
+        !span_fits(p, n_tokens, q_out_token_stride, p->n_q_heads, q_out_head_stride))
+      return INFLLM_E_UNSUPPORTED;
+  }
+  if (k != nullptr) {
+    if ((st = check_strided(p, k, k_token_stride, k_head_stride)) != INFLLM_OK) return st;
+    if ((st = check_out(p, k_out, n_tokens, k_out_token_stride, p->n_kv_heads, k_out_head_stride)) != INFLLM_OK) return st;
+    if (!span_fits(p, n_tokens, k_token_stride, p->n_kv_heads, k_head_stride) ||
+        !span_fits(p, n_tokens, k_out_token_stride, p->n_kv_heads, k_out_head_stride))
+      return INFLLM_E_UNSUPPORTED;
+  }
+  const int n_q = q != nullptr ? p->n_q_heads : 0, n_k = k != nullptr ? p->n_kv_heads : 0;
+  if (!rotate_fits(n_tokens, (int64_t)n_q + n_k)) return INFLLM_E_UNSUPPORTED;
+  if ((st = check_device()) != INFLLM_OK) return st;
+  RotateArgs a;
+  std::memset(&a, 0, sizeof(a));
+  set_rotary(p, rot, &a);
+  a.n_tokens = n_tokens;
+  a.n_q = n_q;
+  a.n_k = n_k;
+  a.q = q;
+  a.k = k;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.q_tok = q_token_stride;
+  a.q_head = q_head_stride;
+  a.kv_tok = k_token_stride;
+  a.kv_head = k_head_stride;
+  a.qo_tok = q_out_token_stride;
+  a.qo_head = q_out_head_stride;
+  a.ko_tok = k_out_token_stride;
+  a.ko_head = k_out_head_stride;
+  a.positions = positions;
+  a.first_position = first_position;
+  return launch_status(launch_rotate(a, (hipStream_t)stream));
+}
+
+infllm_status infllm_paged_append(const infllm_params* p, const infllm_rotary* rot, const infllm_pages* pages,
+                                  int32_t n_seqs, const int32_t* seq_lens, const int64_t* past_lens,
+                                  const int32_t* page_table, int64_t table_stride, const void* q,
+                                  int64_t q_token_stride, int64_t q_head_stride, void* q_out,
+                                  int64_t q_out_token_stride, int64_t q_out_head_stride, const void* k, const void* v,
+                                  int64_t kv_token_stride, int64_t kv_head_stride, void* stream) {
+  infllm_status st;
+  if ((st = check_params(p)) != INFLLM_OK) return st;
+  if (remap(p)) return INFLLM_E_UNSUPPORTED;
+  if (rot != nullptr && (st = check_rotary(p, rot)) != INFLLM_OK) return st;
+  if ((st = check_pages(p, pages)) != INFLLM_OK) return st;
+  int64_t total;
+  if ((st = check_seqs(pages, n_seqs, seq_lens, past_lens, table_stride, &total)) != INFLLM_OK) return st;
+  if ((q == nullptr) != (q_out == nullptr)) return INFLLM_E_NULL;
+  if (total == 0) return INFLLM_OK;
+  if (page_table == nullptr) return INFLLM_E_NULL;
+  if ((reinterpret_cast<uintptr_t>(page_table) & 3u) != 0) return INFLLM_E_SHAPE;
+  if ((st = check_strided(p, k, kv_token_stride, kv_head_stride)) != INFLLM_OK) return st;
+  if ((st = check_strided(p, v, kv_token_stride, kv_head_stride)) != INFLLM_OK) return st;
+  if (!span_fits(p, total, kv_token_stride, p->n_kv_heads, kv_head_stride)) return INFLLM_E_UNSUPPORTED;
+  if (q != nullptr) {
+    if ((st = check_strided(p, q, q_token_stride, q_head_stride)) != INFLLM_OK) return st;
+    if ((st = check_out(p, q_out, total, q_out_token_stride, p->n_q_heads, q_out_head_stride)) != INFLLM_OK) return st;
+    if (!span_fits(p, total, q_token_stride, p->n_q_heads, q_head_stride) ||
+        !span_fits(p, total, q_out_token_stride, p->n_q_heads, q_out_head_stride))
+      return INFLLM_E_UNSUPPORTED;
+  }
+  const int n_q = q != nullptr ? p->n_q_heads : 0;
+  if (!rotate_fits(total, (int64_t)n_q + 2 * (int64_t)p->n_kv_heads)) return INFLLM_E_UNSUPPORTED;
+  if ((st = check_device()) != INFLLM_OK) return st;
+  RotateArgs a;
+  std::memset(&a, 0, sizeof(a));
+  set_rotary(p, rot, &a);
+  a.paged = true;
+  a.n_q = n_q;
+  a.n_k = a.n_v = p->n_kv_heads;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_out = q_out;
+  a.k_out = pages->k;
+  a.v_out = pages->v;
+  a.q_tok = q_token_stride;
+  a.q_head = q_head_stride;
+  a.kv_tok = kv_token_stride;
+  a.kv_head = kv_head_stride;
+  a.qo_tok = q_out_token_stride;
+  a.qo_head = q_out_head_stride;
+  a.page_stride = pages->page_stride;
+  a.ko_tok = pages->token_stride;
+  a.ko_head = pages->head_stride;
+  int64_t at = 0;
+  for (int i = 0; i < n_seqs; i += kMaxPaged) {
+    fill_seqs(pages, n_seqs, seq_lens, past_lens, page_table, table_stride, i, at, &a.seqs);
+    a.first_token = (int)at;
+    at = a.seqs.start[a.seqs.n_seqs];
+    a.n_tokens = (int)at - a.first_token;
+    if (a.n_tokens > 0 && (st = launch_status(launch_rotate(a, (hipStream_t)stream))) != INFLLM_OK) return st;
+  }
+  return INFLLM_OK;
+}
+
+size_t infllm_paged_workspace_bytes(const infllm_params* p, const infllm_pages* pages, int32_t n_seqs,
+                                    const int32_t* seq_lens, const int64_t* past_lens, const infllm_score_form* score) {
+  return 0;
+}
+
+infllm_status infllm_paged_attend(const infllm_params* p, const infllm_pages* pages, int32_t n_seqs,
+                                  const int32_t* seq_lens, const int64_t* past_lens, const int32_t* page_table,
+                                  int64_t table_stride, const infllm_score_form* score, const void* q,
+                                  int64_t q_token_stride, int64_t q_head_stride, void* out, int64_t out_token_stride,
+                                  int64_t out_head_stride, float* lse, void* workspace, size_t workspace_bytes,
+                                  void* stream) {
+  infllm_status st;
+  if ((st = check_params(p)) != INFLLM_OK) return st;
+  if (remap(p)) return INFLLM_E_UNSUPPORTED;
+  if ((st = check_pages(p, pages)) != INFLLM_OK) return st;
+  if ((st = check_score(score)) != INFLLM_OK) return st;
+  int64_t total;
+  if ((st = check_seqs(pages, n_seqs, seq_lens, past_lens, table_stride, &total)) != INFLLM_OK) return st;
+  if (total == 0) return INFLLM_OK;
+  if (page_table == nullptr) return INFLLM_E_NULL;
+  if ((reinterpret_cast<uintptr_t>(page_table) & 3u) != 0 || (reinterpret_cast<uintptr_t>(lse) & 3u) != 0) return INFLLM_E_SHAPE;
+  if ((st = check_strided(p, q, q_token_stride, q_head_stride)) != INFLLM_OK) return st;
+  if ((st = check_out(p, out, total, out_token_stride, p->n_q_heads, out_head_stride)) != INFLLM_OK) return st;
+  if (!span_fits(p, total, q_token_stride, p->n_q_heads, q_head_stride) ||
+      !span_fits(p, total, out_token_stride, p->n_q_heads, out_head_stride))
+    return INFLLM_E_UNSUPPORTED;
+  const int64_t G = p->n_q_heads / p->n_kv_heads;
+  if (total > INT32_MAX / G || (__int128)total * p->n_q_heads > INT32_MAX) return INFLLM_E_UNSUPPORTED;
+  // (keys are addressed by 16-byte pieces in 32 bits)
+  const __int128 span = (__int128)(pages->n_pages - 1) * pages->page_stride + (__int128)(pages->page_size - 1) * pages->token_stride;
+  if (span * esize(p) / 16 >= 0xFFFFFFFFll) return INFLLM_E_UNSUPPORTED;
+  if ((st = check_device()) != INFLLM_OK) return st;
+  PagedArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.n_q_heads = p->n_q_heads;
+  a.n_kv_heads = p->n_kv_heads;
+  a.head_dim = p->head_dim;
+  a.bf16 = p->dtype == INFLLM_BF16;
+  a.sm_scale = p->sm_scale;
+  if (score != nullptr) {
+    a.softcap = score->softcap;
+    a.window = score->window;
+    a.n_init = score->n_init;
+    a.slopes = score->slopes;
+  }
+  a.q = q;
+  a.k = pages->k;
+  a.v = pages->v;
+  a.out = out;
+  a.lse = lse;
+  a.q_tok = q_token_stride;
+  a.q_head = q_head_stride;
+  a.out_tok = out_token_stride;
+  a.out_head = out_head_stride;
+  a.lse_stride = total;
+  a.page_stride = pages->page_stride;
+  a.token_stride = pages->token_stride;
+  a.head_stride = pages->head_stride;
+  int64_t at = 0;
+  for (int i = 0; i < n_seqs; i += kMaxPaged) {
+    fill_seqs(pages, n_seqs, seq_lens, past_lens, page_table, table_stride, i, at, &a.seqs);
+    const bool any = a.seqs.start[a.seqs.n_seqs] > at;
+    at = a.seqs.start[a.seqs.n_seqs];
+    if (any && (st = launch_status(launch_paged(a, (hipStream_t)stream))) != INFLLM_OK) return st;
+  }
+  return INFLLM_OK;
+}
+
+}  // extern "C"

@@ -15,20 +15,6 @@ using namespace infllm;
 
 namespace {
 
-// Rows (token, head) of a tensor read or written in 16-byte pieces: `tok` and `head` are
-// the strides in elements.
-infllm_status check_strided(const infllm_params* p, const void* ptr, int64_t tok, int64_t head) {
-  if (ptr == nullptr) return INFLLM_E_NULL;
-  const int64_t piece = 16 / esize(p);
-  if (tok < 0 || head < 0 || tok % piece != 0 || head % piece != 0 || !aligned16(ptr)) return INFLLM_E_SHAPE;
-  return INFLLM_OK;
-}
-
-// Whether offsets into rows of head_dim elements, n1 by n2 of them with strides s1 and s2,
-// stay within 62 bits: kernels and checks multiply them in 64.
-bool span_fits(const infllm_params* p, int64_t n1, int64_t s1, int64_t n2 = 1, int64_t s2 = 0) {
-  return ((__int128)(n1 - 1) * s1 + (__int128)(n2 - 1) * s2 + p->head_dim) * esize(p) <= (__int128)1 << 62;
-}
 bool store_fits(const infllm_params* p, const infllm_memory* m) {
   return (__int128)m->batch * p->n_kv_heads * m->capacity <= ((__int128)1 << 62) / (p->head_dim * esize(p));
 }

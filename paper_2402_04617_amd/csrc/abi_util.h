@@ -84,6 +84,21 @@ inline infllm_status check_rows(const infllm_params* p, const void* ptr, int64_t
   return INFLLM_OK;
 }
 
+// Rows (token, head) of a tensor read or written in 16-byte pieces: `tok` and `head` are
+// the strides in elements.
+inline infllm_status check_strided(const infllm_params* p, const void* ptr, int64_t tok, int64_t head) {
+  if (ptr == nullptr) return INFLLM_E_NULL;
+  const int64_t piece = 16 / esize(p);
+  if (tok < 0 || head < 0 || tok % piece != 0 || head % piece != 0 || !aligned16(ptr)) return INFLLM_E_SHAPE;
+  return INFLLM_OK;
+}
+
+// Whether offsets into rows of head_dim elements, n1 by n2 of them with strides s1 and s2,
+// stay within 62 bits: kernels and checks multiply them in 64.
+inline bool span_fits(const infllm_params* p, int64_t n1, int64_t s1, int64_t n2 = 1, int64_t s2 = 0) {
+  return ((__int128)(n1 - 1) * s1 + (__int128)(n2 - 1) * s2 + p->head_dim) * esize(p) <= (__int128)1 << 62;
+}
+
 struct Part {
   int64_t n_init, local_begin;
   int32_t n_units;

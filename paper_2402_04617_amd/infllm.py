@@ -20,6 +20,10 @@ INFLLM_F32 = 0
 INFLLM_BF16 = 1
 INFLLM_REPR_TOKENS = 0
 INFLLM_REPR_MEAN = 1
+INFLLM_ROPE_PLAIN = 0
+INFLLM_ROPE_LINEAR = 1
+INFLLM_ROPE_BASE = 2
+INFLLM_ROPE_PARTS = 3
 
 STATUS = {0: "INFLLM_OK", 1: "INFLLM_E_NULL", 2: "INFLLM_E_SHAPE", 3: "INFLLM_E_RANGE",
           4: "INFLLM_E_UNSUPPORTED", 5: "INFLLM_E_WORKSPACE", 6: "INFLLM_E_LAUNCH", 7: "INFLLM_E_DEVICE"}
@@ -29,7 +33,8 @@ EXPORTS = ["infllm_partition", "infllm_workspace_bytes", "infllm_attend_workspac
            "infllm_attend_partial",
            "infllm_lse_merge", "infllm_prompt_workspace_bytes", "infllm_prompt_attend",
            "infllm_prefix_workspace_bytes", "infllm_prefix_score", "infllm_prefix_attend", "infllm_copy_sequences",
-           "infllm_step", "infllm_step_mass", "infllm_step_varlen", "infllm_unit_mass",
+           "infllm_rope_frequencies", "infllm_rotate", "infllm_paged_append", "infllm_paged_workspace_bytes",
+           "infllm_paged_attend", "infllm_step", "infllm_step_mass", "infllm_step_varlen", "infllm_unit_mass",
            "infllm_status_string"]
 
 
@@ -64,6 +69,23 @@ class Memory(ctypes.Structure):
                 ("ring", ctypes.c_int32), ("k_rot", ctypes.c_void_p)]
 
 
+class Rotary(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("inv_freq", ctypes.POINTER(ctypes.c_double)), ("magnitude", ctypes.c_float), ("norm", ctypes.c_int32),
+                ("norm_eps", ctypes.c_float), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+class ScoreForm(ctypes.Structure):
+    _fields_ = [("softcap", ctypes.c_float), ("window", ctypes.c_int32), ("n_init", ctypes.c_int32),
+                ("slopes", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -77,6 +99,7 @@ def lib() -> ctypes.CDLL:
                            "(run `python -m paper_2402_04617_amd.build`)")
     L = ctypes.CDLL(_LIB_PATH)
     P, M = ctypes.POINTER(Params), ctypes.POINTER(Memory)
+    R, G, S = ctypes.POINTER(Rotary), ctypes.POINTER(Pages), ctypes.POINTER(ScoreForm)
     vp, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     sig = {
         "infllm_partition": [P, i64, ctypes.POINTER(i64), ctypes.POINTER(i32), ctypes.POINTER(i64)],
@@ -101,6 +124,11 @@ def lib() -> ctypes.CDLL:
         "infllm_prefix_attend": [P, M, i64, M, vp, vp, i64, vp, vp, i64, i32, vp, i32, vp, i64, vp, vp,
                                  sz, vp],
         "infllm_copy_sequences": [P, M, M, i32, vp, vp, vp, vp, vp],
+        "infllm_rope_frequencies": [i32, ctypes.c_double, i32, ctypes.c_double, i64, ctypes.c_double, ctypes.c_double,
+                                    vp],
+        "infllm_rotate": [P, R, i32, vp, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp, i64, i64, vp],
+        "infllm_paged_append": [P, R, G, i32, vp, vp, vp, i64, vp, i64, i64, vp, i64, i64, vp, vp, i64, i64, vp],
+        "infllm_paged_attend": [P, G, i32, vp, vp, vp, i64, S, vp, i64, i64, vp, i64, i64, vp, vp, sz, vp],
     }
     for name, args in sig.items():
         f = getattr(L, name)
@@ -114,6 +142,8 @@ def lib() -> ctypes.CDLL:
     L.infllm_prompt_workspace_bytes.restype = ctypes.c_size_t
     L.infllm_prefix_workspace_bytes.argtypes = [P, i32, i32, i64, i64]
     L.infllm_prefix_workspace_bytes.restype = ctypes.c_size_t
+    L.infllm_paged_workspace_bytes.argtypes = [P, G, i32, vp, vp, S]
+    L.infllm_paged_workspace_bytes.restype = ctypes.c_size_t
     L.infllm_status_string.argtypes = [ctypes.c_int]
     L.infllm_status_string.restype = ctypes.c_char_p
     _lib = L
@@ -321,6 +351,69 @@ def infllm_copy_sequences(p, dst, src, dst_seq, src_seq, lens, units_built, stre
         _stream(stream)))
 
 
+_SCALINGS = {"plain": INFLLM_ROPE_PLAIN, "linear": INFLLM_ROPE_LINEAR, "base": INFLLM_ROPE_BASE,
+             "parts": INFLLM_ROPE_PARTS}
+
+
+def infllm_rope_frequencies(rotary_dim: int, base: float = 500000.0, scaling: str = "plain", factor: float = 1.0,
+                            original_len: int = 0, slow: float = 1.0, fast: float = 32.0):
+    """The rotary_dim/2 frequencies (a list); scaling: "plain", "linear", "base" or "parts"."""
+    out = (ctypes.c_double * max(1, rotary_dim // 2))()
+    _check("infllm_rope_frequencies", lib().infllm_rope_frequencies(
+        rotary_dim, base, _SCALINGS[scaling], factor, original_len, slow, fast, ctypes.addressof(out)))
+    return list(out)[:rotary_dim // 2]
+
+
+def infllm_rotate(p, rot, n_tokens, positions, q, q_strides, q_out, q_out_strides, k, k_strides, k_out, k_out_strides,
+                  first_position=0, stream=None):
+    """positions: int64 tensor, or None for first_position + t; strides: (token, head) in elements (of what is None
+    they may be None)."""
+    qs, qos, ks, kos = (x or (0, 0) for x in (q_strides, q_out_strides, k_strides, k_out_strides))
+    _check("infllm_rotate", lib().infllm_rotate(
+        ctypes.byref(p), ctypes.byref(rot), n_tokens, _ptr(positions), first_position, _ptr(q), qs[0], qs[1],
+        _ptr(q_out), qos[0], qos[1], _ptr(k), ks[0], ks[1], _ptr(k_out), kos[0], kos[1], _stream(stream)))
+
+
+def _seqs(seq_lens, past_lens, page_table, table_stride):
+    """Host lengths as arrays, and the table's row stride (of a tensor [n_seqs][width], its own)."""
+    lens, pasts = _i32s(seq_lens), _i64s(past_lens)
+    if len(lens) != len(pasts):
+        raise ValueError("one past length per sequence")
+    if table_stride is None:
+        table_stride = 0 if page_table is None else page_table.stride(0)
+        if page_table is not None and page_table.shape[0] < len(lens):
+            raise ValueError(f"page_table needs {len(lens)} rows, got {page_table.shape[0]}")
+    return lens, pasts, table_stride
+
+
+def infllm_paged_append(p, rot, pages, seq_lens, past_lens, page_table, q, q_strides, q_out, q_out_strides, k, v,
+                        kv_strides, table_stride=None, stream=None):
+    """seq_lens, past_lens: host ints, one of each per sequence; page_table: int32 tensor [n_seqs][pages of a sequence];
+    rot, and q with q_out, may be None."""
+    lens, pasts, stride = _seqs(seq_lens, past_lens, page_table, table_stride)
+    qs, qos = q_strides or (0, 0), q_out_strides or (0, 0)
+    _check("infllm_paged_append", lib().infllm_paged_append(
+        ctypes.byref(p), None if rot is None else ctypes.byref(rot), ctypes.byref(pages), len(lens), _at(lens),
+        _at(pasts), _ptr(page_table), stride, _ptr(q), qs[0], qs[1], _ptr(q_out), qos[0], qos[1], _ptr(k), _ptr(v),
+        kv_strides[0], kv_strides[1], _stream(stream)))
+
+
+def infllm_paged_workspace_bytes(p, pages, seq_lens, past_lens, score=None) -> int:
+    lens, pasts, _ = _seqs(seq_lens, past_lens, None, 0)
+    return int(lib().infllm_paged_workspace_bytes(ctypes.byref(p), ctypes.byref(pages), len(lens), _at(lens), _at(pasts),
+                                                  None if score is None else ctypes.byref(score)))
+
+
+def infllm_paged_attend(p, pages, seq_lens, past_lens, page_table, score, q, q_strides, out, out_strides, lse=None,
+                        workspace=None, workspace_bytes=None, table_stride=None, stream=None):
+    """As infllm_paged_append; score: a ScoreForm, or None."""
+    lens, pasts, stride = _seqs(seq_lens, past_lens, page_table, table_stride)
+    _check("infllm_paged_attend", lib().infllm_paged_attend(
+        ctypes.byref(p), ctypes.byref(pages), len(lens), _at(lens), _at(pasts), _ptr(page_table), stride,
+        None if score is None else ctypes.byref(score), _ptr(q), q_strides[0], q_strides[1], _ptr(out), out_strides[0],
+        out_strides[1], _ptr(lse), _ptr(workspace), _wb(workspace, workspace_bytes), _stream(stream)))
+
+
 # ------------------------------------------------------------------ allocation plumbing
 @dataclasses.dataclass
 class LayerMemory:
@@ -383,3 +476,29 @@ def recommended_ring(p: Params, chunk: int) -> int:
     """Ring slots that cover the oldest window unit construction can still need, plus one chunk, so
     that infllm_step can run unit construction and the append in a single launch."""
     return p.n_local + p.block_size + 2 * chunk + 1
+
+
+def rotary(inv_freq, interleaved=False, magnitude=1.0, norm=False, q_weight=None, k_weight=None, eps=1e-6) -> Rotary:
+    """Rotation by the given frequencies (two dimensions each; an empty list turns nothing) and, with norm, per-head
+    norms with weights of head_dim elements (None: ones).  The struct keeps the weights alive."""
+    table = (ctypes.c_double * max(1, len(inv_freq)))(*[float(x) for x in inv_freq])
+    r = Rotary(2 * len(inv_freq), int(bool(interleaved)), ctypes.cast(table, ctypes.POINTER(ctypes.c_double)), magnitude,
+               int(bool(norm)), eps, _ptr(q_weight) if norm else None, _ptr(k_weight) if norm else None)
+    r._held = (table, q_weight, k_weight)  # the struct holds raw pointers
+    return r
+
+
+def pages(k, v, page_size, page_stride=None, token_stride=None, head_stride=None) -> Pages:
+    """Pages in tensors k and v whose first dimension counts them: by default [n_pages][Hkv][page_size][D] with the
+    tensors' own strides."""
+    st = Pages(k.shape[0], page_size, k.data_ptr(), v.data_ptr(), k.stride(0) if page_stride is None else page_stride,
+               k.stride(2) if token_stride is None else token_stride, k.stride(1) if head_stride is None else head_stride)
+    st._held = (k, v)
+    return st
+
+
+def score(softcap=0.0, window=0, n_init=0, slopes=None) -> ScoreForm:
+    """slopes: float32 tensor of one per query head, or None.  The struct keeps it alive."""
+    st = ScoreForm(softcap, window, n_init, _ptr(slopes))
+    st._held = slopes
+    return st
