@@ -123,6 +123,130 @@ void set_rotary(const infllm_params* p, const infllm_rotary* r, RotateArgs* a) {
 // Whether a rotation's launch, at most a wave per row of a token, stays within 2^31 waves.
 bool rotate_fits(int64_t tokens, int64_t rows) { return (__int128)tokens * rows < INT32_MAX / 64; }
 
+// Microseconds of a workgroup of the attention, for each tile of keys and beside them: with
+// the whole chip at work, and of one that runs longer than the others.
+struct ItemCost {
+  float tile, item, lone_tile, lone_item;
+};
+ItemCost item_cost(const PagedArgs& a, bool thin) {
+  const bool wide = a.head_dim == 128;
+  if (a.bf16) {
+    if (thin) return wide ? ItemCost{1.2f, 6.f, 0.8f, 6.f} : ItemCost{0.8f, 6.f, 0.6f, 6.f};
+    return wide ? ItemCost{1.76f, 9.f, 0.95f, 6.5f} : ItemCost{0.96f, 8.5f, 0.72f, 5.5f};
+  }
+  return wide ? ItemCost{6.6f, 12.f, 6.6f, 12.f} : ItemCost{6.2f, 10.f, 4.2f, 8.f};
+}
+// Workgroups that run at a time: by their LDS (bf16 two to a compute unit), float32 by
+// their registers too.
+int resident_wgs(const PagedArgs& a) {
+  if (a.bf16) return 512;
+  if (a.head_dim == 128) return a.rows_log2 == 7 ? 256 : 512;
+  return a.rows_log2 == 7 ? 512 : 1024;
+}
+constexpr float kMergeCost = 6.f;            // microseconds of a merge's launch
+constexpr float kPartialByteCost = 2.5e-7f;  // of a byte of a partial row, written and read
+constexpr float kReadRate = 5.4e6f;          // bytes of keys and values per microsecond
+constexpr int kMostParts = 128;              // of a row tile
+
+// Key parts and item numbers of the sequences in a->seqs; false where an item or its
+// partial rows have no number.  A launch lasts as long as its work shared over the
+// workgroups that run at a time, as its keys' bytes, or as a part, and where the parts do
+// not all start at once about half a part more; a split costs the merge.
+bool plan(PagedArgs* a) {
+  const int n = a->seqs.n_seqs, G = (int)a->d_group.d, Hkv = a->n_kv_heads;
+  auto len = [&](int i) { return a->seqs.start[i + 1] - a->seqs.start[i]; };
+  int most = 0;
+  int64_t most_rows = 0;
+  for (int i = 0; i < n; ++i) most_rows = std::max(most_rows, (int64_t)len(i) * G);
+  a->key_tile = a->bf16 ? 64 : 32;
+  a->rows_log2 = a->bf16 || most_rows > 64 ? 7 : most_rows > 32 ? 6 : 5;
+  const int rows_wg = 1 << a->rows_log2;
+  a->tile_queries = (rows_wg - 1) / G + 2;
+  a->item_rows = (int)std::min<int64_t>(rows_wg, (most_rows + 7) / 8 * 8);
+  // by sequence: row tiles, most key tiles of one, key tiles of all of them
+  int tiles[kMaxPaged], keys[kMaxPaged];
+  float work = 0.f, bytes = 0.f;
+  int64_t row_tiles = 0;
+  const float tile_bytes = (float)(a->key_tile * a->head_dim * (a->bf16 ? 4 : 8));
+  for (int i = 0; i < n; ++i) {
+    tiles[i] = keys[i] = 0;
+    if (len(i) == 0) continue;
+    tiles[i] = paged_row_tiles(*a, G, len(i));
+    keys[i] = paged_most_tiles(*a, a->seqs.past[i], len(i));
+    const int first = paged_range(*a, a->seqs.past[i], 0, std::min(len(i), a->tile_queries) - 1).n;
+    const float tile = item_cost(*a, (int64_t)len(i) * G <= 32).tile;
+    work += tile * (float)tiles[i] * 0.5f * (float)(first + keys[i]);
+    bytes += tile_bytes * (float)keys[i];
+    row_tiles += tiles[i];
+    most = std::max(most, keys[i]);
+  }
+  const ItemCost cost = item_cost(*a, most_rows <= 32);
+  const float share = (float)Hkv / (float)resident_wgs(*a);
+  float best = -1.f;
+  for (int c = 1; c <= kMostParts; c += std::max(1, c / 4)) {
+    const int T = (most + c - 1) / c;
+    if (c > 1 && T < 2) break;
+    int64_t items = 0;
+    for (int i = 0; i < n; ++i)
+      if (tiles[i] > 0) items += (int64_t)tiles[i] * ((keys[i] + T - 1) / T);
+    const float even = std::max(share * (work + (float)items * cost.item), (float)Hkv * bytes / kReadRate);
+    const float part = (float)T * cost.lone_tile + cost.lone_item;
+    float t = std::max(even, part);
+    if (items > row_tiles) {
+      if ((float)items * share > 1.f) t = std::max(even, part + 0.5f * (float)T * cost.tile + cost.item);
+      t += kMergeCost + (float)items * (float)(Hkv * a->item_rows) * (float)(a->head_dim * 2 + 8) * kPartialByteCost;
+    }
+    if (best < 0.f || t < best) {
+      best = t;
+      a->part_tiles = T;
+    }
+    if (even >= part) break;  // (more parts add nothing but workgroups)
+  }
+  a->d_part = fast_div(a->part_tiles);
+  int64_t items = 0;
+  for (int i = 0; i < n; ++i) {
+    a->first[i] = (int32_t)items;
+    if (tiles[i] > 0) items += (int64_t)tiles[i] * ((keys[i] + a->part_tiles - 1) / a->part_tiles);
+    if (items * Hkv * 128 > INT32_MAX) return false;
+  }
+  a->items = (int)items;
+  return true;
+}
+// Partial rows of a launch (0 where no row tile has several parts).
+int64_t partial_rows(const PagedArgs& a) {
+  for (int i = 0; i < a.seqs.n_seqs; ++i) {
+    const int len = a.seqs.start[i + 1] - a.seqs.start[i];
+    if (len > 0 && paged_most_tiles(a, a.seqs.past[i], len) > a.part_tiles)
+      return (int64_t)a.items * a.n_kv_heads * a.item_rows;
+  }
+  return 0;
+}
+
+bool numbers_fit(const infllm_params* p, int64_t total) {
+  return (__int128)total * p->n_q_heads <= INT32_MAX && total * (p->n_q_heads / p->n_kv_heads) <= INT32_MAX - 127;
+}
+
+// The shape fields of `a`, without the sequences.
+void set_shape(const infllm_params* p, const infllm_pages* pages, const infllm_score_form* score, PagedArgs* a) {
+  std::memset(a, 0, sizeof(*a));
+  a->n_q_heads = p->n_q_heads;
+  a->n_kv_heads = p->n_kv_heads;
+  a->head_dim = p->head_dim;
+  a->bf16 = p->dtype == INFLLM_BF16;
+  a->sm_scale = p->sm_scale;
+  if (score != nullptr) {
+    a->softcap = score->softcap;
+    a->window = score->window;
+    a->n_init = score->n_init;
+    a->slopes = score->slopes;
+  }
+  a->d_group = fast_div(p->n_q_heads / p->n_kv_heads);
+  a->d_kv = fast_div(p->n_kv_heads);
+  a->head_stride = pages->head_stride;
+  a->page16 = (uint32_t)(pages->page_stride * esize(p) / 16);
+  a->token16 = (uint32_t)(pages->token_stride * esize(p) / 16);
+}
+
 infllm_status check_score(const infllm_score_form* s) {
   if (s == nullptr) return INFLLM_OK;
   if (!std::isfinite(s->softcap) || s->softcap < 0.f || s->window < 0 || s->n_init < 0) return INFLLM_E_SHAPE;
@@ -274,7 +398,23 @@ infllm_status infllm_paged_append(const infllm_params* p, const infllm_rotary* r
 
 size_t infllm_paged_workspace_bytes(const infllm_params* p, const infllm_pages* pages, int32_t n_seqs,
                                     const int32_t* seq_lens, const int64_t* past_lens, const infllm_score_form* score) {
-  return 0;
+  int64_t total;
+  if (check_params(p) != INFLLM_OK || check_pages(p, pages) != INFLLM_OK || check_score(score) != INFLLM_OK ||
+      check_seqs(pages, n_seqs, seq_lens, past_lens, INT32_MAX, &total) != INFLLM_OK || !numbers_fit(p, total))
+    return 0;
+  PagedArgs a;
+  set_shape(p, pages, score, &a);
+  size_t most = 0;
+  int64_t at = 0;
+  for (int i = 0; i < n_seqs; i += kMaxPaged) {
+    const int64_t from = at;
+    fill_seqs(pages, n_seqs, seq_lens, past_lens, nullptr, 0, i, at, &a.seqs);
+    at = a.seqs.start[a.seqs.n_seqs];
+    if (at == from) continue;
+    if (!plan(&a)) return 0;
+    most = std::max(most, (size_t)partial_rows(a) * part_row_bytes(p));
+  }
+  return (most + 255) & ~(size_t)255;
 }
 
 infllm_status infllm_paged_attend(const infllm_params* p, const infllm_pages* pages, int32_t n_seqs,
@@ -298,25 +438,12 @@ infllm_status infllm_paged_attend(const infllm_params* p, const infllm_pages* pa
   if (!span_fits(p, total, q_token_stride, p->n_q_heads, q_head_stride) ||
       !span_fits(p, total, out_token_stride, p->n_q_heads, out_head_stride))
     return INFLLM_E_UNSUPPORTED;
-  const int64_t G = p->n_q_heads / p->n_kv_heads;
-  if (total > INT32_MAX / G || (__int128)total * p->n_q_heads > INT32_MAX) return INFLLM_E_UNSUPPORTED;
-  // (keys are addressed by 16-byte pieces in 32 bits)
+  if (!numbers_fit(p, total)) return INFLLM_E_UNSUPPORTED;
+  // (keys are addressed by 16-byte pieces in 32 bits; the last number stands for no row)
   const __int128 span = (__int128)(pages->n_pages - 1) * pages->page_stride + (__int128)(pages->page_size - 1) * pages->token_stride;
-  if (span * esize(p) / 16 >= 0xFFFFFFFFll) return INFLLM_E_UNSUPPORTED;
-  if ((st = check_device()) != INFLLM_OK) return st;
+  if (span * esize(p) / 16 >= 0xFFFFFFFFll - p->head_dim) return INFLLM_E_UNSUPPORTED;
   PagedArgs a;
-  std::memset(&a, 0, sizeof(a));
-  a.n_q_heads = p->n_q_heads;
-  a.n_kv_heads = p->n_kv_heads;
-  a.head_dim = p->head_dim;
-  a.bf16 = p->dtype == INFLLM_BF16;
-  a.sm_scale = p->sm_scale;
-  if (score != nullptr) {
-    a.softcap = score->softcap;
-    a.window = score->window;
-    a.n_init = score->n_init;
-    a.slopes = score->slopes;
-  }
+  set_shape(p, pages, score, &a);
   a.q = q;
   a.k = pages->k;
   a.v = pages->v;
@@ -327,15 +454,36 @@ infllm_status infllm_paged_attend(const infllm_params* p, const infllm_pages* pa
   a.out_tok = out_token_stride;
   a.out_head = out_head_stride;
   a.lse_stride = total;
-  a.page_stride = pages->page_stride;
-  a.token_stride = pages->token_stride;
-  a.head_stride = pages->head_stride;
+  // every launch is planned before the first is enqueued (a call's only one is kept)
+  const bool single = n_seqs <= kMaxPaged;
+  size_t need = 0;
   int64_t at = 0;
   for (int i = 0; i < n_seqs; i += kMaxPaged) {
+    const int64_t from = at;
     fill_seqs(pages, n_seqs, seq_lens, past_lens, page_table, table_stride, i, at, &a.seqs);
-    const bool any = a.seqs.start[a.seqs.n_seqs] > at;
     at = a.seqs.start[a.seqs.n_seqs];
-    if (any && (st = launch_status(launch_paged(a, (hipStream_t)stream))) != INFLLM_OK) return st;
+    if (at == from) continue;
+    if (!plan(&a)) return INFLLM_E_UNSUPPORTED;
+    need = std::max(need, (size_t)partial_rows(a) * part_row_bytes(p));
+  }
+  if (need > 0) {
+    if (workspace == nullptr || workspace_bytes < need) return INFLLM_E_WORKSPACE;
+    if (!aligned16(workspace)) return INFLLM_E_SHAPE;
+  }
+  if ((st = check_device()) != INFLLM_OK) return st;
+  at = 0;
+  for (int i = 0; i < n_seqs; i += kMaxPaged) {
+    if (!single) {
+      const int64_t from = at;
+      fill_seqs(pages, n_seqs, seq_lens, past_lens, page_table, table_stride, i, at, &a.seqs);
+      at = a.seqs.start[a.seqs.n_seqs];
+      if (at == from) continue;
+      plan(&a);
+    }
+    const int64_t rows = partial_rows(a);
+    if (rows > 0) partial_layout(p, workspace, 1, rows, &a.part_o, &a.part_lse, &a.part_exp);
+    if ((st = launch_status(launch_paged(a, (hipStream_t)stream))) != INFLLM_OK) return st;
+    if (rows > 0 && (st = launch_status(launch_paged_merge(a, (hipStream_t)stream))) != INFLLM_OK) return st;
   }
   return INFLLM_OK;
 }

@@ -9,6 +9,7 @@
 // least half as many as a workgroup has groups: a workgroup per row, its threads split into groups that take every GR-th part and are
 // joined in LDS -- the parts are then the only parallelism (25 parts of 32 rows: 6.8 us
 // one thread per piece, 4.3 split; 16 parts of 2,048 rows: 3.7 and 6.5).
+#include "paged.h"
 #include "shared.h"
 
 namespace infllm {
@@ -282,6 +283,61 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixArgs a) {
   }
 }
 
+// Paged attention: the parts of a row tile's rows.  The workgroups of an item that is a row
+// tile's first part join its parts' rows (the item numbers of a row tile's parts are
+// consecutive), those of others end at once.  SPLIT: few rows to an item (decoding), a wave
+// per row whose lane groups take every GR-th part; else a group of lanes per row.
+template <typename T, bool HALF, int D, bool SPLIT>
+__global__ void __launch_bounds__(256) paged_merge_kernel(PagedArgs a) {
+  constexpr int DPT = HALF ? 8 : 4, TPR = D / DPT, GR = SPLIT ? 64 / TPR : 1, CH = 8;
+  const int item = div_by(blockIdx.x, a.d_kv), g = (int)blockIdx.x - item * (int)a.d_kv.d;
+  const PagedWork w = paged_work(a, item);
+  if (w.part != 0) return;
+  const int G = (int)a.d_group.d, rows_wg = 1 << a.rows_log2, R = G * w.len, tile0 = w.rt * rows_wg;
+  const int i0 = div_by(tile0, a.d_group), i1 = div_by(min(R, tile0 + rows_wg) - 1, a.d_group);
+  const int n = paged_range(a, w.past, i0, i1).n;
+  if (n <= a.part_tiles) return;
+  const int parts = div_by(n + a.part_tiles - 1, a.d_part);
+  const int r = blockIdx.y * (256 / (TPR * GR)) + threadIdx.x / (TPR * GR);
+  if (r >= min(rows_wg, R - tile0)) return;
+  const int grp = SPLIT ? (threadIdx.x / TPR) % GR : 0, c = threadIdx.x % TPR;
+  const int64_t row0 = ((int64_t)item * a.n_kv_heads + g) * a.item_rows + r, step = (int64_t)a.n_kv_heads * a.item_rows;
+  float M = -__builtin_inff(), tot = 0.f, acc[DPT] = {};
+  for (int p0 = grp; p0 < parts; p0 += CH * GR) {
+    float l[CH], o[CH][DPT];
+#pragma unroll
+    for (int j = 0; j < CH; ++j) load_piece<HALF>(a, row0 + min(p0 + j * GR, parts - 1) * step, c, o[j], l[j]);
+    add_parts<DPT, CH, true>(l, o, (parts - p0 + GR - 1) / GR, p0 > grp, M, tot, acc);
+  }
+  if constexpr (SPLIT) {
+#pragma unroll
+    for (int o = TPR; o < 64; o <<= 1) {
+      const float M2 = __shfl_xor(M, o), tot2 = __shfl_xor(tot, o), m_new = fmaxf(M, M2);
+      const float w1 = M == -__builtin_inff() ? 0.f : expf(M - m_new), w2 = M2 == -__builtin_inff() ? 0.f : expf(M2 - m_new);
+      tot = tot * w1 + tot2 * w2;
+#pragma unroll
+      for (int e = 0; e < DPT; ++e) {
+        const float x2 = __shfl_xor(acc[e], o);
+        acc[e] = (M == -__builtin_inff() ? 0.f : acc[e] * w1) + (M2 == -__builtin_inff() ? 0.f : x2 * w2);
+      }
+      M = m_new;
+    }
+    if (grp != 0) return;
+  }
+  const int i = div_by(tile0 + r, a.d_group), h = g * G + tile0 + r - i * G;
+  store_row_piece<T, DPT>((T*)a.out + (int64_t)(w.start + i) * a.out_tok + (int64_t)h * a.out_head + DPT * c,
+                          a.lse != nullptr && c == 0 ? a.lse + h * a.lse_stride + w.start + i : nullptr, M, tot, acc);
+}
+template <typename T, bool HALF, int D>
+void launch_paged_merge_t(const PagedArgs& a, hipStream_t s) {
+  constexpr int groups = 256 / (D / (HALF ? 8 : 4));  // of a workgroup
+  const bool split = a.item_rows <= 16;
+  const int per_wg = split ? 4 : groups;
+  const dim3 grid(a.items * a.n_kv_heads, (a.item_rows + per_wg - 1) / per_wg), block(256);
+  if (split) hipLaunchKernelGGL((paged_merge_kernel<T, HALF, D, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((paged_merge_kernel<T, HALF, D, false>), grid, block, 0, s, a);
+}
+
 constexpr int kManyRows = 1024;  // most rows whose many parts are split over threads
 
 template <typename T, bool HALF>
@@ -329,6 +385,13 @@ hipError_t launch_prefix_merge(const PrefixArgs& a, hipStream_t s) {
   else if (a.bf16) hipLaunchKernelGGL((prefix_merge_kernel<bf16_t, true, 64>), grid, block, 0, s, a);
   else if (wide) hipLaunchKernelGGL((prefix_merge_kernel<float, false, 128>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((prefix_merge_kernel<float, false, 64>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_merge(const PagedArgs& a, hipStream_t s) {
+  const bool wide = a.head_dim == 128;
+  if (a.bf16) wide ? launch_paged_merge_t<bf16_t, true, 128>(a, s) : launch_paged_merge_t<bf16_t, true, 64>(a, s);
+  else wide ? launch_paged_merge_t<float, false, 128>(a, s) : launch_paged_merge_t<float, false, 64>(a, s);
   return hipGetLastError();
 }
 

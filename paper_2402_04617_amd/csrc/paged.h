@@ -62,7 +62,13 @@ struct RotateArgs {
 };
 hipError_t launch_rotate(const RotateArgs& a, hipStream_t s);
 
-// Attention over pages.
+// Attention over pages.  A row tile is a run of rows (query-major, the group's heads
+// packed) of one sequence.  The key tiles that a row tile sees, in order, are those of the
+// initial tokens that lie before the window, then [first of the window, diagonal]; they
+// are cut into parts of part_tiles.  An item is a part of a row tile (the sequences in
+// their order, of a sequence the last row tile first, of a row tile its parts in order), a
+// workgroup an item and a kv head.  Row tiles with several parts leave partial rows (see
+// common.h), item_rows of them per item and kv head, and a merge.
 struct PagedArgs {
   int n_q_heads, n_kv_heads, head_dim;
   bool bf16;
@@ -75,9 +81,96 @@ struct PagedArgs {
   void* out;
   float* lse;
   int64_t q_tok, q_head, out_tok, out_head, lse_stride;
-  int64_t page_stride, token_stride, head_stride;
+  int64_t head_stride;
+  uint32_t page16, token16;  // strides of pages and their tokens in pieces of 16 bytes (modulo 2^32)
+  int rows_log2;             // rows of a row tile
+  int tile_queries;          // most queries with rows in one row tile
+  int key_tile;              // keys of a tile
+  int part_tiles;
+  int items, item_rows;
+  FastDiv d_group, d_kv, d_part;
+  void* part_o;
+  float* part_lse;
+  int32_t* part_exp;
   PagedSeqs seqs;
+  int32_t first[kMaxPaged];  // first item of a sequence
 };
+static_assert(sizeof(PagedArgs) <= 4096, "arguments of a launch");
+
+// Keys of a row tile whose first and last queries are i0 and i1 of a sequence with `past`
+// tokens before: tiles [0, sink) and [low, low + n - sink).
+struct PagedRange {
+  int sink, low, n;
+};
+__host__ __device__ inline PagedRange paged_range(const PagedArgs& a, int past, int i0, int i1) {
+  PagedRange r;
+  const int end = (past + i1) / a.key_tile + 1;
+  r.low = a.window > 0 ? (past + i0 >= a.window ? past + i0 - a.window + 1 : 0) / a.key_tile : 0;
+  const int init = a.n_init < past + i1 + 1 ? a.n_init : past + i1 + 1;
+  r.sink = (init + a.key_tile - 1) / a.key_tile;
+  if (r.sink > r.low) r.sink = r.low;
+  r.n = r.sink + end - r.low;
+  return r;
+}
+// Most tiles that a row tile of a sequence sees (its items are as many parts for each).
+__host__ __device__ inline int paged_most_tiles(const PagedArgs& a, int past, int len) {
+  const int total = past + len, whole = (total - 1) / a.key_tile + 1;
+  if (a.window == 0) return whole;
+  const int queries = a.tile_queries < len ? a.tile_queries : len;
+  const int64_t keys = (int64_t)(a.window < total ? a.window : total) + queries - 1;
+  const int init = a.n_init < total ? a.n_init : total;
+  const int64_t most = (init + a.key_tile - 1) / a.key_tile + (keys - 1) / a.key_tile + 2;
+  return most < whole ? (int)most : whole;
+}
+__host__ __device__ inline int paged_row_tiles(const PagedArgs& a, int group, int len) {
+  return (int)(((int64_t)len * group + (1 << a.rows_log2) - 1) >> a.rows_log2);
+}
+
+// Where a workgroup of item `item` works.
+struct PagedWork {
+  int s, start, len, past;  // the sequence
+  int rt, part;
+};
+__device__ __forceinline__ PagedWork paged_work(const PagedArgs& a, int item) {
+  constexpr int CH = kMaxPaged / kWave;
+  const int lane = threadIdx.x & 63;
+  int first[CH], start[CH], end[CH], past[CH], n = 0;
+#pragma unroll
+  for (int j = 0; j < CH; ++j) {
+    if (j * kWave >= a.seqs.n_seqs) break;
+    const int i = j * kWave + lane;
+    first[j] = a.first[i];
+    start[j] = a.seqs.start[i];
+    end[j] = a.seqs.start[i + 1];
+    past[j] = a.seqs.past[i];
+  }
+#pragma unroll
+  for (int j = 0; j < CH; ++j) {
+    if (j * kWave >= a.seqs.n_seqs) break;
+    n += __popcll(__ballot(j * kWave + lane < a.seqs.n_seqs && first[j] <= item));
+  }
+  // (sequences without new tokens have no items: the last one that begins at or before)
+  const int s = __builtin_amdgcn_readfirstlane(n) - 1;
+  auto pick = [&](const int (&x)[CH]) {
+    int v = __builtin_amdgcn_readlane(x[0], s & 63);
+#pragma unroll
+    for (int j = 1; j < CH; ++j)
+      if (s >> 6 == j) v = __builtin_amdgcn_readlane(x[j], s & 63);
+    return v;
+  };
+  PagedWork w;
+  w.s = s;
+  w.start = pick(start);
+  w.len = pick(end) - w.start;
+  w.past = pick(past);
+  const int parts = div_by(paged_most_tiles(a, w.past, w.len) + a.part_tiles - 1, a.d_part);
+  const int tiles = paged_row_tiles(a, (int)a.d_group.d, w.len), u = item - pick(first);
+  const int down = parts == 1 ? u : tiles == 1 ? 0 : u / parts;
+  w.part = u - down * parts;
+  w.rt = tiles - 1 - down;
+  return w;
+}
 hipError_t launch_paged(const PagedArgs& a, hipStream_t s);
+hipError_t launch_paged_merge(const PagedArgs& a, hipStream_t s);
 
 }  // namespace infllm

@@ -1,85 +1,955 @@
-// Causal attention of new tokens over paged keys and values (infllm_paged_attend).
+// Causal attention of new tokens over paged keys and values (infllm_paged_attend), bf16 on
+// CDNA4 matrix cores (v_mfma_f32_32x32x16_bf16), fp32 accumulation.
+//
+//   O_i = sum_t softmax_t(z_it) v_t,  z_it = f(sm_scale q_i . k_t) - slope (p_i - t)
+//
+// over the visible keys t of the sequence, f the cap c tanh(x / c) or nothing.
+//
+// A workgroup has a row tile of 128 (query, head) rows of one kv head (four waves of 32)
+// and a part of the key tiles that it sees; two workgroups share a compute unit.  Keys come
+// in tiles of 64 through two LDS buffers of K and of V, loaded directly, each lane from an
+// address of its own: the page of every group of 8 keys (of every key, where the page size
+// is no multiple of 8) is looked up ahead into a table in LDS, as the place of the row in
+// pieces of 16 bytes, which 32 bits hold up to 64 GiB of pages.
+// Per wave and key tile, as in the step's attention: S^T = K Q^T with the keys from LDS and
+// the query rows in registers, so that a lane has 16 scores of one row for each of two key
+// blocks; P^T = exp2(z - m) is the B operand of O^T += V^T P^T as it stands, V^T read
+// transposed.  Products of one tile run beside the exponentials of another.
+#include <type_traits>
+
+#include "mfma_tile.h"
 #include "paged.h"
 
 namespace infllm {
+
 namespace {
 
-// One wave per (new token, query head): 64 keys at a time, a key per lane for the scores,
-// D / 64 dims per lane for the values.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) paged_rows_kernel(PagedArgs a) {
-  constexpr int DPL = D / 64;
-  __shared__ float qs[4][D];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t first = a.seqs.start[0], tokens = a.seqs.start[a.seqs.n_seqs] - first;
-  const int64_t item = (int64_t)blockIdx.x * 4 + wave;
-  const int64_t t = first + item / a.n_q_heads;
-  const int h = (int)(item % a.n_q_heads);
-  if (t >= first + tokens) return;
-  const int s = paged_seq_of(a.seqs, (int)t);
-  const int pos = a.seqs.past[s] + ((int)t - a.seqs.start[s]);
-  const T* q = (const T*)a.q + t * a.q_tok + h * a.q_head;
-  for (int d = lane; d < D; d += 64) qs[wave][d] = Elem<T>::load(q + d);
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
-  const int64_t head = (h / (a.n_q_heads / a.n_kv_heads)) * a.head_stride;
-  const float slope = a.slopes != nullptr ? a.slopes[h] : 0.f;
-  const int low = a.window > 0 ? max(0, pos - a.window + 1) : 0;  // first key of the window
-  float m = -__builtin_inff(), l = 0.f, acc[DPL] = {};
-  for (int t0 = 0; t0 <= pos; t0 += 64) {
-    if (t0 >= a.n_init && t0 + 64 <= low) {
-      t0 = low / 64 * 64 - 64;
-      continue;
-    }
-    const int key = t0 + lane;
-    int64_t at = -1;
-    float z = -__builtin_inff();
-    if (key <= pos && (key >= low || key < a.n_init)) {
-      const int x = div_by(key, a.seqs.d_page), page = a.seqs.table[s * a.seqs.table_stride + x];
-      if (page >= 0 && page < a.seqs.n_pages) {
-        at = page * a.page_stride + (key - x * a.seqs.page_size) * a.token_stride + head;
-        float dot = 0.f;
-        for (int d = 0; d < D; ++d) dot = __builtin_fmaf(qs[wave][d], Elem<T>::load((const T*)a.k + at + d), dot);
-        z = dot * a.sm_scale;
-        if (a.softcap > 0.f) z = a.softcap * tanhf(z / a.softcap);
-        if (a.slopes != nullptr) z -= slope * (float)(pos - key);
-      }
-    }
-    const float m_new = fmaxf(m, wave_max(z));
-    const bool nan = __ballot(z != z) != 0;
-    if (m_new == -__builtin_inff() && !nan) continue;
-    const float corr = m == -__builtin_inff() ? 0.f : expf(m - m_new);
-    const float p = at >= 0 ? expf(z - m_new) : 0.f;
-    l = l * corr + wave_sum(p);
-    m = m_new;
-    for (int e = 0; e < DPL; ++e) acc[e] *= corr;
-    for (int j = 0; j < 64; ++j) {
-      const int64_t aj = __shfl(at, j);
-      const float pj = __shfl(p, j);
-      if (aj < 0) continue;
-      for (int e = 0; e < DPL; ++e) acc[e] = __builtin_fmaf(pj, Elem<T>::load((const T*)a.v + aj + DPL * lane + e), acc[e]);
-    }
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  T* o = (T*)a.out + t * a.out_tok + h * a.out_head;
-  for (int e = 0; e < DPL; ++e) Elem<T>::store(o + DPL * lane + e, acc[e] * inv);
-  if (lane == 0 && a.lse != nullptr) a.lse[h * a.lse_stride + t] = l == 0.f ? -__builtin_inff() : m + logf(l);
+constexpr int kCap = 1, kSlopes = 2;  // what scores become
+constexpr int kTable = 1024;          // key groups whose places are in LDS
+constexpr int kAhead = 3;             // a step looks up the tile that many ahead
+
+template <int D>
+struct PagedSmem {
+  bf16_t k[2][KB * D];
+  bf16_t v[2][KB * D];
+  uint32_t rows[kTable];  // place of a key group's first row in pieces of 16 bytes, or kNoRow
+  int bad[4];             // whether a wave met a page that is not there
+};
+
+// The kernel's arguments, read where they are used rather than held through the loop.
+typedef const __attribute__((address_space(4))) PagedArgs LateArgs;
+__device__ __forceinline__ LateArgs& late_args() {
+  LateArgs* p = (LateArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *p;
 }
 
-template <typename T>
-void launch_t(const PagedArgs& a, hipStream_t s) {
-  const int64_t items = (int64_t)(a.seqs.start[a.seqs.n_seqs] - a.seqs.start[0]) * a.n_q_heads;
-  const dim3 grid((unsigned)((items + 3) / 4)), block(256);
-  if (a.head_dim == 128) hipLaunchKernelGGL((paged_rows_kernel<T, 128>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((paged_rows_kernel<T, 64>), grid, block, 0, s, a);
+// A sequence's row of the page table.
+struct PageRow {
+  const int32_t* table;
+  FastDiv d_page;
+  int page_size, n_pages;
+  uint32_t page16, token16;
+  // Place of a key in pieces of 16 bytes, given its page's entry x; kNoRow where that is not followed.
+  __device__ __forceinline__ uint32_t place(int key, int x, int32_t page) const {
+    const bool there = page >= 0 && page < n_pages;
+    return there ? (uint32_t)page * page16 + (uint32_t)(key - x * page_size) * token16 : kNoRow;
+  }
+  __device__ __forceinline__ uint32_t place(int key) const {
+    const int x = div_by(key, d_page);
+    return place(key, x, table[x]);
+  }
+};
+__device__ __forceinline__ PageRow page_row(int s) {
+  LateArgs& a = late_args();
+  return PageRow{a.seqs.table + s * a.seqs.table_stride, FastDiv{a.seqs.d_page.d, a.seqs.d_page.mul}, a.seqs.page_size,
+                 a.seqs.n_pages, a.page16, a.token16};
+}
+
+// The key tiles of a workgroup's part, in order, and the table of their rows' places.
+template <int KT, int THREADS>
+struct KeyTiles {
+  int sink, shift;      // tile t < sink is at t * KT, others at (t + shift) * KT
+  int t_begin, t_end;   // the part's
+  int last;             // the sequence's last key
+  int seq;
+  int gshift;           // keys of a table entry: 8, or 1
+  int w0;               // first tile of the table's window
+  __device__ __forceinline__ int key_of(int t) const { return (t < sink ? t : t + shift) * KT; }
+  __device__ __forceinline__ int tile_groups() const { return KT >> gshift; }
+  __device__ __forceinline__ int window() const { return kTable / tile_groups(); }
+  // Fills the table from tile `first` on; whether a page was not there.
+  __device__ __forceinline__ bool fill(uint32_t* rows, int first) {
+    w0 = first;
+    const PageRow pr = page_row(seq);
+    const int gmask = (1 << gshift) - 1, count = min(kTable, (t_end - first) * tile_groups());
+    bool bad = false;
+    for (int i = threadIdx.x; i < count; i += THREADS) {
+      const int key = min(key_of(first + (i << gshift) / KT) + ((i << gshift) & (KT - 1)), last & ~gmask);
+      const uint32_t p = pr.place(key);
+      rows[i] = p;
+      bad |= p == kNoRow;
+    }
+    return bad;
+  }
+  // The same for the part's first window, and for the pages of the part behind it.
+  __device__ __forceinline__ bool fill_first(uint32_t* rows) {
+    bool bad = fill(rows, t_begin);
+    if (t_begin + window() < t_end) {
+      const PageRow pr = page_row(seq);
+      const int from = div_by(key_of(t_begin + window()), pr.d_page);
+      const int to = div_by(min(key_of(t_end - 1) + KT - 1, last), pr.d_page);
+      for (int x = from + (int)threadIdx.x; x <= to; x += THREADS) {
+        const int32_t page = pr.table[x];
+        bad |= page < 0 || page >= pr.n_pages;
+      }
+    }
+    return bad;
+  }
+};
+
+// What a row sees of a tile's keys from k0 on: a bit for each, the window and the initial
+// tokens taken into account.
+__device__ __forceinline__ uint64_t seen_keys(int pos, int k0, int window, int n_init) {
+  auto below = [](int x) {  // the first x of 64 bits
+    const int n = min(max(x, 0), 64);
+    return n == 0 ? 0ull : ~0ull >> (64 - n);
+  };
+  uint64_t vis = below(pos - k0 + 1);
+  if (window > 0) vis &= ~below(max(0, pos - window + 1) - k0) | below(n_init - k0);
+  return vis;
+}
+
+// One row formed by its wave from the keys that it sees in the tiles [t_begin, t_end), for
+// rows that a masked value which is not finite has reached: sum_t weight(q . k_t, t) v_t,
+// DPL dims a lane.
+template <typename T, int D, int KT, int THREADS, typename Weight>
+__device__ __forceinline__ void form_row(const KeyTiles<KT, THREADS>& keys, const char* kbase, const char* vbase, const T* qp,
+                                         int pos, int window, int n_init, Weight weight, float (&acc)[D / 64]) {
+  constexpr int DPL = D / 64;
+  const int lane = threadIdx.x & 63;
+  const PageRow pr = page_row(keys.seq);
+#pragma unroll
+  for (int e = 0; e < DPL; ++e) acc[e] = 0.f;
+  for (int t = keys.t_begin; t < keys.t_end; ++t) {
+    const int k0 = keys.key_of(t), key = k0 + lane;
+    uint32_t at = kNoRow;
+    if (lane < KT && ((seen_keys(pos, k0, window, n_init) >> lane) & 1u) != 0) at = pr.place(key);
+    float p = 0.f;
+    if (at != kNoRow) {
+      const T* kp = (const T*)(kbase + (uint64_t)at * 16);
+      float s = 0.f;
+      for (int d = 0; d < D; ++d) s = __builtin_fmaf(Elem<T>::load(kp + d), Elem<T>::load(qp + d), s);
+      p = weight(s, key);
+    }
+    for (uint64_t left = __ballot(at != kNoRow); left != 0; left &= left - 1) {
+      const int j = __builtin_ctzll(left);
+      const uint32_t aj = (uint32_t)__builtin_amdgcn_readlane((int)at, j);
+      const float pj = __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(p), j));
+      const T* vp = (const T*)(vbase + (uint64_t)aj * 16) + DPL * lane;
+#pragma unroll
+      for (int e = 0; e < DPL; ++e) acc[e] = __builtin_fmaf(pj, Elem<T>::load(vp + e), acc[e]);
+    }
+  }
+}
+
+template <int D, int MOD>
+__global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
+  constexpr int CH = D / 8;                       // 16-byte pieces of a row
+  constexpr int KSTEPS = D / 16, DBLK = D / 32;
+  constexpr int RPI = 64 / CH;                    // tile rows per load instruction
+  constexpr int NI = KB * D * 2 / (4 * 1024);     // load instructions per wave and tile (K or V)
+  constexpr uint32_t kTileBytes = KB * D * 2;
+  __shared__ __attribute__((aligned(256))) PagedSmem<D> sm;
+  static_assert(sizeof(sm) <= 80 * 1024, "two workgroups share a compute unit's LDS");
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, gsel = lane >> 5;
+  const int G = (int)a.d_group.d;
+  // the kv heads side by side (8 of them: one per XCD, whose L2 then holds its keys)
+  const int item = div_by(blockIdx.x, a.d_kv), g = (int)blockIdx.x - item * (int)a.d_kv.d;
+  const PagedWork w = paged_work(a, item);
+  const int R = G * w.len, tile0 = w.rt * 128;
+  const int i0 = div_by(tile0, a.d_group), i1 = div_by(min(R, tile0 + 128) - 1, a.d_group);
+  const PagedRange range = paged_range(a, w.past, i0, i1);
+  const int t_begin = w.part * a.part_tiles, t_end = min(t_begin + a.part_tiles, range.n);
+  if (t_begin >= t_end) return;  // (the parts of a sequence are as many for each of its row tiles)
+  const bool one_part = range.n <= a.part_tiles;
+  const int last = w.past + w.len - 1;
+  KeyTiles<KB, 256> keys{range.sink, range.low - range.sink, t_begin, t_end, last, w.s, (a.seqs.page_size & 7) == 0 ? 3 : 0, t_begin};
+  auto key_of = [&](int t) { return keys.key_of(t); };  // first key of tile t
+
+  const int row0 = tile0 + wave * 32, row = row0 + n;
+  const bool active = row0 < R;  // a wave without rows loads its share of the tiles
+  const int row_c = min(row, R - 1);
+  const int qi = div_by(row_c, a.d_group), qh = g * G + row_c - qi * G;
+  const int pos = w.past + qi;
+
+  const char* kbase = (const char*)a.k + g * a.head_stride * 2;
+  const char* vbase = (const char*)a.v + g * a.head_stride * 2;
+  // Load instruction j of wave w fills pieces [(NI*w + j)*64, +64) of a tile: rows lrow +
+  // RPI*j; a lane's slot holds piece (lane % CH) ^ swz(row) of its row.
+  const int lrow = KB / 4 * wave + lane / CH;
+  auto piece_of = [&](int j) { return (uint32_t)(lane % CH) ^ (uint32_t)swz<D>(lrow + RPI * j); };
+  const uint32_t lds_k0 = (uint32_t)(uintptr_t)(INFLLM_LDS bf16_t*)sm.k[0];
+  const uint32_t lds_v0 = (uint32_t)(uintptr_t)(INFLLM_LDS bf16_t*)sm.v[0];
+  const uint32_t lds_k = lds_k0 + NI * wave * 1024, lds_v = lds_v0 + NI * wave * 1024;
+  struct Places {
+    uint32_t o[NI];
+  };
+  auto load_k = [&](int buf, const Places& f, int j) {
+    lds_load_lane(lds_k + buf * kTileBytes + j * 1024, kbase + (uint64_t)f.o[j] * 16);
+  };
+  auto load_v = [&](int buf, const Places& f, int j) {
+    lds_load_lane(lds_v + buf * kTileBytes + j * 1024, vbase + (uint64_t)f.o[j] * 16);
+  };
+
+  // The first tile's pages, the table's, and the query rows are requested at once.
+  Places f0;
+  {
+    const PageRow pr = page_row(w.s);
+    int key[NI], x[NI], page[NI];
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      key[j] = min(key_of(t_begin) + lrow + RPI * j, last);
+      x[j] = div_by(key[j], pr.d_page);
+      page[j] = pr.table[x[j]];
+    }
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const uint32_t p = pr.place(key[j], x[j], page[j]);
+      f0.o[j] = (p == kNoRow ? 0u : p) + piece_of(j);  // (a row that is not there: page 0's, masked)
+    }
+  }
+  bf16x8 qreg[KSTEPS];
+  if (active) {
+    const bf16_t* qp = (const bf16_t*)a.q + (int64_t)(w.start + qi) * a.q_tok + (int64_t)qh * a.q_head + 8 * gsel;
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) qreg[s] = *(const bf16x8*)(qp + 16 * s);
+  }
+  float slope = 0.f;
+  if constexpr (MOD & kSlopes) slope = a.slopes[qh] * 1.4426950408889634f;
+
+  const int gshift = keys.gshift;
+  const uint32_t gmask = (1u << gshift) - 1u;
+  const bool bad = keys.fill_first(sm.rows);
+#pragma unroll
+  for (int j = 0; j < NI; ++j) load_k(0, f0, j);
+#pragma unroll
+  for (int j = 0; j < NI; ++j) load_v(0, f0, j);
+  {
+    const bool any = __ballot(bad) != 0;
+    if (lane == 0) sm.bad[wave] = any;
+  }
+  lds_barrier();
+  const bool has_bad = (sm.bad[0] | sm.bad[1] | sm.bad[2] | sm.bad[3]) != 0;
+
+  // Places of this lane's rows of tile t (past the part's end: of its last tile again,
+  // whose keys come from the cache and are not used).
+  const uint32_t lds_rows = (uint32_t)(uintptr_t)(INFLLM_LDS uint32_t*)sm.rows;
+  auto places = [&](int t, Places& f) {
+    t = min(t, t_end - 1);
+    const int in_tile = min(KB - 1, last - key_of(t));  // last row that is the sequence's
+    const uint32_t at = lds_rows + 4u * (uint32_t)((t - keys.w0) * keys.tile_groups());
+    const int lr = (int)opaque_v((uint32_t)lrow);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const uint32_t r = (uint32_t)min(lr + RPI * j, in_tile);
+      uint32_t p = *(const INFLLM_LDS uint32_t*)(uintptr_t)(at + 4u * (r >> gshift));
+      if (has_bad) p = p == kNoRow ? 0u : p;
+      f.o[j] = p + (r & gmask) * a.token16 + ((uint32_t)(lane % CH) ^ (uint32_t)swz<D>(lr + RPI * j));
+    }
+  };
+
+  // LDS offsets of the fragments; under the swizzle they are XOR-related (see attend_mfma).
+  constexpr uint32_t VX = D == 128 ? 32 : 0;
+  const uint32_t koff0 = 2u * tile_off<D>(n, gsel);
+  uint32_t voff0;
+  {
+    const int h = lane >> 4, q = (lane & 15) >> 2, m = lane & 3;
+    const int vr = 4 * (h >> 1) + q, d0 = 16 * (h & 1) + 4 * m;
+    voff0 = 2u * (tile_off<D>(vr, d0 >> 3) + (d0 & 7));
+  }
+  auto kfrag_at = [&](uint32_t kaddr, int kb, int s) {
+    return *(const INFLLM_LDS bf16x8*)(uintptr_t)((kaddr ^ (32u * s)) + kb * 64u * D);
+  };
+  auto vfrag_at = [&](uint32_t vaddr, int db, int j) {
+    const uint32_t a0 = (vaddr ^ (64u * db)) + j * 32u * D;
+    const uint32_t a1 = ((vaddr ^ (64u * db) ^ VX) + 16u * D) + j * 32u * D;
+    const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((INFLLM_LDS i16x4*)(uintptr_t)a0);
+    const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((INFLLM_LDS i16x4*)(uintptr_t)a1);
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  auto kaddr_of = [&](int buf) { return opaque_s(lds_k0 + buf * kTileBytes) + koff0; };
+  auto vaddr_of = [&](int buf) { return opaque_s(lds_v0 + buf * kTileBytes) + voff0; };
+
+  f32x16 oacc[DBLK];
+#pragma unroll
+  for (int db = 0; db < DBLK; ++db)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) oacc[db][j] = 0.f;
+  float m_run = -__builtin_inff(), neg_m = 0.f, l_run = 0.f;
+
+  // Scores in the base-2 domain.  Without a form the scale is part of the exponential's
+  // argument; with one a score becomes its final value first.  c tanh(x / c) = c - 2 c / (1 +
+  // e^{2 x / c}): its error of some 2^-23 c is far below what rounding P to bf16 does.
+  const float log2e = 1.4426950408889634f, c2 = a.sm_scale * log2e;
+  float cap_in = 0.f, cap2 = 0.f;
+  if constexpr (MOD & kCap) {
+    cap_in = 2.f * c2 / a.softcap;
+    cap2 = a.softcap * log2e;
+  }
+  auto capped = [&](float s) {
+    if constexpr (MOD & kCap)
+      return __builtin_fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + fast_exp2(s * cap_in)), cap2);
+    return s * c2;
+  };
+  auto weight = [&](float z) { return MOD ? fast_exp2(z + neg_m) : fast_exp2(__builtin_fmaf(z, c2, neg_m)); };
+  // Key place c of a tile (element e = 16 kb + j of a lane: 32 kb + 8 (j / 4) + j % 4, its
+  // half's 4 gsel aside).
+  auto place_of = [](int e) { return 32 * (e >> 4) + 8 * ((e & 15) >> 2) + (e & 3); };
+  // What a row sees of a tile, a bit for each key of this lane's half from its first on, and
+  // the bias of that key.
+  struct Lims {
+    uint32_t vis[2];
+    float base;
+  };
+  auto lims_of = [&](int t, bool masked) {
+    Lims l{};
+    const int k0 = key_of(t);
+    if (masked) {
+      uint64_t vis = seen_keys(pos, k0, a.window, a.n_init);
+      if (has_bad) {
+        const uint32_t at = lds_rows + 4u * (uint32_t)((t - keys.w0) * keys.tile_groups() + (min(lane, last - k0) >> gshift));
+        vis &= __ballot(*(const INFLLM_LDS uint32_t*)(uintptr_t)at != kNoRow);
+      }
+      vis >>= 4 * gsel;
+      l.vis[0] = (uint32_t)vis;
+      l.vis[1] = (uint32_t)(vis >> 32);
+    }
+    if constexpr (MOD & kSlopes) l.base = slope * (float)(k0 + 4 * gsel - pos);
+    return l;
+  };
+  // Elements [8i, 8i + 8) of a tile's scores: their form, and -inf where the row does not see the key.
+  auto form8 = [&](f32x16 (&s)[2], int i, const Lims& l, bool masked) {
+#pragma unroll
+    for (int e = 8 * i; e < 8 * i + 8; ++e) {
+      const int c = place_of(e);
+      float z = s[e >> 4][e & 15];
+      if constexpr (MOD != 0) z = capped(z);
+      if constexpr (MOD & kSlopes) z += __builtin_fmaf(slope, (float)c, l.base);
+      if (masked) {
+        const uint32_t see = (uint32_t)((int32_t)(l.vis[e >> 4] << (31 - (c & 31))) >> 31);  // all ones or none
+        z = __uint_as_float((__float_as_uint(z) & see) | (0xFF800000u & ~see));
+      }
+      s[e >> 4][e & 15] = z;
+    }
+  };
+  auto tile_max = [&](const f32x16 (&s)[2]) {
+    float mx = -__builtin_inff();
+#pragma unroll
+    for (int e = 0; e < 32; ++e) mx = fmaxf(mx, s[e >> 4][e & 15]);
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+    return MOD ? mx : mx * c2;
+  };
+  // Lazy running maximum, as in the step's attention: a tile's P is formed against the
+  // maximum so far, and only where a row's sum of P passes 2^16 (or it has met no visible
+  // key yet) is the tile's own maximum taken and the row rescaled.
+  constexpr float kLazy = 65536.f;
+  float bound = 0.f;
+  auto set_max = [&](float mx) {
+    m_run = mx;
+    neg_m = mx == -__builtin_inff() ? 0.f : -mx;
+    // (a row that sees none of the part's keys: its P are 0)
+    bound = mx != -__builtin_inff() ? kLazy : (int)opaque_v((uint32_t)pos) < key_of(t_begin) ? 0.f : -1.f;
+  };
+  auto outgrown = [&](float l_tile, const f32x16 (&s)[2]) -> bool {
+    if (__ballot(l_tile > bound) == 0) return false;
+    const float mx = tile_max(s);
+    if (__ballot(bound < 0.f ? mx != -__builtin_inff() : l_tile > bound) == 0) return false;
+    const float m_new = fmaxf(m_run, mx);
+    const float alpha = m_new == -__builtin_inff() ? 1.f : fast_exp2(m_run - m_new);
+    l_run *= alpha;
+#pragma unroll
+    for (int db = 0; db < DBLK; ++db)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) oacc[db][j] *= alpha;
+    set_max(m_new);
+    return true;
+  };
+  // Two weights as a bf16 pair; the row sums add them unrounded.  (Rounded by at most 2^-8
+  // of each: the instruction takes bf16 weights with bf16 values.)
+  auto p_pair = [&](float z0, float z1, float (&acc)[2], bool first) -> uint32_t {
+    const float e0 = weight(z0), e1 = weight(z1);
+    acc[0] = first ? e0 : acc[0] + e0;
+    acc[1] = first ? e1 : acc[1] + e1;
+    bf16x2 pr;
+    pr[0] = (__bf16)e0;
+    pr[1] = (__bf16)e1;
+    return opaque_v(__builtin_bit_cast(uint32_t, pr));
+  };
+  auto half_p = [&](const f32x16& s, u32x4 (&p)[2]) {
+    float ps[2];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i >> 2][i & 3] = p_pair(s[2 * i], s[2 * i + 1], ps, i == 0);
+    return ps[0] + ps[1];
+  };
+  auto as_frag = [](const u32x4& x) { return __builtin_bit_cast(bf16x8, x); };
+
+  // Tiles all of whose keys every row of the workgroup sees: [plain0, plain1).
+  int plain0 = t_begin, plain1 = has_bad ? 0 : min(t_end, (w.past + i0 + 1) / KB - keys.shift);
+  if (a.window > 0) plain0 = max(t_begin, (max(0, w.past + i1 - a.window + 1) + KB - 1) / KB - keys.shift);
+
+  // Step of tile t: QK(t+1) beside the second half of P(t), then PV(t) beside the form, mask
+  // and first half of P of tile t+1.  At its top K(t+1) and V(t) have landed; it requests
+  // K(t+2) and V(t+1) into the buffers that the barrier freed.
+  f32x16 sA[2], sB[2];
+  u32x4 p0[2];
+  float l_pend = 0.f;
+  Places f1, f2;  // of tiles t+1 and t+2
+  auto top = [&](int t) {
+    __builtin_amdgcn_s_setprio(0);
+    publish_barrier<0>();
+    // (the table's readers are past the barrier; it keeps tile t+1, whose mask may ask it)
+    if (t + kAhead >= keys.w0 + keys.window() && t + kAhead < t_end) {
+      keys.fill(sm.rows, t + 1);
+      publish_barrier<0>();
+    }
+    __builtin_amdgcn_s_setprio(1);
+  };
+  auto step = [&](int t, f32x16 (&cur)[2], f32x16 (&nxt)[2], auto next_masked) {
+    constexpr bool MASK = decltype(next_masked)::value;
+    const int bc = (t - t_begin) & 1, bn = bc ^ 1;
+    u32x4 w1[2];
+    float ps1[2];
+    bf16x8 va[DBLK];
+    const uint32_t vaddr = vaddr_of(bc);
+    {
+      const uint32_t ka = kaddr_of(bn);
+      bf16x8 a0[2], a1[2];
+      a0[0] = kfrag_at(ka, 0, 0);
+      a1[0] = kfrag_at(ka, 1, 0);
+      constexpr int EPC = 16 / KSTEPS;
+      static_assert(EPC % 2 == 0 && 2 * NI <= KSTEPS, "pairs, and one load per chunk");
+#pragma unroll
+      for (int s = 0; s < KSTEPS; ++s) {
+        if (s + 1 < KSTEPS) {
+          a0[(s + 1) & 1] = kfrag_at(ka, 0, s + 1);
+          a1[(s + 1) & 1] = kfrag_at(ka, 1, s + 1);
+        } else {
+#pragma unroll
+          for (int db = 0; db < DBLK; ++db) va[db] = vfrag_at(vaddr, db, 0);
+        }
+        if (s == 0) {
+          const f32x16 zero = {};
+          nxt[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0[0], qreg[0], zero, 0, 0, 0);
+          nxt[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1[0], qreg[0], zero, 0, 0, 0);
+        } else {
+          nxt[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a0[s & 1], qreg[s], nxt[0], 0, 0, 0);
+          nxt[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a1[s & 1], qreg[s], nxt[1], 0, 0, 0);
+        }
+        if (s < NI) load_k(bc, f2, s);
+        else if (s < 2 * NI) load_v(bn, f1, s - NI);
+#pragma unroll
+        for (int i = 0; i < EPC; i += 2) {
+          const int x = (EPC * s + i) >> 1;
+          w1[x >> 2][x & 3] = p_pair(cur[1][2 * x], cur[1][2 * x + 1], ps1, x == 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    float l_tile = l_pend + (ps1[0] + ps1[1]);
+    if (outgrown(l_tile, cur)) {
+      l_tile = half_p(cur[0], p0);
+      l_tile += half_p(cur[1], w1);
+    }
+    l_run += l_tile;
+    u32x4 q0[2];
+    float ps0[2];
+    {
+      const Lims l = lims_of(t + 1, MASK);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (j == 1) {
+          f1 = f2;
+          places(t + kAhead, f2);
+        }
+#pragma unroll
+        for (int db = 0; db < DBLK; ++db) {
+          oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[db], as_frag(j < 2 ? p0[j & 1] : w1[j & 1]), oacc[db], 0, 0, 0);
+          if (j + 1 < 4) va[db] = vfrag_at(vaddr, db, j + 1);
+        }
+        form8(nxt, j, l, MASK);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int x = 2 * j + i;
+          q0[x >> 2][x & 3] = p_pair(nxt[0][2 * x], nxt[0][2 * x + 1], ps0, x == 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    p0[0] = q0[0];
+    p0[1] = q0[1];
+    l_pend = ps0[0] + ps0[1];
+  };
+  places(t_begin + 1, f1);
+  places(t_begin + 2, f2);
+#pragma unroll
+  for (int j = 0; j < NI; ++j) load_k(1, f1, j);
+  // K(t0) and V(t0) have landed, K(t0 + 1) is in flight
+  publish_barrier<NI>();
+  if (!active) {
+    int t = t_begin;
+    for (; t + 1 < t_end; ++t) {
+      top(t);
+      const int bc = (t - t_begin) & 1;
+#pragma unroll
+      for (int j = 0; j < NI; ++j) load_k(bc, f2, j);
+#pragma unroll
+      for (int j = 0; j < NI; ++j) load_v(bc ^ 1, f1, j);
+      f1 = f2;
+      places(t + kAhead, f2);
+    }
+    top(t);
+  } else {
+    {
+      const uint32_t ka = kaddr_of(0);
+#pragma unroll
+      for (int s = 0; s < KSTEPS; ++s) {
+        const f32x16 zero = {};
+        sA[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kfrag_at(ka, 0, s), qreg[s], s == 0 ? zero : sA[0], 0, 0, 0);
+        sA[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kfrag_at(ka, 1, s), qreg[s], s == 0 ? zero : sA[1], 0, 0, 0);
+      }
+    }
+    {
+      const bool mk = t_begin < plain0 || t_begin >= plain1;
+      const Lims l = lims_of(t_begin, mk);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) form8(sA, i, l, mk);
+    }
+    set_max(tile_max(sA));  // the first tile's maximum
+    l_pend = half_p(sA[0], p0);
+    int t = t_begin;
+    // pairs whose next tiles need a mask, plain pairs, pairs that need one again
+    for (; t + 2 < t_end && t + 1 < plain0; t += 2) {
+      top(t);
+      step(t, sA, sB, std::true_type{});
+      top(t + 1);
+      step(t + 1, sB, sA, std::true_type{});
+    }
+    for (; t + 2 < plain1; t += 2) {
+      top(t);
+      step(t, sA, sB, std::false_type{});
+      top(t + 1);
+      step(t + 1, sB, sA, std::false_type{});
+    }
+    for (; t + 2 < t_end; t += 2) {
+      top(t);
+      step(t, sA, sB, std::true_type{});
+      top(t + 1);
+      step(t + 1, sB, sA, std::true_type{});
+    }
+    if (t + 1 < t_end) {
+      top(t);
+      step(t, sA, sB, std::true_type{});
+      sA[0] = sB[0];
+      sA[1] = sB[1];
+      ++t;
+    }
+    top(t);
+    // the last tile's P and PV
+    u32x4 w1[2];
+    float l_tile = l_pend + half_p(sA[1], w1);
+    if (outgrown(l_tile, sA)) {
+      l_tile = half_p(sA[0], p0);
+      l_tile += half_p(sA[1], w1);
+    }
+    l_run += l_tile;
+    const uint32_t vaddr = vaddr_of((t - t_begin) & 1);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int db = 0; db < DBLK; ++db)
+        oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vfrag_at(vaddr, db, j), as_frag(j < 2 ? p0[j & 1] : w1[j & 1]), oacc[db], 0, 0, 0);
+  }
+  publish_barrier<0>();  // no load in flight, every wave done with the tile buffers
+  __builtin_amdgcn_s_setprio(0);
+
+  // Epilogue: the row's sum, its rows staged through LDS so that a store moves 16 bytes of
+  // a row and a wave's store whole rows.
+  // What it needs of the arguments and the row is formed again rather than held through the
+  // loop.
+  LateArgs& late = late_args();
+  const FastDiv d_group{late.d_group.d, late.d_group.mul};
+  const int lane_e = (int)opaque_v((uint32_t)lane), n_e = lane_e & 31, row_e = row0 + n_e;
+  const bool row_ok = row_e < R;
+  const float l_tot = l_run + __shfl_xor(l_run, 32);
+  float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+  float lse_v = m_run == -__builtin_inff() || l_tot <= 0.f ? -__builtin_inff() : (m_run + __log2f(l_tot)) * 0.6931471805599453f;
+  if (l_tot != l_tot) {  // a NaN among the row's scores is the row's, through the merge as well
+    inv = l_tot;
+    lse_v = one_part ? l_tot : __builtin_inff();
+  }
+  float sc = inv;
+  int ex = 0;
+  if (!one_part) {
+    float amax = 0.f;
+#pragma unroll
+    for (int db = 0; db < DBLK; ++db)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) amax = fmaxf(amax, fabsf(oacc[db][j]));
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(amax), __float_as_uint(amax), false, false);
+    ex = partial_row_exponent(fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * inv);
+    sc = inv * exp2_int(-ex);
+  }
+  constexpr int kStageRow = D * 2 + 16;  // padded: the 32 rows of a wave spread over the LDS banks
+  static_assert(4 * 32 * kStageRow <= (int)(sizeof(sm.k) + sizeof(sm.v)), "staging fits the tile buffers");
+  INFLLM_LDS char* stage = (INFLLM_LDS char*)(INFLLM_LDS bf16_t*)sm.k[0] + wave * 32 * kStageRow;
+#pragma unroll
+  for (int db = 0; db < DBLK; ++db) {
+#pragma unroll
+    for (int jq = 0; jq < 4; ++jq) {
+      const float o0 = oacc[db][4 * jq] * sc, o1 = oacc[db][4 * jq + 1] * sc;
+      const float o2 = oacc[db][4 * jq + 2] * sc, o3 = oacc[db][4 * jq + 3] * sc;
+      u32x2 x;
+      if (one_part) {
+        x[0] = (uint32_t)f32_to_bf16(o0) | ((uint32_t)f32_to_bf16(o1) << 16);
+        x[1] = (uint32_t)f32_to_bf16(o2) | ((uint32_t)f32_to_bf16(o3) << 16);
+      } else {
+        x[0] = pack_f16x2(o0, o1);
+        x[1] = pack_f16x2(o2, o3);
+      }
+      *(INFLLM_LDS u32x2*)(stage + n_e * kStageRow + (32 * db + 8 * jq + 4 * (lane_e >> 5)) * 2) = x;
+    }
+  }
+  auto lds_order = []() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+  };
+  // Values that are not finite must not reach rows that do not see their key: in a masked
+  // tile such a value meets P = 0 and leaves a NaN.  A row that came out so is formed again
+  // by the wave from the keys it sees, 64 at a time, against its maximum.
+  {
+    float z4[4] = {};
+#pragma unroll
+    for (int db = 0; db < DBLK; ++db)
+#pragma unroll
+      for (int j = 0; j < 16; ++j) z4[j & 3] = __builtin_fmaf(oacc[db][j], 0.f, z4[j & 3]);
+    const float z = (z4[0] + z4[1]) + (z4[2] + z4[3]);
+    const uint64_t odd = __ballot(row_ok && !(z == 0.f) && l_tot == l_tot);
+    uint32_t rows = (uint32_t)odd | (uint32_t)(odd >> 32);
+    if (__builtin_expect(rows != 0, 0)) {
+      lds_order();
+      constexpr int DPL = D / 64;
+      for (; rows != 0; rows &= rows - 1) {
+        const int r = __builtin_ctz(rows);
+        const int i = div_by(row0 + r, d_group), h = g * G + row0 + r - i * G, p_r = w.past + i;
+        const float nm = __shfl(neg_m, r), inv_r = __shfl(inv, r), slope_r = __shfl(slope, r);
+        float acc[DPL];
+        form_row<bf16_t, D>(keys, kbase, vbase, (const bf16_t*)late.q + (int64_t)(w.start + i) * late.q_tok + (int64_t)h * late.q_head,
+                            p_r, a.window, a.n_init,
+                            [&](float s, int key) { return fast_exp2(capped(s) + slope_r * (float)(key - p_r) + nm); }, acc);
+        float amax = 0.f;  // (of the finite ones, which keep their precision)
+#pragma unroll
+        for (int e = 0; e < DPL; ++e) {
+          acc[e] *= inv_r;
+          const float x = fabsf(acc[e]);
+          amax = x < __builtin_inff() ? fmaxf(amax, x) : amax;
+        }
+        const int ex_r = one_part ? 0 : partial_row_exponent(wave_max(amax));
+        if (n_e == r) ex = ex_r;
+        const float back = exp2_int(-ex_r);
+#pragma unroll
+        for (int e = 0; e < DPL; ++e) {
+          const uint32_t x = one_part ? f32_to_bf16(acc[e]) : pack_f16x2(acc[e] * back, 0.f) & 0xFFFFu;
+          *(INFLLM_LDS uint16_t*)(stage + r * kStageRow + 2 * (DPL * lane + e)) = (uint16_t)x;
+        }
+      }
+    }
+  }
+  const int64_t prow0 = ((int64_t)blockIdx.x) * late.item_rows;  // of the item's partial rows
+  if (row_ok && lane_e < 32) {
+    if (!one_part) {
+      late.part_lse[prow0 + row_e - tile0] = lse_v;
+      late.part_exp[prow0 + row_e - tile0] = ex;
+    } else if (late.lse != nullptr) {
+      const int i = div_by(row_e, d_group), h = g * G + row_e - i * G;
+      late.lse[h * late.lse_stride + w.start + i] = lse_v;
+    }
+  }
+  lds_order();
+  {
+    constexpr int NP = 32 * CH / 64;  // pieces of a lane
+    const int r0 = lane_e / CH, ch = lane_e % CH;
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+      if (row0 + RPI * k >= R) break;  // (uniform)
+      const int r = row0 + RPI * k + r0;
+      if (r >= R) continue;
+      const u32x4 x = *(const INFLLM_LDS u32x4*)(stage + (RPI * k + r0) * kStageRow + ch * 16);
+      if (one_part) {
+        const int i = div_by(r, d_group), h = g * G + r - i * G;
+        *(u32x4*)((bf16_t*)late.out + (int64_t)(w.start + i) * late.out_tok + (int64_t)h * late.out_head + 8 * ch) = x;
+      } else {
+        *(u32x4*)((char*)late.part_o + (prow0 + r - tile0) * (D * 2) + 16 * ch) = x;
+      }
+    }
+  }
+}
+
+// Float32: NW waves of 32 rows on the float32 matrix cores (v_mfma_f32_32x32x2_f32), key
+// tiles of 32 through two LDS buffers, one tile ahead.  S^T = K Q^T takes the dims in the
+// order that lets one 16-byte read feed four products; sums of 16 products are joined by
+// additions.  O^T += V^T P^T with P^T as it stands; output block db holds dims DBLK*m + db,
+// so that one read feeds all blocks.  Rows of an LDS tile are XOR-swizzled by piece, which
+// leaves both reads without conflicts.
+constexpr int kF32Tile = 32;
+
+// e^x for x <= 0 (and NaN): 2^t, t = x log2(e) rounded, which moves e^x by at most 2^-25 of
+// the row's largest weight.
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269502f); }
+
+template <int D, int NW, int MOD>
+__global__ void __launch_bounds__(64 * NW, D == 64 && NW > 1 ? 2 : 1) paged_f32_kernel(PagedArgs a) {
+  constexpr int KT = kF32Tile, RW = 32 * NW, QL = D / 2, DBLK = D / 32;
+  constexpr int GPR = D / 4, RPI = 64 / GPR, NI = KT / (RPI * NW);
+  constexpr uint32_t kTileBytes = KT * D * 4;
+  __shared__ __attribute__((aligned(256))) float ks[2][KT * D];
+  __shared__ __attribute__((aligned(256))) float vs[2][KT * D];
+  __shared__ uint32_t rows[kTable];
+  __shared__ int wave_bad[NW];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 31, gsel = lane >> 5;
+  const int G = (int)a.d_group.d;
+  const int item = div_by(blockIdx.x, a.d_kv), g = (int)blockIdx.x - item * (int)a.d_kv.d;
+  const PagedWork w = paged_work(a, item);
+  const int R = G * w.len, tile0 = w.rt * RW;
+  const int i0 = div_by(tile0, a.d_group), i1 = div_by(min(R, tile0 + RW) - 1, a.d_group);
+  const PagedRange range = paged_range(a, w.past, i0, i1);
+  const int t_begin = w.part * a.part_tiles, t_end = min(t_begin + a.part_tiles, range.n);
+  if (t_begin >= t_end) return;
+  const bool one_part = range.n <= a.part_tiles;
+  const int last = w.past + w.len - 1;
+  KeyTiles<KT, 64 * NW> keys{range.sink, range.low - range.sink, t_begin, t_end, last, w.s, (a.seqs.page_size & 7) == 0 ? 3 : 0, t_begin};
+
+  const int row0 = tile0 + wave * 32, row = row0 + n;
+  const bool active = row0 < R, row_ok = row < R;
+  const int row_c = min(row, R - 1);
+  const int qi = div_by(row_c, a.d_group), qh = g * G + row_c - qi * G;
+  const int pos = w.past + qi;
+  const char* kbase = (const char*)a.k + g * a.head_stride * 4;
+  const char* vbase = (const char*)a.v + g * a.head_stride * 4;
+  const float* qp = (const float*)a.q + (int64_t)(w.start + qi) * a.q_tok + (int64_t)qh * a.q_head;
+  float qv[QL];
+#pragma unroll
+  for (int i = 0; i < QL / 4; ++i) {
+    const f32x4 x = *(const f32x4*)(qp + 8 * i + 4 * gsel);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) qv[4 * i + e] = x[e];
+  }
+  float slope = 0.f;
+  if constexpr (MOD & kSlopes) slope = a.slopes[qh];
+
+  {
+    const bool any = __ballot(keys.fill_first(rows)) != 0;
+    if (lane == 0) wave_bad[wave] = any;
+  }
+  lds_barrier();
+  bool has_bad = false;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) has_bad |= wave_bad[i] != 0;
+
+  const uint32_t lds_k = (uint32_t)(uintptr_t)(INFLLM_LDS float*)ks[0] + NI * wave * 1024;
+  const uint32_t lds_v = (uint32_t)(uintptr_t)(INFLLM_LDS float*)vs[0] + NI * wave * 1024;
+  const uint32_t gmask = (1u << keys.gshift) - 1u;
+  auto load_tile = [&](int t) {
+    const uint32_t buf = ((t - t_begin) & 1) * kTileBytes;
+    const int in_tile = min(KT - 1, last - keys.key_of(t));
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const int lr = (NI * wave + j) * RPI + lane / GPR;
+      const uint32_t r = (uint32_t)min(lr, in_tile);
+      uint32_t p = rows[(t - keys.w0) * keys.tile_groups() + (r >> keys.gshift)];
+      p = p == kNoRow ? 0u : p + (r & gmask) * a.token16;  // (a row that is not there: page 0's, masked)
+      const uint64_t off = ((uint64_t)p + (uint32_t)((lane % GPR) ^ (lr & 15))) * 16;
+      lds_load_lane(lds_k + buf + j * 1024, kbase + off);
+      lds_load_lane(lds_v + buf + j * 1024, vbase + off);
+    }
+  };
+
+  f32x16 o[DBLK];
+#pragma unroll
+  for (int db = 0; db < DBLK; ++db)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) o[db][j] = 0.f;
+  float m = -__builtin_inff(), l = 0.f;
+  auto score_of = [&](float s, int distance) {  // distance: of the key from the query, <= 0
+    float z = s * a.sm_scale;
+    if constexpr (MOD & kCap) z = a.softcap * tanhf(z / a.softcap);
+    if constexpr (MOD & kSlopes) z = __builtin_fmaf(slope, (float)distance, z);
+    return z;
+  };
+  // tiles all of whose keys every row of the wave sees: [plain0, plain1)
+  const int w0 = div_by(min(row0, R - 1), a.d_group), w1 = div_by(min(row0 + 31, R - 1), a.d_group);
+  int plain0 = t_begin;
+  const int plain1 = has_bad ? 0 : min(t_end, (w.past + w0 + 1) / KT - keys.shift);
+  if (a.window > 0) plain0 = (max(0, w.past + w1 - a.window + 1) + KT - 1) / KT - keys.shift;
+
+  load_tile(t_begin);
+  for (int t = t_begin; t < t_end; ++t) {
+    publish_barrier<0>();  // tile t has landed; the other buffer is free
+    asm volatile("" ::: "memory");
+    if (t + 1 < t_end) {
+      if (t + 1 >= keys.w0 + keys.window()) {
+        keys.fill(rows, t);  // (tile t's mask may ask it)
+        lds_barrier();
+      }
+      load_tile(t + 1);
+    }
+    if (!active) continue;
+    const float *kt = ks[(t - t_begin) & 1], *vt = vs[(t - t_begin) & 1];
+    f32x16 s;
+#pragma unroll
+    for (int i0 = 0; i0 < QL / 4; i0 += 4) {
+      f32x16 s0 = {}, s1 = {};
+#pragma unroll
+      for (int i = i0; i < i0 + 4; ++i) {
+        const f32x4 kf = *(const f32x4*)(kt + n * D + 4 * ((2 * i + gsel) ^ (n & 15)));
+        s0 = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[0], qv[4 * i], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[1], qv[4 * i + 1], s1, 0, 0, 0);
+        s0 = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[2], qv[4 * i + 2], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[3], qv[4 * i + 3], s1, 0, 0, 0);
+      }
+      s = i0 == 0 ? s0 + s1 : s + (s0 + s1);
+    }
+    const bool plain = t >= plain0 && t < plain1;
+    const int k0 = keys.key_of(t);
+    // (without a form a plain tile's scale is part of the exponential's argument)
+    const float in_exp = MOD == 0 && plain ? a.sm_scale : 1.f;
+    if (MOD != 0 || !plain) {
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s[j] = score_of(s[j], k0 + 8 * (j >> 2) + 4 * gsel + (j & 3) - pos);
+    }
+    if (!plain) {
+      uint64_t vis = seen_keys(pos, k0, a.window, a.n_init);
+      if (has_bad) vis &= __ballot(rows[(t - keys.w0) * keys.tile_groups() + (min(n, last - k0) >> keys.gshift)] != kNoRow);
+      const uint32_t see = (uint32_t)vis >> (4 * gsel);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) s[j] = ((see >> (8 * (j >> 2) + (j & 3))) & 1u) != 0 ? s[j] : -__builtin_inff();
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int j = 1; j < 16; ++j) mx = fmaxf(mx, s[j]);
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * in_exp;
+    if (__ballot(mx > m)) {
+      const float m_new = fmaxf(m, mx), corr = m_new == -__builtin_inff() ? 1.f : expf(m - m_new);
+      m = m_new;
+      l *= corr;
+#pragma unroll
+      for (int db = 0; db < DBLK; ++db)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[db][j] *= corr;
+    }
+    const float base = m == -__builtin_inff() ? 0.f : m;
+    float ls[2] = {0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      s[j] = exp_of(__builtin_fmaf(s[j], in_exp, -base));
+      ls[j & 1] += s[j];
+    }
+    l += ls[0] + ls[1];
+    typedef float vfrag_t __attribute__((ext_vector_type(DBLK)));
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const int r = 8 * (j >> 2) + 4 * gsel + (j & 3), d0 = DBLK * n;
+      const vfrag_t vf = *(const vfrag_t*)(vt + r * D + 4 * ((d0 >> 2) ^ (r & 15)) + (d0 & 3));
+#pragma unroll
+      for (int db = 0; db < DBLK; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[db], s[j], o[db], 0, 0, 0);
+    }
+  }
+  if (!active) return;
+
+  const auto lw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  const float l_tot = __uint_as_float(lw[0]) + __uint_as_float(lw[1]);
+  float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+  float lse_v = l_tot > 0.f ? m + logf(l_tot) : -__builtin_inff();
+  if (l_tot != l_tot) {  // a NaN among the row's scores is the row's, through the merge as well
+    inv = l_tot;
+    lse_v = one_part ? l_tot : __builtin_inff();
+  }
+  const int64_t prow = (int64_t)blockIdx.x * a.item_rows - tile0;  // plus a row: its partial row
+  typedef float orow_t __attribute__((ext_vector_type(DBLK)));
+  float z4[4] = {};
+#pragma unroll
+  for (int db = 0; db < DBLK; ++db)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) z4[j & 3] = __builtin_fmaf(o[db][j], 0.f, z4[j & 3]);
+  const bool odd = row_ok && !((z4[0] + z4[1]) + (z4[2] + z4[3]) == 0.f) && l_tot == l_tot;
+  if (row_ok) {
+    float* op = one_part ? (float*)a.out + (int64_t)(w.start + qi) * a.out_tok + (int64_t)qh * a.out_head
+                         : (float*)a.part_o + (prow + row) * D;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      orow_t x;
+#pragma unroll
+      for (int db = 0; db < DBLK; ++db) x[db] = o[db][j] * inv;
+      if (!odd) *(orow_t*)(op + DBLK * (8 * (j >> 2) + 4 * gsel + (j & 3))) = x;
+    }
+    if (gsel == 0) {
+      if (!one_part) a.part_lse[prow + row] = lse_v;
+      else if (a.lse != nullptr) a.lse[qh * a.lse_stride + w.start + qi] = lse_v;
+    }
+  }
+  // Rows that a masked value which is not finite has reached (0 times it) are formed again
+  // from the keys that they see.
+  const uint64_t odds = __ballot(odd);
+  for (uint32_t left = (uint32_t)odds | (uint32_t)(odds >> 32); left != 0; left &= left - 1) {
+    const int r = __builtin_ctz(left);
+    const int i = div_by(row0 + r, a.d_group), h = g * G + row0 + r - i * G, p_r = w.past + i;
+    const float m_r = __shfl(m, r), base_r = m_r == -__builtin_inff() ? 0.f : m_r, inv_r = __shfl(inv, r);
+    const float slope_r = __shfl(slope, r);
+    float acc[D / 64];
+    form_row<float, D>(keys, kbase, vbase, (const float*)a.q + (int64_t)(w.start + i) * a.q_tok + (int64_t)h * a.q_head, p_r, a.window, a.n_init,
+                       [&](float x, int key) {
+                         float z = x * a.sm_scale;
+                         if constexpr (MOD & kCap) z = a.softcap * tanhf(z / a.softcap);
+                         return exp_of(__builtin_fmaf(slope_r, (float)(key - p_r), z) - base_r);
+                       }, acc);
+    float* op = one_part ? (float*)a.out + (int64_t)(w.start + i) * a.out_tok + (int64_t)h * a.out_head
+                         : (float*)a.part_o + (prow + row0 + r) * D;
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) op[D / 64 * lane + e] = acc[e] * inv_r;
+  }
+}
+
+template <int D, int MOD>
+void launch_form(const PagedArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)(a.items * a.n_kv_heads)), block(2 << a.rows_log2);
+  if (a.bf16) hipLaunchKernelGGL((paged_mfma_kernel<D, MOD>), grid, block, 0, s, a);
+  else if (a.rows_log2 == 7) hipLaunchKernelGGL((paged_f32_kernel<D, 4, MOD>), grid, block, 0, s, a);
+  else if (a.rows_log2 == 6) hipLaunchKernelGGL((paged_f32_kernel<D, 2, MOD>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((paged_f32_kernel<D, 1, MOD>), grid, block, 0, s, a);
+}
+template <int D>
+void launch_d(const PagedArgs& a, hipStream_t s) {
+  const int mod = (a.softcap > 0.f ? kCap : 0) | (a.slopes != nullptr ? kSlopes : 0);
+  if (mod == 0) launch_form<D, 0>(a, s);
+  else if (mod == kCap) launch_form<D, kCap>(a, s);
+  else if (mod == kSlopes) launch_form<D, kSlopes>(a, s);
+  else launch_form<D, kCap | kSlopes>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_paged(const PagedArgs& a, hipStream_t s) {
-  if (a.bf16) launch_t<bf16_t>(a, s);
-  else launch_t<float>(a, s);
+  if (a.head_dim == 128) launch_d<128>(a, s);
+  else launch_d<64>(a, s);
   return hipGetLastError();
 }
 
