@@ -574,7 +574,7 @@ size_t infllm_paged_workspace_bytes(const infllm_params* p, const infllm_pages* 
  *     optional [Hq][total] float32, total the sum of seq_lens.
  * A query that sees nothing (its pages not followed) gets zeros and lse -inf.
  * E_RANGE as in infllm_paged_append.  E_UNSUPPORTED where the rows of k span more than
- * 64 GiB, or the work exceeds 32-bit numbers (total * G past 2^31 - 1, positions past
+ * 64 GiB or a page's tokens lie 256 MiB apart, or the work exceeds 32-bit numbers (total * G past 2^31 - 1, positions past
  * 2^31 - 256, or some 2^32 / 256 workgroups). */
 infllm_status infllm_paged_attend(const infllm_params* p, const infllm_pages* pages, int32_t n_seqs,
                                   const int32_t* seq_lens, const int64_t* past_lens, const int32_t* page_table,

@@ -124,15 +124,16 @@ void set_rotary(const infllm_params* p, const infllm_rotary* r, RotateArgs* a) {
 bool rotate_fits(int64_t tokens, int64_t rows) { return (__int128)tokens * rows < INT32_MAX / 64; }
 
 // Microseconds of a workgroup of the attention, for each tile of keys and beside them: with
-// the whole chip at work, and of one that runs longer than the others.
+// the whole chip at work, and of one that runs longer than the others.  Row tiles of few
+// rows read their keys at the memory's rate, of many they share them in the cache.
 struct ItemCost {
   float tile, item, lone_tile, lone_item;
 };
 ItemCost item_cost(const PagedArgs& a, bool thin) {
   const bool wide = a.head_dim == 128;
   if (a.bf16) {
-    if (thin) return wide ? ItemCost{1.2f, 6.f, 0.8f, 6.f} : ItemCost{0.8f, 6.f, 0.6f, 6.f};
-    return wide ? ItemCost{1.76f, 9.f, 0.95f, 6.5f} : ItemCost{0.96f, 8.5f, 0.72f, 5.5f};
+    if (thin) return wide ? ItemCost{2.9f, 8.f, 0.75f, 7.f} : ItemCost{1.5f, 8.f, 0.6f, 7.f};
+    return wide ? ItemCost{1.9f, 9.f, 1.1f, 8.f} : ItemCost{1.0f, 8.5f, 0.75f, 7.f};
   }
   return wide ? ItemCost{6.6f, 12.f, 6.6f, 12.f} : ItemCost{6.2f, 10.f, 4.2f, 8.f};
 }
@@ -145,80 +146,108 @@ int resident_wgs(const PagedArgs& a) {
 }
 constexpr float kMergeCost = 6.f;            // microseconds of a merge's launch
 constexpr float kPartialByteCost = 2.5e-7f;  // of a byte of a partial row, written and read
-constexpr float kReadRate = 5.4e6f;          // bytes of keys and values per microsecond
-constexpr int kMostParts = 128;              // of a row tile
+constexpr int kMostParts = 256;              // of a row tile
 
-// Key parts and item numbers of the sequences in a->seqs; false where an item or its
-// partial rows have no number.  A launch lasts as long as its work shared over the
-// workgroups that run at a time, as its keys' bytes, or as a part, and where the parts do
-// not all start at once about half a part more; a split costs the merge.
-bool plan(PagedArgs* a) {
-  const int n = a->seqs.n_seqs, G = (int)a->d_group.d, Hkv = a->n_kv_heads;
-  auto len = [&](int i) { return a->seqs.start[i + 1] - a->seqs.start[i]; };
-  int most = 0;
+// The sequences of the next launch, from lens[*i] on (first token *at): their parts and item
+// numbers.  False where none is left, or (*ok) an item or its partial rows have no number.
+// A row tile of n key tiles has ceil(n / T) parts of one length.  A launch lasts as long as
+// its work shared over the workgroups that run at a time, or as the rounds of the items that
+// are about as long as the longest (a round that does not fill the chip runs faster), and a
+// split costs the merge.
+bool plan(const infllm_params* p, int32_t n_seqs, const int32_t* lens, const int64_t* pasts, int* i, int64_t* at, PagedArgs* a,
+          bool* ok) {
+  const int G = (int)a->d_group.d, Hkv = a->n_kv_heads;
+  int n = 0;
+  int32_t start[kMaxAttend], len[kMaxAttend], past[kMaxAttend];
+  uint8_t row[kMaxAttend];
+  *ok = true;
+  a->table += *i * a->table_stride;
   int64_t most_rows = 0;
-  for (int i = 0; i < n; ++i) most_rows = std::max(most_rows, (int64_t)len(i) * G);
+  const int from = *i;
+  for (; *i < n_seqs && *i - from < kMaxAttend; *at += lens[(*i)++]) {
+    if (lens[*i] == 0) continue;
+    start[n] = (int32_t)*at;
+    len[n] = lens[*i];
+    past[n] = (int32_t)pasts[*i];
+    row[n] = (uint8_t)(*i - from);
+    most_rows = std::max(most_rows, (int64_t)lens[*i] * G);
+    ++n;
+  }
+  a->n_seqs = n;
+  a->items = 0;
+  if (n == 0) return *i < n_seqs;
   a->key_tile = a->bf16 ? 64 : 32;
   a->rows_log2 = a->bf16 || most_rows > 64 ? 7 : most_rows > 32 ? 6 : 5;
   const int rows_wg = 1 << a->rows_log2;
   a->tile_queries = (rows_wg - 1) / G + 2;
   a->item_rows = (int)std::min<int64_t>(rows_wg, (most_rows + 7) / 8 * 8);
-  // by sequence: row tiles, most key tiles of one, key tiles of all of them
-  int tiles[kMaxPaged], keys[kMaxPaged];
-  float work = 0.f, bytes = 0.f;
-  int64_t row_tiles = 0;
-  const float tile_bytes = (float)(a->key_tile * a->head_dim * (a->bf16 ? 4 : 8));
-  for (int i = 0; i < n; ++i) {
-    tiles[i] = keys[i] = 0;
-    if (len(i) == 0) continue;
-    tiles[i] = paged_row_tiles(*a, G, len(i));
-    keys[i] = paged_most_tiles(*a, a->seqs.past[i], len(i));
-    const int first = paged_range(*a, a->seqs.past[i], 0, std::min(len(i), a->tile_queries) - 1).n;
-    const float tile = item_cost(*a, (int64_t)len(i) * G <= 32).tile;
-    work += tile * (float)tiles[i] * 0.5f * (float)(first + keys[i]);
-    bytes += tile_bytes * (float)keys[i];
-    row_tiles += tiles[i];
-    most = std::max(most, keys[i]);
+  // by sequence: row tiles, and most key tiles of one
+  int tiles[kMaxAttend], keys[kMaxAttend], most = 0;
+  const int slots = resident_wgs(*a);
+  float work = 0.f, lone = 0.f;
+  for (int j = 0; j < n; ++j) {
+    tiles[j] = paged_row_tiles(*a, G, len[j]);
+    keys[j] = paged_most_tiles(*a, past[j], len[j]);
+    const int first = paged_range(*a, past[j], 0, std::min(len[j], a->tile_queries) - 1).n;
+    const ItemCost c = item_cost(*a, (int64_t)len[j] * G <= 32);
+    work += c.tile * (float)tiles[j] * 0.5f * (float)(first + keys[j]);
+    lone = std::max(lone, c.lone_tile);
+    most = std::max(most, keys[j]);
   }
   const ItemCost cost = item_cost(*a, most_rows <= 32);
-  const float share = (float)Hkv / (float)resident_wgs(*a);
   float best = -1.f;
-  for (int c = 1; c <= kMostParts; c += std::max(1, c / 4)) {
+  int best_T = most;
+  for (int c = 1; c <= kMostParts; c += std::max(1, c / 5)) {
     const int T = (most + c - 1) / c;
     if (c > 1 && T < 2) break;
-    int64_t items = 0;
-    for (int i = 0; i < n; ++i)
-      if (tiles[i] > 0) items += (int64_t)tiles[i] * ((keys[i] + T - 1) / T);
-    const float even = std::max(share * (work + (float)items * cost.item), (float)Hkv * bytes / kReadRate);
-    const float part = (float)T * cost.lone_tile + cost.lone_item;
-    float t = std::max(even, part);
-    if (items > row_tiles) {
-      if ((float)items * share > 1.f) t = std::max(even, part + 0.5f * (float)T * cost.tile + cost.item);
-      t += kMergeCost + (float)items * (float)(Hkv * a->item_rows) * (float)(a->head_dim * 2 + 8) * kPartialByteCost;
+    int64_t items = 0, row_tiles = 0, longs = 0;
+    for (int j = 0; j < n; ++j) {
+      const int parts = (keys[j] + T - 1) / T;
+      items += (int64_t)tiles[j] * parts;
+      row_tiles += tiles[j];
+      if ((keys[j] + parts - 1) / parts * 4 > 3 * T) longs += (int64_t)tiles[j] * parts;
     }
+    const float even = (float)Hkv / (float)slots * (work + (float)items * cost.item);
+    const int64_t rounds = longs * Hkv / slots, rest = longs * Hkv % slots;
+    float t = (float)rounds * ((float)T * cost.tile + cost.item);
+    if (rest > 0) t += (float)T * std::max(lone, cost.tile * (float)rest / (float)slots) + cost.lone_item;
+    const float part = t;
+    t = std::max(t, even);
+    if (items > row_tiles)
+      t += kMergeCost + (float)items * (float)(Hkv * a->item_rows) * (float)(a->head_dim * 2 + 8) * kPartialByteCost;
     if (best < 0.f || t < best) {
       best = t;
-      a->part_tiles = T;
+      best_T = T;
     }
-    if (even >= part) break;  // (more parts add nothing but workgroups)
+    if (even >= 1.5f * part) break;  // (more parts add nothing but workgroups)
   }
-  a->d_part = fast_div(a->part_tiles);
+  uint8_t order[kMaxAttend];
+  int length[kMaxAttend];  // of a sequence's parts
+  for (int j = 0; j < n; ++j) {
+    const int parts = std::min(kMostParts, (keys[j] + best_T - 1) / best_T);
+    length[j] = (keys[j] + parts - 1) / parts;
+    order[j] = (uint8_t)j;
+  }
+  std::sort(order, order + n, [&](int x, int y) { return length[x] != length[y] ? length[x] > length[y] : x < y; });
   int64_t items = 0;
-  for (int i = 0; i < n; ++i) {
-    a->first[i] = (int32_t)items;
-    if (tiles[i] > 0) items += (int64_t)tiles[i] * ((keys[i] + a->part_tiles - 1) / a->part_tiles);
-    if (items * Hkv * 128 > INT32_MAX) return false;
+  for (int x = 0; x < n; ++x) {
+    const int j = order[x], parts = (keys[j] + length[j] - 1) / length[j];
+    a->first[x] = (int32_t)items;
+    a->start[x] = start[j];
+    a->len[x] = len[j];
+    a->past[x] = past[j];
+    a->parts[x] = (uint8_t)(parts - 1);
+    a->table_row[x] = row[j];
+    items += (int64_t)tiles[j] * parts;
+    if (items * Hkv * 128 > INT32_MAX) *ok = false;
   }
-  a->items = (int)items;
+  a->items = *ok ? (int)items : 0;
   return true;
 }
 // Partial rows of a launch (0 where no row tile has several parts).
 int64_t partial_rows(const PagedArgs& a) {
-  for (int i = 0; i < a.seqs.n_seqs; ++i) {
-    const int len = a.seqs.start[i + 1] - a.seqs.start[i];
-    if (len > 0 && paged_most_tiles(a, a.seqs.past[i], len) > a.part_tiles)
-      return (int64_t)a.items * a.n_kv_heads * a.item_rows;
-  }
+  for (int i = 0; i < a.n_seqs; ++i)
+    if (a.parts[i] > 0) return (int64_t)a.items * a.n_kv_heads * a.item_rows;
   return 0;
 }
 
@@ -245,6 +274,9 @@ void set_shape(const infllm_params* p, const infllm_pages* pages, const infllm_s
   a->head_stride = pages->head_stride;
   a->page16 = (uint32_t)(pages->page_stride * esize(p) / 16);
   a->token16 = (uint32_t)(pages->token_stride * esize(p) / 16);
+  a->n_pages = pages->n_pages;
+  a->page_size = pages->page_size;
+  a->d_page = fast_div(pages->page_size);
 }
 
 infllm_status check_score(const infllm_score_form* s) {
@@ -406,12 +438,9 @@ size_t infllm_paged_workspace_bytes(const infllm_params* p, const infllm_pages* 
   set_shape(p, pages, score, &a);
   size_t most = 0;
   int64_t at = 0;
-  for (int i = 0; i < n_seqs; i += kMaxPaged) {
-    const int64_t from = at;
-    fill_seqs(pages, n_seqs, seq_lens, past_lens, nullptr, 0, i, at, &a.seqs);
-    at = a.seqs.start[a.seqs.n_seqs];
-    if (at == from) continue;
-    if (!plan(&a)) return 0;
+  bool ok;
+  for (int i = 0; plan(p, n_seqs, seq_lens, past_lens, &i, &at, &a, &ok);) {
+    if (!ok) return 0;
     most = std::max(most, (size_t)partial_rows(a) * part_row_bytes(p));
   }
   return (most + 255) & ~(size_t)255;
@@ -442,6 +471,7 @@ infllm_status infllm_paged_attend(const infllm_params* p, const infllm_pages* pa
   // (keys are addressed by 16-byte pieces in 32 bits; the last number stands for no row)
   const __int128 span = (__int128)(pages->n_pages - 1) * pages->page_stride + (__int128)(pages->page_size - 1) * pages->token_stride;
   if (span * esize(p) / 16 >= 0xFFFFFFFFll - p->head_dim) return INFLLM_E_UNSUPPORTED;
+  if (pages->page_size > 1 && pages->token_stride * esize(p) / 16 >= 1 << 24) return INFLLM_E_UNSUPPORTED;
   PagedArgs a;
   set_shape(p, pages, score, &a);
   a.q = q;
@@ -454,17 +484,21 @@ infllm_status infllm_paged_attend(const infllm_params* p, const infllm_pages* pa
   a.out_tok = out_token_stride;
   a.out_head = out_head_stride;
   a.lse_stride = total;
-  // every launch is planned before the first is enqueued (a call's only one is kept)
-  const bool single = n_seqs <= kMaxPaged;
+  a.table_stride = table_stride;
+  // every launch is planned before the first is enqueued
   size_t need = 0;
   int64_t at = 0;
-  for (int i = 0; i < n_seqs; i += kMaxPaged) {
-    const int64_t from = at;
-    fill_seqs(pages, n_seqs, seq_lens, past_lens, page_table, table_stride, i, at, &a.seqs);
-    at = a.seqs.start[a.seqs.n_seqs];
-    if (at == from) continue;
-    if (!plan(&a)) return INFLLM_E_UNSUPPORTED;
+  int launches = 0;
+  bool ok;
+  a.table = page_table;
+  for (int i = 0; plan(p, n_seqs, seq_lens, past_lens, &i, &at, &a, &ok); ++launches) {
+    if (!ok) return INFLLM_E_UNSUPPORTED;
     need = std::max(need, (size_t)partial_rows(a) * part_row_bytes(p));
+    if (i == n_seqs && launches == 0) {  // (a call's only launch is kept)
+      ++launches;
+      break;
+    }
+    a.table = page_table;
   }
   if (need > 0) {
     if (workspace == nullptr || workspace_bytes < need) return INFLLM_E_WORKSPACE;
@@ -472,14 +506,12 @@ infllm_status infllm_paged_attend(const infllm_params* p, const infllm_pages* pa
   }
   if ((st = check_device()) != INFLLM_OK) return st;
   at = 0;
-  for (int i = 0; i < n_seqs; i += kMaxPaged) {
-    if (!single) {
-      const int64_t from = at;
-      fill_seqs(pages, n_seqs, seq_lens, past_lens, page_table, table_stride, i, at, &a.seqs);
-      at = a.seqs.start[a.seqs.n_seqs];
-      if (at == from) continue;
-      plan(&a);
+  for (int i = 0, l = 0; l < launches; ++l) {
+    if (launches > 1) {
+      a.table = page_table;
+      plan(p, n_seqs, seq_lens, past_lens, &i, &at, &a, &ok);
     }
+    if (a.items == 0) continue;
     const int64_t rows = partial_rows(a);
     if (rows > 0) partial_layout(p, workspace, 1, rows, &a.part_o, &a.part_lse, &a.part_exp);
     if ((st = launch_status(launch_paged(a, (hipStream_t)stream))) != INFLLM_OK) return st;

@@ -296,8 +296,8 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedArgs a) {
   const int G = (int)a.d_group.d, rows_wg = 1 << a.rows_log2, R = G * w.len, tile0 = w.rt * rows_wg;
   const int i0 = div_by(tile0, a.d_group), i1 = div_by(min(R, tile0 + rows_wg) - 1, a.d_group);
   const int n = paged_range(a, w.past, i0, i1).n;
-  if (n <= a.part_tiles) return;
-  const int parts = div_by(n + a.part_tiles - 1, a.d_part);
+  if (n <= w.part_tiles) return;
+  const int parts = (n + w.part_tiles - 1) / w.part_tiles;
   const int r = blockIdx.y * (256 / (TPR * GR)) + threadIdx.x / (TPR * GR);
   if (r >= min(rows_wg, R - tile0)) return;
   const int grp = SPLIT ? (threadIdx.x / TPR) % GR : 0, c = threadIdx.x % TPR;

@@ -65,10 +65,13 @@ hipError_t launch_rotate(const RotateArgs& a, hipStream_t s);
 // Attention over pages.  A row tile is a run of rows (query-major, the group's heads
 // packed) of one sequence.  The key tiles that a row tile sees, in order, are those of the
 // initial tokens that lie before the window, then [first of the window, diagonal]; they
-// are cut into parts of part_tiles.  An item is a part of a row tile (the sequences in
-// their order, of a sequence the last row tile first, of a row tile its parts in order), a
+// are cut into parts.  An item is a part of a row tile (the sequences in the order of the
+// list, of a sequence the last row tile first, of a row tile its parts in order), a
 // workgroup an item and a kv head.  Row tiles with several parts leave partial rows (see
 // common.h), item_rows of them per item and kv head, and a merge.
+// A sequence's row tiles are cut into parts of one length, the sequences listed by falling
+// length of their parts, those without new tokens left out.
+constexpr int kMaxAttend = 192;  // sequences of one launch
 struct PagedArgs {
   int n_q_heads, n_kv_heads, head_dim;
   bool bf16;
@@ -86,14 +89,22 @@ struct PagedArgs {
   int rows_log2;             // rows of a row tile
   int tile_queries;          // most queries with rows in one row tile
   int key_tile;              // keys of a tile
-  int part_tiles;
   int items, item_rows;
-  FastDiv d_group, d_kv, d_part;
+  FastDiv d_group, d_kv;
   void* part_o;
   float* part_lse;
   int32_t* part_exp;
-  PagedSeqs seqs;
-  int32_t first[kMaxPaged];  // first item of a sequence
+  int n_pages, page_size;
+  FastDiv d_page;
+  const int32_t* table;
+  int64_t table_stride;
+  int n_seqs;
+  int32_t first[kMaxAttend];       // first item of a sequence
+  int32_t start[kMaxAttend];       // its first new token
+  int32_t len[kMaxAttend];
+  int32_t past[kMaxAttend];        // tokens before it
+  uint8_t parts[kMaxAttend];       // most parts of its row tiles, less 1
+  uint8_t table_row[kMaxAttend];   // its row of the page table
 };
 static_assert(sizeof(PagedArgs) <= 4096, "arguments of a launch");
 
@@ -128,28 +139,31 @@ __host__ __device__ inline int paged_row_tiles(const PagedArgs& a, int group, in
 
 // Where a workgroup of item `item` works.
 struct PagedWork {
-  int s, start, len, past;  // the sequence
+  int start, len, past;  // the sequence
+  int table_row;
   int rt, part;
+  int part_tiles;  // key tiles of a part
 };
 __device__ __forceinline__ PagedWork paged_work(const PagedArgs& a, int item) {
-  constexpr int CH = kMaxPaged / kWave;
+  constexpr int CH = kMaxAttend / kWave;
+  static_assert(CH * kWave == kMaxAttend, "whole waves");
   const int lane = threadIdx.x & 63;
-  int first[CH], start[CH], end[CH], past[CH], n = 0;
+  int first[CH], start[CH], len[CH], past[CH], more[CH], n = 0;
 #pragma unroll
   for (int j = 0; j < CH; ++j) {
-    if (j * kWave >= a.seqs.n_seqs) break;
+    if (j * kWave >= a.n_seqs) break;
     const int i = j * kWave + lane;
     first[j] = a.first[i];
-    start[j] = a.seqs.start[i];
-    end[j] = a.seqs.start[i + 1];
-    past[j] = a.seqs.past[i];
+    start[j] = a.start[i];
+    len[j] = a.len[i];
+    past[j] = a.past[i];
+    more[j] = a.parts[i] | a.table_row[i] << 8;
   }
 #pragma unroll
   for (int j = 0; j < CH; ++j) {
-    if (j * kWave >= a.seqs.n_seqs) break;
-    n += __popcll(__ballot(j * kWave + lane < a.seqs.n_seqs && first[j] <= item));
+    if (j * kWave >= a.n_seqs) break;
+    n += __popcll(__ballot(j * kWave + lane < a.n_seqs && first[j] <= item));
   }
-  // (sequences without new tokens have no items: the last one that begins at or before)
   const int s = __builtin_amdgcn_readfirstlane(n) - 1;
   auto pick = [&](const int (&x)[CH]) {
     int v = __builtin_amdgcn_readlane(x[0], s & 63);
@@ -159,15 +173,18 @@ __device__ __forceinline__ PagedWork paged_work(const PagedArgs& a, int item) {
     return v;
   };
   PagedWork w;
-  w.s = s;
   w.start = pick(start);
-  w.len = pick(end) - w.start;
+  w.len = pick(len);
   w.past = pick(past);
-  const int parts = div_by(paged_most_tiles(a, w.past, w.len) + a.part_tiles - 1, a.d_part);
+  const int m = pick(more);
+  w.table_row = m >> 8;
+  const int parts = (m & 255) + 1;
   const int tiles = paged_row_tiles(a, (int)a.d_group.d, w.len), u = item - pick(first);
   const int down = parts == 1 ? u : tiles == 1 ? 0 : u / parts;
   w.part = u - down * parts;
   w.rt = tiles - 1 - down;
+  const int most = paged_most_tiles(a, w.past, w.len);
+  w.part_tiles = parts == 1 ? most : (most + parts - 1) / parts;
   return w;
 }
 hipError_t launch_paged(const PagedArgs& a, hipStream_t s);

@@ -28,12 +28,19 @@ constexpr int kCap = 1, kSlopes = 2;  // what scores become
 constexpr int kTable = 1024;          // key groups whose places are in LDS
 constexpr int kAhead = 3;             // a step looks up the tile that many ahead
 
+// Places of the first rows of a window's key groups in pieces of 16 bytes (0, which is
+// there, for a page that is not), and whether they are there, a bit each.
+struct KeyTable {
+  uint32_t place[kTable];
+  uint64_t there[kTable / 64];
+};
+
 template <int D>
 struct PagedSmem {
   bf16_t k[2][KB * D];
   bf16_t v[2][KB * D];
-  uint32_t rows[kTable];  // place of a key group's first row in pieces of 16 bytes, or kNoRow
-  int bad[4];             // whether a wave met a page that is not there
+  KeyTable table;
+  int bad[4];  // whether a wave met a page that is not there
 };
 
 // The kernel's arguments, read where they are used rather than held through the loop.
@@ -60,51 +67,71 @@ struct PageRow {
     return place(key, x, table[x]);
   }
 };
-__device__ __forceinline__ PageRow page_row(int s) {
+__device__ __forceinline__ PageRow page_row(int row) {
   LateArgs& a = late_args();
-  return PageRow{a.seqs.table + s * a.seqs.table_stride, FastDiv{a.seqs.d_page.d, a.seqs.d_page.mul}, a.seqs.page_size,
-                 a.seqs.n_pages, a.page16, a.token16};
+  return PageRow{a.table + row * a.table_stride, FastDiv{a.d_page.d, a.d_page.mul}, a.page_size, a.n_pages, a.page16, a.token16};
 }
 
-// The key tiles of a workgroup's part, in order, and the table of their rows' places.
-template <int KT, int THREADS>
+// The key tiles of a workgroup's part, in the order they are taken, and the table of their
+// rows' places.  BACK: from the diagonal backwards.
+template <int KT, int THREADS, bool BACK>
 struct KeyTiles {
-  int sink, shift;      // tile t < sink is at t * KT, others at (t + shift) * KT
+  int sink, shift;      // tile t < sink of the row tile's is at t * KT, others at (t + shift) * KT
   int t_begin, t_end;   // the part's
   int last;             // the sequence's last key
-  int seq;
+  int table_row;
   int gshift;           // keys of a table entry: 8, or 1
   int w0;               // first tile of the table's window
-  __device__ __forceinline__ int key_of(int t) const { return (t < sink ? t : t + shift) * KT; }
+  __device__ __forceinline__ int key_of(int t) const {
+    if (BACK) t = t_begin + t_end - 1 - t;
+    return (t < sink ? t : t + shift) * KT;
+  }
+  // First key of the part's lowest tile.
+  __device__ __forceinline__ int lowest() const { return key_of(BACK ? t_end - 1 : t_begin); }
+  // The tiles [*a, *b) of all but the sink's, counted from key 0, in the order they are taken.
+  __device__ __forceinline__ void range(int* a, int* b) const {
+    const int x = max(*a - shift, t_begin), y = min(*b - shift, t_end);
+    *a = BACK ? t_begin + t_end - y : x;
+    *b = BACK ? t_begin + t_end - x : y;
+  }
   __device__ __forceinline__ int tile_groups() const { return KT >> gshift; }
   __device__ __forceinline__ int window() const { return kTable / tile_groups(); }
   // Fills the table from tile `first` on; whether a page was not there.
-  __device__ __forceinline__ bool fill(uint32_t* rows, int first) {
+  __device__ __forceinline__ bool fill(KeyTable& table, int first) {
     w0 = first;
-    const PageRow pr = page_row(seq);
+    const PageRow pr = page_row(table_row);
     const int gmask = (1 << gshift) - 1, count = min(kTable, (t_end - first) * tile_groups());
     bool bad = false;
-    for (int i = threadIdx.x; i < count; i += THREADS) {
-      const int key = min(key_of(first + (i << gshift) / KT) + ((i << gshift) & (KT - 1)), last & ~gmask);
+    for (int i = threadIdx.x; i - (int)(threadIdx.x & 63) < count; i += THREADS) {  // (whole waves)
+      const int j = min(i, count - 1);
+      const int key = min(key_of(first + (j << gshift) / KT) + ((j << gshift) & (KT - 1)), last & ~gmask);
       const uint32_t p = pr.place(key);
-      rows[i] = p;
+      table.place[i] = p == kNoRow ? 0u : p;
+      const uint64_t there = __ballot(p != kNoRow);
+      if ((i & 63) == 0) table.there[i >> 6] = there;
       bad |= p == kNoRow;
     }
     return bad;
   }
   // The same for the part's first window, and for the pages of the part behind it.
-  __device__ __forceinline__ bool fill_first(uint32_t* rows) {
-    bool bad = fill(rows, t_begin);
+  __device__ __forceinline__ bool fill_first(KeyTable& table) {
+    bool bad = fill(table, t_begin);
     if (t_begin + window() < t_end) {
-      const PageRow pr = page_row(seq);
-      const int from = div_by(key_of(t_begin + window()), pr.d_page);
-      const int to = div_by(min(key_of(t_end - 1) + KT - 1, last), pr.d_page);
+      const PageRow pr = page_row(table_row);
+      const int one = key_of(t_begin + window()), other = key_of(t_end - 1);
+      const int from = div_by(min(one, other), pr.d_page);
+      const int to = div_by(min(max(one, other) + KT - 1, last), pr.d_page);
       for (int x = from + (int)threadIdx.x; x <= to; x += THREADS) {
         const int32_t page = pr.table[x];
         bad |= page < 0 || page >= pr.n_pages;
       }
     }
     return bad;
+  }
+  // Which keys of tile t are there.
+  __device__ __forceinline__ uint64_t there(const KeyTable& table, int t) const {
+    const int i = (t - w0) * tile_groups() + (min((int)(threadIdx.x & 63), min(KT - 1, last - key_of(t))) >> gshift);
+    return __ballot(((table.there[i >> 6] >> (i & 63)) & 1u) != 0);
   }
 };
 
@@ -123,12 +150,12 @@ __device__ __forceinline__ uint64_t seen_keys(int pos, int k0, int window, int n
 // One row formed by its wave from the keys that it sees in the tiles [t_begin, t_end), for
 // rows that a masked value which is not finite has reached: sum_t weight(q . k_t, t) v_t,
 // DPL dims a lane.
-template <typename T, int D, int KT, int THREADS, typename Weight>
-__device__ __forceinline__ void form_row(const KeyTiles<KT, THREADS>& keys, const char* kbase, const char* vbase, const T* qp,
+template <typename T, int D, int KT, int THREADS, bool BACK, typename Weight>
+__device__ __forceinline__ void form_row(const KeyTiles<KT, THREADS, BACK>& keys, const char* kbase, const char* vbase, const T* qp,
                                          int pos, int window, int n_init, Weight weight, float (&acc)[D / 64]) {
   constexpr int DPL = D / 64;
   const int lane = threadIdx.x & 63;
-  const PageRow pr = page_row(keys.seq);
+  const PageRow pr = page_row(keys.table_row);
 #pragma unroll
   for (int e = 0; e < DPL; ++e) acc[e] = 0.f;
   for (int t = keys.t_begin; t < keys.t_end; ++t) {
@@ -173,11 +200,11 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   const int R = G * w.len, tile0 = w.rt * 128;
   const int i0 = div_by(tile0, a.d_group), i1 = div_by(min(R, tile0 + 128) - 1, a.d_group);
   const PagedRange range = paged_range(a, w.past, i0, i1);
-  const int t_begin = w.part * a.part_tiles, t_end = min(t_begin + a.part_tiles, range.n);
+  const int t_begin = w.part * w.part_tiles, t_end = min(t_begin + w.part_tiles, range.n);
   if (t_begin >= t_end) return;  // (the parts of a sequence are as many for each of its row tiles)
-  const bool one_part = range.n <= a.part_tiles;
+  const bool one_part = range.n <= w.part_tiles;
   const int last = w.past + w.len - 1;
-  KeyTiles<KB, 256> keys{range.sink, range.low - range.sink, t_begin, t_end, last, w.s, (a.seqs.page_size & 7) == 0 ? 3 : 0, t_begin};
+  KeyTiles<KB, 256, (MOD & kSlopes) != 0> keys{range.sink, range.low - range.sink, t_begin, t_end, last, w.table_row, (a.page_size & 7) == 0 ? 3 : 0, t_begin};
   auto key_of = [&](int t) { return keys.key_of(t); };  // first key of tile t
 
   const int row0 = tile0 + wave * 32, row = row0 + n;
@@ -191,7 +218,9 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   // Load instruction j of wave w fills pieces [(NI*w + j)*64, +64) of a tile: rows lrow +
   // RPI*j; a lane's slot holds piece (lane % CH) ^ swz(row) of its row.
   const int lrow = KB / 4 * wave + lane / CH;
-  auto piece_of = [&](int j) { return (uint32_t)(lane % CH) ^ (uint32_t)swz<D>(lrow + RPI * j); };
+  // (swz(lrow + RPI * j) is swz(lrow) ^ j at D = 128, swz(lrow) at D = 64)
+  const uint32_t piece0 = (uint32_t)(lane % CH) ^ (uint32_t)swz<D>(lrow);
+  auto piece_of = [&](int j) { return D == 128 ? piece0 ^ (uint32_t)j : piece0; };
   const uint32_t lds_k0 = (uint32_t)(uintptr_t)(INFLLM_LDS bf16_t*)sm.k[0];
   const uint32_t lds_v0 = (uint32_t)(uintptr_t)(INFLLM_LDS bf16_t*)sm.v[0];
   const uint32_t lds_k = lds_k0 + NI * wave * 1024, lds_v = lds_v0 + NI * wave * 1024;
@@ -199,16 +228,16 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     uint32_t o[NI];
   };
   auto load_k = [&](int buf, const Places& f, int j) {
-    lds_load_lane(lds_k + buf * kTileBytes + j * 1024, kbase + (uint64_t)f.o[j] * 16);
+    lds_load_lane(lds_k + buf * kTileBytes + j * 1024, kbase + (uint64_t)(f.o[j] + piece_of(j)) * 16);
   };
   auto load_v = [&](int buf, const Places& f, int j) {
-    lds_load_lane(lds_v + buf * kTileBytes + j * 1024, vbase + (uint64_t)f.o[j] * 16);
+    lds_load_lane(lds_v + buf * kTileBytes + j * 1024, vbase + (uint64_t)(f.o[j] + piece_of(j)) * 16);
   };
 
   // The first tile's pages, the table's, and the query rows are requested at once.
   Places f0;
   {
-    const PageRow pr = page_row(w.s);
+    const PageRow pr = page_row(w.table_row);
     int key[NI], x[NI], page[NI];
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
@@ -219,7 +248,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       const uint32_t p = pr.place(key[j], x[j], page[j]);
-      f0.o[j] = (p == kNoRow ? 0u : p) + piece_of(j);  // (a row that is not there: page 0's, masked)
+      f0.o[j] = p == kNoRow ? 0u : p;  // (a row that is not there: page 0's, masked)
     }
   }
   bf16x8 qreg[KSTEPS];
@@ -233,7 +262,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
 
   const int gshift = keys.gshift;
   const uint32_t gmask = (1u << gshift) - 1u;
-  const bool bad = keys.fill_first(sm.rows);
+  const bool bad = keys.fill_first(sm.table);
 #pragma unroll
   for (int j = 0; j < NI; ++j) load_k(0, f0, j);
 #pragma unroll
@@ -247,19 +276,29 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
 
   // Places of this lane's rows of tile t (past the part's end: of its last tile again,
   // whose keys come from the cache and are not used).
-  const uint32_t lds_rows = (uint32_t)(uintptr_t)(INFLLM_LDS uint32_t*)sm.rows;
-  auto places = [&](int t, Places& f) {
+  const uint32_t lds_rows = (uint32_t)(uintptr_t)(INFLLM_LDS uint32_t*)sm.table.place;
+  struct Entries {
+    uint32_t e[NI];
+    int in_tile;  // last row of the tile that is the sequence's
+  };
+  auto read_entries = [&](int t, Entries& en) {
     t = min(t, t_end - 1);
-    const int in_tile = min(KB - 1, last - key_of(t));  // last row that is the sequence's
+    en.in_tile = min(KB - 1, last - key_of(t));
     const uint32_t at = lds_rows + 4u * (uint32_t)((t - keys.w0) * keys.tile_groups());
-    const int lr = (int)opaque_v((uint32_t)lrow);
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-      const uint32_t r = (uint32_t)min(lr + RPI * j, in_tile);
-      uint32_t p = *(const INFLLM_LDS uint32_t*)(uintptr_t)(at + 4u * (r >> gshift));
-      if (has_bad) p = p == kNoRow ? 0u : p;
-      f.o[j] = p + (r & gmask) * a.token16 + ((uint32_t)(lane % CH) ^ (uint32_t)swz<D>(lr + RPI * j));
+      const uint32_t r = (uint32_t)min(lrow + RPI * j, en.in_tile);
+      en.e[j] = *(const INFLLM_LDS uint32_t*)(uintptr_t)(at + ((r >> gshift) << 2));
     }
+  };
+  auto to_places = [&](const Entries& en, Places& f) {
+#pragma unroll
+    for (int j = 0; j < NI; ++j) f.o[j] = en.e[j] + __umul24((uint32_t)min(lrow + RPI * j, en.in_tile) & gmask, a.token16);
+  };
+  auto places = [&](int t, Places& f) {
+    Entries en;
+    read_entries(t, en);
+    to_places(en, f);
   };
 
   // LDS offsets of the fragments; under the swizzle they are XOR-related (see attend_mfma).
@@ -291,9 +330,11 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     for (int j = 0; j < 16; ++j) oacc[db][j] = 0.f;
   float m_run = -__builtin_inff(), neg_m = 0.f, l_run = 0.f;
 
-  // Scores in the base-2 domain.  Without a form the scale is part of the exponential's
-  // argument; with one a score becomes its final value first.  c tanh(x / c) = c - 2 c / (1 +
-  // e^{2 x / c}): its error of some 2^-23 c is far below what rounding P to bf16 does.
+  // Scores in the base-2 domain.  The scale and the bias are part of the exponential's
+  // argument; a capped score becomes its value first.  c tanh(x / c) = c - 2 c / (1 + e^{2 x /
+  // c}): its error of some 2^-23 c is far below what rounding P to bf16 does.  With a bias
+  // the tiles are taken from the diagonal backwards, where it falls (forwards, the maximum
+  // of a steep one grew with every tile).
   const float log2e = 1.4426950408889634f, c2 = a.sm_scale * log2e;
   float cap_in = 0.f, cap2 = 0.f;
   if constexpr (MOD & kCap) {
@@ -301,44 +342,41 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     cap2 = a.softcap * log2e;
   }
   auto capped = [&](float s) {
-    if constexpr (MOD & kCap)
-      return __builtin_fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + fast_exp2(s * cap_in)), cap2);
-    return s * c2;
+    return __builtin_fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + fast_exp2(s * cap_in)), cap2);
   };
-  auto weight = [&](float z) { return MOD ? fast_exp2(z + neg_m) : fast_exp2(__builtin_fmaf(z, c2, neg_m)); };
   // Key place c of a tile (element e = 16 kb + j of a lane: 32 kb + 8 (j / 4) + j % 4, its
   // half's 4 gsel aside).
   auto place_of = [](int e) { return 32 * (e >> 4) + 8 * ((e & 15) >> 2) + (e & 3); };
-  // What a row sees of a tile, a bit for each key of this lane's half from its first on, and
-  // the bias of that key.
+  // The bias of this half's first key of a tile.
+  auto bias_of = [&](int t) { return MOD & kSlopes ? slope * (float)(key_of(t) + 4 * gsel - pos) : 0.f; };
+  // The exponent of element e of a tile, b its bias_of plus what is to be added.
+  auto exponent = [&](float s, int e, float b) {
+    if constexpr (MOD & kSlopes) b = __builtin_fmaf(slope, (float)place_of(e), b);
+    return MOD & kCap ? s + b : __builtin_fmaf(s, c2, b);
+  };
+  // What a row sees of a tile: a bit for each key of this lane's half from its first on.
   struct Lims {
     uint32_t vis[2];
-    float base;
   };
   auto lims_of = [&](int t, bool masked) {
     Lims l{};
     const int k0 = key_of(t);
     if (masked) {
       uint64_t vis = seen_keys(pos, k0, a.window, a.n_init);
-      if (has_bad) {
-        const uint32_t at = lds_rows + 4u * (uint32_t)((t - keys.w0) * keys.tile_groups() + (min(lane, last - k0) >> gshift));
-        vis &= __ballot(*(const INFLLM_LDS uint32_t*)(uintptr_t)at != kNoRow);
-      }
+      if (has_bad) vis &= keys.there(sm.table, t);
       vis >>= 4 * gsel;
       l.vis[0] = (uint32_t)vis;
       l.vis[1] = (uint32_t)(vis >> 32);
     }
-    if constexpr (MOD & kSlopes) l.base = slope * (float)(k0 + 4 * gsel - pos);
     return l;
   };
-  // Elements [8i, 8i + 8) of a tile's scores: their form, and -inf where the row does not see the key.
+  // Elements [8i, 8i + 8) of a tile's scores: capped, and -inf where the row does not see the key.
   auto form8 = [&](f32x16 (&s)[2], int i, const Lims& l, bool masked) {
 #pragma unroll
     for (int e = 8 * i; e < 8 * i + 8; ++e) {
       const int c = place_of(e);
       float z = s[e >> 4][e & 15];
-      if constexpr (MOD != 0) z = capped(z);
-      if constexpr (MOD & kSlopes) z += __builtin_fmaf(slope, (float)c, l.base);
+      if constexpr (MOD & kCap) z = capped(z);
       if (masked) {
         const uint32_t see = (uint32_t)((int32_t)(l.vis[e >> 4] << (31 - (c & 31))) >> 31);  // all ones or none
         z = __uint_as_float((__float_as_uint(z) & see) | (0xFF800000u & ~see));
@@ -346,10 +384,11 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
       s[e >> 4][e & 15] = z;
     }
   };
-  auto tile_max = [&](const f32x16 (&s)[2]) {
+  auto tile_max = [&](const f32x16 (&s)[2], int t) {
     float mx = -__builtin_inff();
+    const float b = bias_of(t);
 #pragma unroll
-    for (int e = 0; e < 32; ++e) mx = fmaxf(mx, s[e >> 4][e & 15]);
+    for (int e = 0; e < 32; ++e) mx = fmaxf(mx, MOD & kSlopes ? exponent(s[e >> 4][e & 15], e, b) : s[e >> 4][e & 15]);
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
     mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
     return MOD ? mx : mx * c2;
@@ -363,11 +402,11 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     m_run = mx;
     neg_m = mx == -__builtin_inff() ? 0.f : -mx;
     // (a row that sees none of the part's keys: its P are 0)
-    bound = mx != -__builtin_inff() ? kLazy : (int)opaque_v((uint32_t)pos) < key_of(t_begin) ? 0.f : -1.f;
+    bound = mx != -__builtin_inff() ? kLazy : (int)opaque_v((uint32_t)pos) < keys.lowest() ? 0.f : -1.f;
   };
-  auto outgrown = [&](float l_tile, const f32x16 (&s)[2]) -> bool {
+  auto outgrown = [&](float l_tile, const f32x16 (&s)[2], int t) -> bool {
     if (__ballot(l_tile > bound) == 0) return false;
-    const float mx = tile_max(s);
+    const float mx = tile_max(s, t);
     if (__ballot(bound < 0.f ? mx != -__builtin_inff() : l_tile > bound) == 0) return false;
     const float m_new = fmaxf(m_run, mx);
     const float alpha = m_new == -__builtin_inff() ? 1.f : fast_exp2(m_run - m_new);
@@ -381,8 +420,8 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   };
   // Two weights as a bf16 pair; the row sums add them unrounded.  (Rounded by at most 2^-8
   // of each: the instruction takes bf16 weights with bf16 values.)
-  auto p_pair = [&](float z0, float z1, float (&acc)[2], bool first) -> uint32_t {
-    const float e0 = weight(z0), e1 = weight(z1);
+  auto p_pair = [&](float z0, float z1, int e, float b, float (&acc)[2], bool first) -> uint32_t {
+    const float e0 = fast_exp2(exponent(z0, e, b)), e1 = fast_exp2(exponent(z1, e + 1, b));
     acc[0] = first ? e0 : acc[0] + e0;
     acc[1] = first ? e1 : acc[1] + e1;
     bf16x2 pr;
@@ -390,17 +429,19 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     pr[1] = (__bf16)e1;
     return opaque_v(__builtin_bit_cast(uint32_t, pr));
   };
-  auto half_p = [&](const f32x16& s, u32x4 (&p)[2]) {
+  auto half_p = [&](const f32x16 (&s)[2], int h, int t, u32x4 (&p)[2]) {
     float ps[2];
+    const float b = bias_of(t) + neg_m;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) p[i >> 2][i & 3] = p_pair(s[2 * i], s[2 * i + 1], ps, i == 0);
+    for (int i = 0; i < 8; ++i) p[i >> 2][i & 3] = p_pair(s[h][2 * i], s[h][2 * i + 1], 16 * h + 2 * i, b, ps, i == 0);
     return ps[0] + ps[1];
   };
   auto as_frag = [](const u32x4& x) { return __builtin_bit_cast(bf16x8, x); };
 
   // Tiles all of whose keys every row of the workgroup sees: [plain0, plain1).
-  int plain0 = t_begin, plain1 = has_bad ? 0 : min(t_end, (w.past + i0 + 1) / KB - keys.shift);
-  if (a.window > 0) plain0 = max(t_begin, (max(0, w.past + i1 - a.window + 1) + KB - 1) / KB - keys.shift);
+  int plain0 = a.window > 0 ? (max(0, w.past + i1 - a.window + 1) + KB - 1) / KB : 0;
+  int plain1 = has_bad ? 0 : (w.past + i0 + 1) / KB;
+  keys.range(&plain0, &plain1);
 
   // Step of tile t: QK(t+1) beside the second half of P(t), then PV(t) beside the form, mask
   // and first half of P of tile t+1.  At its top K(t+1) and V(t) have landed; it requests
@@ -414,7 +455,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     publish_barrier<0>();
     // (the table's readers are past the barrier; it keeps tile t+1, whose mask may ask it)
     if (t + kAhead >= keys.w0 + keys.window() && t + kAhead < t_end) {
-      keys.fill(sm.rows, t + 1);
+      keys.fill(sm.table, t + 1);
       publish_barrier<0>();
     }
     __builtin_amdgcn_s_setprio(1);
@@ -426,6 +467,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     float ps1[2];
     bf16x8 va[DBLK];
     const uint32_t vaddr = vaddr_of(bc);
+    const float bc_m = bias_of(t) + neg_m;
     {
       const uint32_t ka = kaddr_of(bn);
       bf16x8 a0[2], a1[2];
@@ -455,44 +497,52 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
 #pragma unroll
         for (int i = 0; i < EPC; i += 2) {
           const int x = (EPC * s + i) >> 1;
-          w1[x >> 2][x & 3] = p_pair(cur[1][2 * x], cur[1][2 * x + 1], ps1, x == 0);
+          w1[x >> 2][x & 3] = p_pair(cur[1][2 * x], cur[1][2 * x + 1], 16 + 2 * x, bc_m, ps1, x == 0);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
     float l_tile = l_pend + (ps1[0] + ps1[1]);
-    if (outgrown(l_tile, cur)) {
-      l_tile = half_p(cur[0], p0);
-      l_tile += half_p(cur[1], w1);
+    if (outgrown(l_tile, cur, t)) {
+      l_tile = half_p(cur, 0, t, p0);
+      l_tile += half_p(cur, 1, t, w1);
     }
     l_run += l_tile;
     u32x4 q0[2];
     float ps0[2];
     {
       const Lims l = lims_of(t + 1, MASK);
+      const float bn_m = bias_of(t + 1) + neg_m;
+      Entries en;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if (j == 1) {
+        if (j == 0) {
           f1 = f2;
-          places(t + kAhead, f2);
+          read_entries(t + kAhead, en);
+        } else if (j == 2) {
+          to_places(en, f2);
         }
 #pragma unroll
         for (int db = 0; db < DBLK; ++db) {
           oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[db], as_frag(j < 2 ? p0[j & 1] : w1[j & 1]), oacc[db], 0, 0, 0);
           if (j + 1 < 4) va[db] = vfrag_at(vaddr, db, j + 1);
         }
+        if (j == 3) {  // (formed here, and not between this step and the next)
+#pragma unroll
+          for (int i = 0; i < NI; ++i) f2.o[i] = opaque_v(f2.o[i]);
+        }
         form8(nxt, j, l, MASK);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int x = 2 * j + i;
-          q0[x >> 2][x & 3] = p_pair(nxt[0][2 * x], nxt[0][2 * x + 1], ps0, x == 0);
+          q0[x >> 2][x & 3] = p_pair(nxt[0][2 * x], nxt[0][2 * x + 1], 2 * x, bn_m, ps0, x == 0);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
     p0[0] = q0[0];
     p0[1] = q0[1];
-    l_pend = ps0[0] + ps0[1];
+    l_pend = __uint_as_float(opaque_v(__float_as_uint(ps0[0] + ps0[1])));
   };
   places(t_begin + 1, f1);
   places(t_begin + 2, f2);
@@ -529,8 +579,8 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) form8(sA, i, l, mk);
     }
-    set_max(tile_max(sA));  // the first tile's maximum
-    l_pend = half_p(sA[0], p0);
+    set_max(tile_max(sA, t_begin));  // the first tile's maximum
+    l_pend = half_p(sA, 0, t_begin, p0);
     int t = t_begin;
     // pairs whose next tiles need a mask, plain pairs, pairs that need one again
     for (; t + 2 < t_end && t + 1 < plain0; t += 2) {
@@ -561,10 +611,10 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     top(t);
     // the last tile's P and PV
     u32x4 w1[2];
-    float l_tile = l_pend + half_p(sA[1], w1);
-    if (outgrown(l_tile, sA)) {
-      l_tile = half_p(sA[0], p0);
-      l_tile += half_p(sA[1], w1);
+    float l_tile = l_pend + half_p(sA, 1, t, w1);
+    if (outgrown(l_tile, sA, t)) {
+      l_tile = half_p(sA, 0, t, p0);
+      l_tile += half_p(sA, 1, t, w1);
     }
     l_run += l_tile;
     const uint32_t vaddr = vaddr_of((t - t_begin) & 1);
@@ -651,7 +701,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
         float acc[DPL];
         form_row<bf16_t, D>(keys, kbase, vbase, (const bf16_t*)late.q + (int64_t)(w.start + i) * late.q_tok + (int64_t)h * late.q_head,
                             p_r, a.window, a.n_init,
-                            [&](float s, int key) { return fast_exp2(capped(s) + slope_r * (float)(key - p_r) + nm); }, acc);
+                            [&](float s, int key) { return fast_exp2((MOD & kCap ? capped(s) : s * c2) + slope_r * (float)(key - p_r) + nm); }, acc);
         float amax = 0.f;  // (of the finite ones, which keep their precision)
 #pragma unroll
         for (int e = 0; e < DPL; ++e) {
@@ -719,7 +769,7 @@ __global__ void __launch_bounds__(64 * NW, D == 64 && NW > 1 ? 2 : 1) paged_f32_
   constexpr uint32_t kTileBytes = KT * D * 4;
   __shared__ __attribute__((aligned(256))) float ks[2][KT * D];
   __shared__ __attribute__((aligned(256))) float vs[2][KT * D];
-  __shared__ uint32_t rows[kTable];
+  __shared__ KeyTable table;
   __shared__ int wave_bad[NW];
 
   const int tid = threadIdx.x, lane = tid & 63;
@@ -731,11 +781,11 @@ __global__ void __launch_bounds__(64 * NW, D == 64 && NW > 1 ? 2 : 1) paged_f32_
   const int R = G * w.len, tile0 = w.rt * RW;
   const int i0 = div_by(tile0, a.d_group), i1 = div_by(min(R, tile0 + RW) - 1, a.d_group);
   const PagedRange range = paged_range(a, w.past, i0, i1);
-  const int t_begin = w.part * a.part_tiles, t_end = min(t_begin + a.part_tiles, range.n);
+  const int t_begin = w.part * w.part_tiles, t_end = min(t_begin + w.part_tiles, range.n);
   if (t_begin >= t_end) return;
-  const bool one_part = range.n <= a.part_tiles;
+  const bool one_part = range.n <= w.part_tiles;
   const int last = w.past + w.len - 1;
-  KeyTiles<KT, 64 * NW> keys{range.sink, range.low - range.sink, t_begin, t_end, last, w.s, (a.seqs.page_size & 7) == 0 ? 3 : 0, t_begin};
+  KeyTiles<KT, 64 * NW, (MOD & kSlopes) != 0> keys{range.sink, range.low - range.sink, t_begin, t_end, last, w.table_row, (a.page_size & 7) == 0 ? 3 : 0, t_begin};
 
   const int row0 = tile0 + wave * 32, row = row0 + n;
   const bool active = row0 < R, row_ok = row < R;
@@ -756,7 +806,7 @@ __global__ void __launch_bounds__(64 * NW, D == 64 && NW > 1 ? 2 : 1) paged_f32_
   if constexpr (MOD & kSlopes) slope = a.slopes[qh];
 
   {
-    const bool any = __ballot(keys.fill_first(rows)) != 0;
+    const bool any = __ballot(keys.fill_first(table)) != 0;
     if (lane == 0) wave_bad[wave] = any;
   }
   lds_barrier();
@@ -774,8 +824,7 @@ __global__ void __launch_bounds__(64 * NW, D == 64 && NW > 1 ? 2 : 1) paged_f32_
     for (int j = 0; j < NI; ++j) {
       const int lr = (NI * wave + j) * RPI + lane / GPR;
       const uint32_t r = (uint32_t)min(lr, in_tile);
-      uint32_t p = rows[(t - keys.w0) * keys.tile_groups() + (r >> keys.gshift)];
-      p = p == kNoRow ? 0u : p + (r & gmask) * a.token16;  // (a row that is not there: page 0's, masked)
+      const uint32_t p = table.place[(t - keys.w0) * keys.tile_groups() + (r >> keys.gshift)] + __umul24(r & gmask, a.token16);
       const uint64_t off = ((uint64_t)p + (uint32_t)((lane % GPR) ^ (lr & 15))) * 16;
       lds_load_lane(lds_k + buf + j * 1024, kbase + off);
       lds_load_lane(lds_v + buf + j * 1024, vbase + off);
@@ -796,9 +845,9 @@ __global__ void __launch_bounds__(64 * NW, D == 64 && NW > 1 ? 2 : 1) paged_f32_
   };
   // tiles all of whose keys every row of the wave sees: [plain0, plain1)
   const int w0 = div_by(min(row0, R - 1), a.d_group), w1 = div_by(min(row0 + 31, R - 1), a.d_group);
-  int plain0 = t_begin;
-  const int plain1 = has_bad ? 0 : min(t_end, (w.past + w0 + 1) / KT - keys.shift);
-  if (a.window > 0) plain0 = (max(0, w.past + w1 - a.window + 1) + KT - 1) / KT - keys.shift;
+  int plain0 = a.window > 0 ? (max(0, w.past + w1 - a.window + 1) + KT - 1) / KT : 0;
+  int plain1 = has_bad ? 0 : (w.past + w0 + 1) / KT;
+  keys.range(&plain0, &plain1);
 
   load_tile(t_begin);
   for (int t = t_begin; t < t_end; ++t) {
@@ -806,7 +855,7 @@ __global__ void __launch_bounds__(64 * NW, D == 64 && NW > 1 ? 2 : 1) paged_f32_
     asm volatile("" ::: "memory");
     if (t + 1 < t_end) {
       if (t + 1 >= keys.w0 + keys.window()) {
-        keys.fill(rows, t);  // (tile t's mask may ask it)
+        keys.fill(table, t);  // (tile t's mask may ask it)
         lds_barrier();
       }
       load_tile(t + 1);
@@ -837,7 +886,7 @@ __global__ void __launch_bounds__(64 * NW, D == 64 && NW > 1 ? 2 : 1) paged_f32_
     }
     if (!plain) {
       uint64_t vis = seen_keys(pos, k0, a.window, a.n_init);
-      if (has_bad) vis &= __ballot(rows[(t - keys.w0) * keys.tile_groups() + (min(n, last - k0) >> keys.gshift)] != kNoRow);
+      if (has_bad) vis &= keys.there(table, t);
       const uint32_t see = (uint32_t)vis >> (4 * gsel);
 #pragma unroll
       for (int j = 0; j < 16; ++j) s[j] = ((see >> (8 * (j >> 2) + (j & 3))) & 1u) != 0 ? s[j] : -__builtin_inff();

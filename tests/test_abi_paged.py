@@ -166,6 +166,8 @@ def test_attend_refusals(L):  # noqa: F811
     assert call(lse=FAKE + 2) == SHAPE
     # rows of k past 64 GiB
     assert call(pages=pages(page_stride=(1 << 35) // 99 // 8 * 8 + 64)) == UNSUPPORTED
+    # tokens 256 MiB apart
+    assert call(pages=pages(token_stride=1 << 27, page_stride=1 << 31, n_pages=2)) == UNSUPPORTED
     # total * G past 2^31
     assert call(lens=i32(1 << 29, 0, 1), pasts=i64(0, 0, 0), width=1 << 30) == UNSUPPORTED
     pr = P(rope_inv_freq=F.rope_frequencies(128))
