@@ -9,6 +9,8 @@
 // least half as many as a workgroup has groups: a workgroup per row, its threads split into groups that take every GR-th part and are
 // joined in LDS -- the parts are then the only parallelism (25 parts of 32 rows: 6.8 us
 // one thread per piece, 4.3 split; 16 parts of 2,048 rows: 3.7 and 6.5).
+#include <type_traits>
+
 #include "paged.h"
 #include "shared.h"
 
@@ -283,32 +285,40 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixArgs a) {
   }
 }
 
-// Paged attention: the parts of a row tile's rows.  The workgroups of an item that is a row
-// tile's first part join its parts' rows (the item numbers of a row tile's parts are
-// consecutive), those of others end at once.  SPLIT: few rows to an item (decoding), a wave
-// per row whose lane groups take every GR-th part; else a group of lanes per row.
+// Paged attention: the parts of a row tile's rows.  Of a row tile with P parts the
+// workgroups of each part's item join a P-th of the rows, so that none is idle.  SPLIT: few
+// rows to an item (decoding), a wave per row whose lane groups take every GR-th part; else
+// a group of lanes per row.  Bound by its chain of loads (arguments, the parts' rows): 5 us
+// for one token's parts.
 template <typename T, bool HALF, int D, bool SPLIT>
 __global__ void __launch_bounds__(256) paged_merge_kernel(PagedArgs a) {
-  constexpr int DPT = HALF ? 8 : 4, TPR = D / DPT, GR = SPLIT ? 64 / TPR : 1, CH = 8;
+  constexpr int DPT = HALF ? 8 : 4, TPR = D / DPT, GR = SPLIT ? 64 / TPR : 1;
   const int item = div_by(blockIdx.x, a.d_kv), g = (int)blockIdx.x - item * (int)a.d_kv.d;
   const PagedWork w = paged_work(a, item);
-  if (w.part != 0) return;
   const int G = (int)a.d_group.d, rows_wg = 1 << a.rows_log2, R = G * w.len, tile0 = w.rt * rows_wg;
   const int i0 = div_by(tile0, a.d_group), i1 = div_by(min(R, tile0 + rows_wg) - 1, a.d_group);
   const int n = paged_range(a, w.past, i0, i1).n;
-  if (n <= w.part_tiles) return;
   const int parts = (n + w.part_tiles - 1) / w.part_tiles;
-  const int r = blockIdx.y * (256 / (TPR * GR)) + threadIdx.x / (TPR * GR);
-  if (r >= min(rows_wg, R - tile0)) return;
+  if (parts == 1 || w.part >= parts) return;
+  const int rows = min(rows_wg, R - tile0), share = (rows + parts - 1) / parts;
+  const int r_end = min(rows, (w.part + 1) * share);
+  const int r = w.part * share + blockIdx.y * (256 / (TPR * GR)) + threadIdx.x / (TPR * GR);
+  if (r >= r_end) return;
   const int grp = SPLIT ? (threadIdx.x / TPR) % GR : 0, c = threadIdx.x % TPR;
-  const int64_t row0 = ((int64_t)item * a.n_kv_heads + g) * a.item_rows + r, step = (int64_t)a.n_kv_heads * a.item_rows;
+  const int64_t row0 = ((int64_t)(item - w.part) * a.n_kv_heads + g) * a.item_rows + r, step = (int64_t)a.n_kv_heads * a.item_rows;
   float M = -__builtin_inff(), tot = 0.f, acc[DPT] = {};
-  for (int p0 = grp; p0 < parts; p0 += CH * GR) {
-    float l[CH], o[CH][DPT];
+  auto join = [&](auto chunk) {
+    constexpr int CH = decltype(chunk)::value;
+    for (int p0 = grp; p0 < parts; p0 += CH * GR) {
+      float l[CH], o[CH][DPT];
 #pragma unroll
-    for (int j = 0; j < CH; ++j) load_piece<HALF>(a, row0 + min(p0 + j * GR, parts - 1) * step, c, o[j], l[j]);
-    add_parts<DPT, CH, true>(l, o, (parts - p0 + GR - 1) / GR, p0 > grp, M, tot, acc);
-  }
+      for (int j = 0; j < CH; ++j) load_piece<HALF>(a, row0 + min(p0 + j * GR, parts - 1) * step, c, o[j], l[j]);
+      add_parts<DPT, CH, true>(l, o, (parts - p0 + GR - 1) / GR, p0 > grp, M, tot, acc);
+    }
+  };
+  if (parts <= 2 * GR) join(std::integral_constant<int, 2>{});
+  else if (parts <= 4 * GR) join(std::integral_constant<int, 4>{});
+  else join(std::integral_constant<int, 8>{});
   if constexpr (SPLIT) {
 #pragma unroll
     for (int o = TPR; o < 64; o <<= 1) {
@@ -332,8 +342,8 @@ template <typename T, bool HALF, int D>
 void launch_paged_merge_t(const PagedArgs& a, hipStream_t s) {
   constexpr int groups = 256 / (D / (HALF ? 8 : 4));  // of a workgroup
   const bool split = a.item_rows <= 16;
-  const int per_wg = split ? 4 : groups;
-  const dim3 grid(a.items * a.n_kv_heads, (a.item_rows + per_wg - 1) / per_wg), block(256);
+  const int per_wg = split ? 4 : groups, share = (a.item_rows + 1) / 2;  // (of two parts, the most)
+  const dim3 grid(a.items * a.n_kv_heads, (share + per_wg - 1) / per_wg), block(256);
   if (split) hipLaunchKernelGGL((paged_merge_kernel<T, HALF, D, true>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((paged_merge_kernel<T, HALF, D, false>), grid, block, 0, s, a);
 }
