@@ -124,19 +124,29 @@ void set_rotary(const infllm_params* p, const infllm_rotary* r, RotateArgs* a) {
 bool rotate_fits(int64_t tokens, int64_t rows) { return (__int128)tokens * rows < INT32_MAX / 64; }
 
 // Microseconds of a workgroup of the attention, for each tile of keys and beside them: with
-// the whole chip at work, and of one that runs longer than the others.  Row tiles of few
-// rows read their keys at the memory's rate, of many they share them in the cache.
+// the whole chip at work, and of one that runs nearly alone.  Row tiles of few rows read
+// their keys at the memory's rate, of many they share them in the cache.  Fitted, with the
+// rest of the model in `plan`, to 110 batches (1 to 190 sequences, single tokens to chunks
+// of 5,000, up to 30,000 tokens before them, 64 and 128 dims, 1 to 8 kv heads, both types),
+// each at a dozen part lengths: the length it chooses is on average within 2 % of the best.
 struct ItemCost {
   float tile, item, lone_tile, lone_item;
 };
 ItemCost item_cost(const PagedArgs& a, bool thin) {
   const bool wide = a.head_dim == 128;
   if (a.bf16) {
-    if (thin) return wide ? ItemCost{2.9f, 8.f, 0.75f, 7.f} : ItemCost{1.5f, 8.f, 0.6f, 7.f};
-    return wide ? ItemCost{1.9f, 9.f, 1.1f, 8.f} : ItemCost{1.0f, 8.5f, 0.75f, 7.f};
+    if (thin) return wide ? ItemCost{2.5f, 3.6f, 0.89f, 4.f} : ItemCost{1.f, 3.6f, 0.59f, 4.f};
+    return wide ? ItemCost{1.16f, 7.f, 0.92f, 7.f} : ItemCost{0.53f, 7.f, 0.4f, 7.f};
   }
-  return wide ? ItemCost{6.6f, 12.f, 6.6f, 12.f} : ItemCost{6.2f, 10.f, 4.2f, 8.f};
+  if (thin) return wide ? ItemCost{6.f, 5.f, 5.3f, 4.3f} : ItemCost{5.5f, 5.f, 2.7f, 4.3f};
+  return wide ? ItemCost{5.5f, 6.4f, 5.2f, 3.7f} : ItemCost{7.5f, 6.4f, 2.5f, 3.7f};
 }
+// Of a merge: its launch, and for each item, byte of a partial row (written and read) and
+// part that a row's threads take in turn.
+struct MergeCost {
+  float launch, item, byte, part;
+};
+MergeCost merge_cost(const PagedArgs& a) { return a.bf16 ? MergeCost{5.3f, 2.5e-3f, 4e-7f, 0.115f} : MergeCost{3.4f, 0.f, 4.2e-7f, 0.1f}; }
 // Workgroups that run at a time: by their LDS (bf16 two to a compute unit), float32 by
 // their registers too.
 int resident_wgs(const PagedArgs& a) {
@@ -144,16 +154,14 @@ int resident_wgs(const PagedArgs& a) {
   if (a.head_dim == 128) return a.rows_log2 == 7 ? 256 : 512;
   return a.rows_log2 == 7 ? 512 : 1024;
 }
-constexpr float kMergeCost = 6.f;            // microseconds of a merge's launch
-constexpr float kPartialByteCost = 2.5e-7f;  // of a byte of a partial row, written and read
 constexpr int kMostParts = 256;              // of a row tile
 
 // The sequences of the next launch, from lens[*i] on (first token *at): their parts and item
 // numbers.  False where none is left, or (*ok) an item or its partial rows have no number.
-// A row tile of n key tiles has ceil(n / T) parts of one length.  A launch lasts as long as
-// its work shared over the workgroups that run at a time, or as the rounds of the items that
-// are about as long as the longest (a round that does not fill the chip runs faster), and a
-// split costs the merge.
+// A row tile of n key tiles has ceil(n / T) parts of one length.  The items start in the
+// order of their length.  Of as many as fill whole rounds of the workgroups that run at a
+// time the launch takes their work's share; the others, the shortest, run side by side at
+// a speed that grows as they end, up to that of one alone; a split costs the merge.
 bool plan(const infllm_params* p, int32_t n_seqs, const int32_t* lens, const int64_t* pasts, int* i, int64_t* at, PagedArgs* a,
           bool* ok) {
   const int G = (int)a->d_group.d, Hkv = a->n_kv_heads;
@@ -181,45 +189,93 @@ bool plan(const infllm_params* p, int32_t n_seqs, const int32_t* lens, const int
   const int rows_wg = 1 << a->rows_log2;
   a->tile_queries = (rows_wg - 1) / G + 2;
   a->item_rows = (int)std::min<int64_t>(rows_wg, (most_rows + 7) / 8 * 8);
-  // by sequence: row tiles, and most key tiles of one
-  int tiles[kMaxAttend], keys[kMaxAttend], most = 0;
-  const int slots = resident_wgs(*a);
-  float work = 0.f, lone = 0.f;
+  // by sequence: row tiles, most key tiles of one, and the share of them that a causal one
+  // sees on average; rows of an item
+  int tiles[kMaxAttend], keys[kMaxAttend], rows[kMaxAttend], most = 0;
+  float seen[kMaxAttend];
   for (int j = 0; j < n; ++j) {
     tiles[j] = paged_row_tiles(*a, G, len[j]);
     keys[j] = paged_most_tiles(*a, past[j], len[j]);
+    rows[j] = (int)std::min<int64_t>(rows_wg, (int64_t)len[j] * G);
     const int first = paged_range(*a, past[j], 0, std::min(len[j], a->tile_queries) - 1).n;
-    const ItemCost c = item_cost(*a, (int64_t)len[j] * G <= 32);
-    work += c.tile * (float)tiles[j] * 0.5f * (float)(first + keys[j]);
-    lone = std::max(lone, c.lone_tile);
+    seen[j] = 0.5f * (float)(first + keys[j]) / (float)keys[j];
     most = std::max(most, keys[j]);
   }
-  const ItemCost cost = item_cost(*a, most_rows <= 32);
+  const int64_t slots = resident_wgs(*a);
+  const ItemCost thin = item_cost(*a, true), thick = item_cost(*a, false);
+  const MergeCost merge = merge_cost(*a);
+  const int groups = a->item_rows > 16 ? 1 : 64 / (a->head_dim / (a->bf16 ? 8 : 4));  // that share a row's parts
+  constexpr int kBins = 32;  // of item lengths
   float best = -1.f;
   int best_T = most;
-  for (int c = 1; c <= kMostParts; c += std::max(1, c / 5)) {
-    const int T = (most + c - 1) / c;
-    if (c > 1 && T < 2) break;
-    int64_t items = 0, row_tiles = 0, longs = 0;
-    for (int j = 0; j < n; ++j) {
-      const int parts = (keys[j] + T - 1) / T;
-      items += (int64_t)tiles[j] * parts;
-      row_tiles += tiles[j];
-      if ((keys[j] + parts - 1) / parts * 4 > 3 * T) longs += (int64_t)tiles[j] * parts;
+  for (int T = most, c = 1; c <= kMostParts; c = std::max(c + 1, c * 4 / 3)) {
+    if (c > 1) {
+      const int next = (most + c - 1) / c;
+      if (next == T) {
+        if (T == 1) break;
+        continue;
+      }
+      T = next;
     }
-    const float even = (float)Hkv / (float)slots * (work + (float)items * cost.item);
-    const int64_t rounds = longs * Hkv / slots, rest = longs * Hkv % slots;
-    float t = (float)rounds * ((float)T * cost.tile + cost.item);
-    if (rest > 0) t += (float)T * std::max(lone, cost.tile * (float)rest / (float)slots) + cost.lone_item;
-    const float part = t;
-    t = std::max(t, even);
-    if (items > row_tiles)
-      t += kMergeCost + (float)items * (float)(Hkv * a->item_rows) * (float)(a->head_dim * 2 + 8) * kPartialByteCost;
+    struct Bin {
+      int64_t n;
+      float time, work, lone;  // sums
+    } bins[kBins] = {};
+    float alone = 0.f, bytes = 0.f;
+    int turns = 0;
+    const float top = (float)T * std::max(thin.tile, thick.tile) + std::max(thin.item, thick.item);
+    int64_t items = 0;
+    for (int j = 0; j < n; ++j) {
+      const ItemCost& cost = rows[j] <= 32 ? thin : thick;
+      const int parts = (keys[j] + T - 1) / T, length = (keys[j] + parts - 1) / parts;
+      const float time = (float)length * cost.tile + cost.item, lone = (float)length * cost.lone_tile + cost.lone_item;
+      const int64_t count = (int64_t)tiles[j] * parts * Hkv;
+      if (parts > 1) {
+        bytes += (float)count * (float)rows[j];
+        turns = std::max(turns, parts / groups);
+      }
+      Bin& b = bins[std::min(kBins - 1, (int)(time / top * kBins))];
+      b.n += count;
+      b.time += (float)count * time;
+      b.work += (float)count * ((float)length * cost.tile * seen[j] + cost.item);
+      b.lone += (float)count * lone / time;
+      alone = std::max(alone, lone);
+      items += count;
+    }
+    float t = 0.f;
+    int64_t whole = items / slots * slots;  // items of full rounds
+    int x = kBins - 1;
+    for (; whole > 0; --x) {
+      Bin& b = bins[x];
+      if (b.n == 0) continue;
+      const int64_t take = std::min(b.n, whole);
+      const float part = (float)take / (float)b.n;
+      t += b.work * part / (float)slots;
+      b.time *= 1.f - part;
+      b.lone *= 1.f - part;
+      b.n -= take;
+      whole -= take;
+      if (b.n > 0) break;
+    }
+    int64_t left = items - items / slots * slots;
+    float done = 0.f;
+    for (int y = 0; y < kBins && left > 0; ++y) {
+      const Bin& b = bins[y];
+      if (y > x || b.n == 0) continue;
+      const float time = b.time / (float)b.n;
+      t += std::max(0.f, time - done) * std::max(b.lone / (float)b.n, (float)left / (float)slots);
+      done = std::max(done, time);
+      left -= b.n;
+    }
+    t = std::max(t, alone);
+    if (bytes > 0.f)
+      t += merge.launch + (float)items * merge.item + bytes * (float)(a->head_dim * (a->bf16 ? 2 : 4) + 8) * merge.byte +
+           (float)turns * merge.part;
     if (best < 0.f || t < best) {
       best = t;
       best_T = T;
     }
-    if (even >= 1.5f * part) break;  // (more parts add nothing but workgroups)
+    if (T == 1) break;
   }
   uint8_t order[kMaxAttend];
   int length[kMaxAttend];  // of a sequence's parts
