@@ -180,7 +180,13 @@ __device__ __forceinline__ void form_row(const KeyTiles<KT, THREADS, BACK>& keys
   }
 }
 
-template <int D, int MOD>
+// GROUPS: pages of a multiple of 8 tokens.  The rows of a load instruction then lie in one
+// group of 8 keys, whose place is uniform: its base goes through scalar registers, and a
+// lane's offset from it is the same for every tile.  (With an address formed by every lane
+// for every load the loop had 6.4 vector instructions for a matrix instruction instead of
+// 5.)  Rows of the last group behind the sequence's end are loaded with it, whatever the
+// page holds there, and those values are cleared in LDS.
+template <int D, int MOD, bool GROUPS>
 __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   constexpr int CH = D / 8;                       // 16-byte pieces of a row
   constexpr int KSTEPS = D / 16, DBLK = D / 32;
@@ -204,7 +210,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   if (t_begin >= t_end) return;  // (the parts of a sequence are as many for each of its row tiles)
   const bool one_part = range.n <= w.part_tiles;
   const int last = w.past + w.len - 1;
-  KeyTiles<KB, 256, (MOD & kSlopes) != 0> keys{range.sink, range.low - range.sink, t_begin, t_end, last, w.table_row, (a.page_size & 7) == 0 ? 3 : 0, t_begin};
+  KeyTiles<KB, 256, (MOD & kSlopes) != 0> keys{range.sink, range.low - range.sink, t_begin, t_end, last, w.table_row, GROUPS ? 3 : 0, t_begin};
   auto key_of = [&](int t) { return keys.key_of(t); };  // first key of tile t
 
   const int row0 = tile0 + wave * 32, row = row0 + n;
@@ -224,31 +230,37 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   const uint32_t lds_k0 = (uint32_t)(uintptr_t)(INFLLM_LDS bf16_t*)sm.k[0];
   const uint32_t lds_v0 = (uint32_t)(uintptr_t)(INFLLM_LDS bf16_t*)sm.v[0];
   const uint32_t lds_k = lds_k0 + NI * wave * 1024, lds_v = lds_v0 + NI * wave * 1024;
+  // Places of a tile's rows: of the wave's two groups, or of the row of each load.
+  constexpr int NP = GROUPS ? 2 : NI;
   struct Places {
-    uint32_t o[NI];
+    uint32_t o[NP];
   };
-  auto load_k = [&](int buf, const Places& f, int j) {
-    lds_load_lane(lds_k + buf * kTileBytes + j * 1024, kbase + (uint64_t)(f.o[j] + piece_of(j)) * 16);
+  uint32_t voff[NI];  // bytes from a group's place to this lane's piece
+#pragma unroll
+  for (int j = 0; j < NI; ++j) voff[j] = 16u * (piece_of(j) + __umul24((uint32_t)(RPI * j + lane / CH) & 7u, a.token16));
+  auto load = [&](uint32_t lds, const char* base, const Places& f, int j) {
+    if constexpr (GROUPS) lds_load(lds, base + ((uint64_t)f.o[RPI * j / 8] << 4), voff[j]);
+    else lds_load_lane(lds, base + (uint64_t)(f.o[j] + piece_of(j)) * 16);
   };
-  auto load_v = [&](int buf, const Places& f, int j) {
-    lds_load_lane(lds_v + buf * kTileBytes + j * 1024, vbase + (uint64_t)(f.o[j] + piece_of(j)) * 16);
-  };
+  auto load_k = [&](int buf, const Places& f, int j) { load(lds_k + buf * kTileBytes + j * 1024, kbase, f, j); };
+  auto load_v = [&](int buf, const Places& f, int j) { load(lds_v + buf * kTileBytes + j * 1024, vbase, f, j); };
 
   // The first tile's pages, the table's, and the query rows are requested at once.
   Places f0;
   {
     const PageRow pr = page_row(w.table_row);
-    int key[NI], x[NI], page[NI];
+    int key[NP], x[NP], page[NP];
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      key[j] = min(key_of(t_begin) + lrow + RPI * j, last);
+    for (int j = 0; j < NP; ++j) {
+      key[j] = GROUPS ? min(key_of(t_begin) + KB / 4 * wave + 8 * j, last & ~7) : min(key_of(t_begin) + lrow + RPI * j, last);
       x[j] = div_by(key[j], pr.d_page);
       page[j] = pr.table[x[j]];
     }
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
+    for (int j = 0; j < NP; ++j) {
       const uint32_t p = pr.place(key[j], x[j], page[j]);
       f0.o[j] = p == kNoRow ? 0u : p;  // (a row that is not there: page 0's, masked)
+      if constexpr (GROUPS) f0.o[j] = (uint32_t)__builtin_amdgcn_readfirstlane((int)f0.o[j]);
     }
   }
   bf16x8 qreg[KSTEPS];
@@ -260,8 +272,6 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   float slope = 0.f;
   if constexpr (MOD & kSlopes) slope = a.slopes[qh] * 1.4426950408889634f;
 
-  const int gshift = keys.gshift;
-  const uint32_t gmask = (1u << gshift) - 1u;
   const bool bad = keys.fill_first(sm.table);
 #pragma unroll
   for (int j = 0; j < NI; ++j) load_k(0, f0, j);
@@ -274,26 +284,29 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   lds_barrier();
   const bool has_bad = (sm.bad[0] | sm.bad[1] | sm.bad[2] | sm.bad[3]) != 0;
 
-  // Places of this lane's rows of tile t (past the part's end: of its last tile again,
+  // Places of the wave's rows of tile t (past the part's end: of its last tile again,
   // whose keys come from the cache and are not used).
   const uint32_t lds_rows = (uint32_t)(uintptr_t)(INFLLM_LDS uint32_t*)sm.table.place;
   struct Entries {
-    uint32_t e[NI];
-    int in_tile;  // last row of the tile that is the sequence's
+    uint32_t e[NP];
   };
   auto read_entries = [&](int t, Entries& en) {
-    t = min(t, t_end - 1);
-    en.in_tile = min(KB - 1, last - key_of(t));
-    const uint32_t at = lds_rows + 4u * (uint32_t)((t - keys.w0) * keys.tile_groups());
+    const uint32_t at = lds_rows + 4u * (uint32_t)((min(t, t_end - 1) - keys.w0) * keys.tile_groups());
+    if constexpr (GROUPS) {
+      const u32x2 x = *(const INFLLM_LDS u32x2*)(uintptr_t)(at + 8u * wave);
+      en.e[0] = x[0];
+      en.e[1] = x[1];
+    } else {
 #pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      const uint32_t r = (uint32_t)min(lrow + RPI * j, en.in_tile);
-      en.e[j] = *(const INFLLM_LDS uint32_t*)(uintptr_t)(at + ((r >> gshift) << 2));
+      for (int j = 0; j < NP; ++j) en.e[j] = *(const INFLLM_LDS uint32_t*)(uintptr_t)(at + 4u * (uint32_t)(lrow + RPI * j));
     }
   };
   auto to_places = [&](const Entries& en, Places& f) {
 #pragma unroll
-    for (int j = 0; j < NI; ++j) f.o[j] = en.e[j] + __umul24((uint32_t)min(lrow + RPI * j, en.in_tile) & gmask, a.token16);
+    for (int j = 0; j < NP; ++j) {
+      if constexpr (GROUPS) f.o[j] = (uint32_t)__builtin_amdgcn_readfirstlane((int)en.e[j]);
+      else f.o[j] = opaque_v(en.e[j]);
+    }
   };
   auto places = [&](int t, Places& f) {
     Entries en;
@@ -453,6 +466,12 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   auto top = [&](int t) {
     __builtin_amdgcn_s_setprio(0);
     publish_barrier<0>();
+    if (GROUPS && key_of(t) + KB - 1 > last) {
+      // V rows behind the sequence's end: whatever the page holds meets weights of 0
+      for (int i = (last - key_of(t) + 1) * CH + tid; i < KB * CH; i += 256)
+        *(INFLLM_LDS u32x4*)(uintptr_t)(lds_v0 + ((t - t_begin) & 1) * kTileBytes + 16u * i) = u32x4{0, 0, 0, 0};
+      lds_barrier();
+    }
     // (the table's readers are past the barrier; it keeps tile t+1, whose mask may ask it)
     if (t + kAhead >= keys.w0 + keys.window() && t + kAhead < t_end) {
       keys.fill(sm.table, t + 1);
@@ -526,10 +545,6 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
         for (int db = 0; db < DBLK; ++db) {
           oacc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[db], as_frag(j < 2 ? p0[j & 1] : w1[j & 1]), oacc[db], 0, 0, 0);
           if (j + 1 < 4) va[db] = vfrag_at(vaddr, db, j + 1);
-        }
-        if (j == 3) {  // (formed here, and not between this step and the next)
-#pragma unroll
-          for (int i = 0; i < NI; ++i) f2.o[i] = opaque_v(f2.o[i]);
         }
         form8(nxt, j, l, MASK);
 #pragma unroll
@@ -732,10 +747,10 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   }
   lds_order();
   {
-    constexpr int NP = 32 * CH / 64;  // pieces of a lane
+    constexpr int NS = 32 * CH / 64;  // pieces of a lane
     const int r0 = lane_e / CH, ch = lane_e % CH;
 #pragma unroll
-    for (int k = 0; k < NP; ++k) {
+    for (int k = 0; k < NS; ++k) {
       if (row0 + RPI * k >= R) break;  // (uniform)
       const int r = row0 + RPI * k + r0;
       if (r >= R) continue;
@@ -980,7 +995,8 @@ __global__ void __launch_bounds__(64 * NW, D == 64 && NW > 1 ? 2 : 1) paged_f32_
 template <int D, int MOD>
 void launch_form(const PagedArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(a.items * a.n_kv_heads)), block(2 << a.rows_log2);
-  if (a.bf16) hipLaunchKernelGGL((paged_mfma_kernel<D, MOD>), grid, block, 0, s, a);
+  if (a.bf16 && a.page_size % 8 == 0) hipLaunchKernelGGL((paged_mfma_kernel<D, MOD, true>), grid, block, 0, s, a);
+  else if (a.bf16) hipLaunchKernelGGL((paged_mfma_kernel<D, MOD, false>), grid, block, 0, s, a);
   else if (a.rows_log2 == 7) hipLaunchKernelGGL((paged_f32_kernel<D, 4, MOD>), grid, block, 0, s, a);
   else if (a.rows_log2 == 6) hipLaunchKernelGGL((paged_f32_kernel<D, 2, MOD>), grid, block, 0, s, a);
   else hipLaunchKernelGGL((paged_f32_kernel<D, 1, MOD>), grid, block, 0, s, a);

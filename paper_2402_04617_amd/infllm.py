@@ -368,10 +368,13 @@ def infllm_rotate(p, rot, n_tokens, positions, q, q_strides, q_out, q_out_stride
                   first_position=0, stream=None):
     """positions: int64 tensor, or None for first_position + t; strides: (token, head) in elements (of what is None
     they may be None)."""
-    qs, qos, ks, kos = (x or (0, 0) for x in (q_strides, q_out_strides, k_strides, k_out_strides))
+    qt, qh = q_strides or (0, 0)
+    qot, qoh = q_out_strides or (0, 0)
+    kt, kh = k_strides or (0, 0)
+    kot, koh = k_out_strides or (0, 0)
     _check("infllm_rotate", lib().infllm_rotate(
-        ctypes.byref(p), ctypes.byref(rot), n_tokens, _ptr(positions), first_position, _ptr(q), qs[0], qs[1],
-        _ptr(q_out), qos[0], qos[1], _ptr(k), ks[0], ks[1], _ptr(k_out), kos[0], kos[1], _stream(stream)))
+        ctypes.byref(p), ctypes.byref(rot), n_tokens, _ptr(positions), first_position, _ptr(q), qt, qh, _ptr(q_out),
+        qot, qoh, _ptr(k), kt, kh, _ptr(k_out), kot, koh, _stream(stream)))
 
 
 def _seqs(seq_lens, past_lens, page_table, table_stride):
@@ -380,9 +383,11 @@ def _seqs(seq_lens, past_lens, page_table, table_stride):
     if len(lens) != len(pasts):
         raise ValueError("one past length per sequence")
     if table_stride is None:
-        table_stride = 0 if page_table is None else page_table.stride(0)
-        if page_table is not None and page_table.shape[0] < len(lens):
-            raise ValueError(f"page_table needs {len(lens)} rows, got {page_table.shape[0]}")
+        if page_table is None:
+            return lens, pasts, 0
+        if page_table.size(0) < len(lens):
+            raise ValueError(f"page_table needs {len(lens)} rows, got {page_table.size(0)}")
+        table_stride = page_table.stride(0)
     return lens, pasts, table_stride
 
 
