@@ -180,6 +180,343 @@ __device__ __forceinline__ void form_row(const KeyTiles<KT, THREADS, BACK>& keys
   }
 }
 
+// Scores in the base-2 domain.  The scale and the bias are part of the exponential's
+// argument; a capped score becomes its value first.  c tanh(x / c) = c - 2 c / (1 + e^{2 x /
+// c}): its error of some 2^-23 c is far below what rounding P to bf16 does.
+template <int MOD>
+struct Scores {
+  float c2, cap_in, cap2;
+  __device__ __forceinline__ explicit Scores(const PagedArgs& a) : c2(a.sm_scale * 1.4426950408889634f), cap_in(0.f), cap2(0.f) {
+    if constexpr (MOD & kCap) {
+      cap_in = 2.f * c2 / a.softcap;
+      cap2 = a.softcap * 1.4426950408889634f;
+    }
+  }
+  __device__ __forceinline__ float capped(float s) const {
+    return __builtin_fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + fast_exp2(s * cap_in)), cap2);
+  }
+  // The exponent of a score (capped already, if it is to be), b what is to be added.
+  __device__ __forceinline__ float exponent(float s, float b) const { return MOD & kCap ? s + b : __builtin_fmaf(s, c2, b); }
+};
+
+// This wave's LDS accesses before it come before those after it.
+__device__ __forceinline__ void wave_lds_order() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
+// A part of a row tile of at most 16 RB rows (single tokens, a few guessed ones): the waves
+// share the keys instead of the rows.  Wave w takes the 16 keys of every tile that it loads
+// itself, so that the waves run without a barrier, each with its next two tiles' keys and
+// values in flight, and join their shares in LDS at the end.  S^T = K Q^T with
+// v_mfma_f32_16x16x32_bf16: a lane has keys 4 (lane / 16) .. + 3 of row lane % 16, which is
+// the B operand of v_mfma_f32_16x16x16_bf16 as it stands; V^T read transposed.  Bound by
+// memory: one wave of four with all rows of the tile (of 32, four used) took 348 us for 48
+// sequences of up to 20,000 tokens.
+template <int D, int MOD, bool GROUPS, int RB>
+__device__ __forceinline__ void few_rows(const PagedArgs& a, PagedSmem<D>& sm, const PagedWork& w, const PagedRange& range, int g, int i0,
+                                         int i1) {
+  constexpr int CH = D / 8, KSTEPS = D / 32, DBLK = D / 16;
+  constexpr int RPI = 64 / CH, NI = 16 / RPI;
+  constexpr uint32_t kTileBytes = KB * D * 2;
+  typedef KeyTiles<KB, 256, (MOD & kSlopes) != 0> Keys;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c = lane & 15, q4 = lane >> 4;
+  const int G = (int)a.d_group.d, R = G * w.len;
+  const int t_begin = w.part * w.part_tiles, t_end = min(t_begin + w.part_tiles, range.n);
+  const bool one_part = range.n <= w.part_tiles;
+  const int last = w.past + w.len - 1;
+  const Keys keys{range.sink, range.low - range.sink, t_begin, t_end, last, w.table_row, GROUPS ? 3 : 0, t_begin};
+  const PageRow pr = page_row(w.table_row);
+  const char* kbase = (const char*)a.k + g * a.head_stride * 2;
+  const char* vbase = (const char*)a.v + g * a.head_stride * 2;
+
+  // Places of the wave's key groups (keys) of the next 32 (4) tiles, one a lane, and of the
+  // 32 (4) after them, requested a window ahead.
+  constexpr int kPer = GROUPS ? 2 : 16, kWindow = 64 / kPer;
+  auto look_up = [&](int t0) -> uint32_t {
+    const int t = min(t0 + lane / kPer, t_end - 1), first = keys.key_of(t) + 16 * wave;
+    const int key = GROUPS ? min(first + 8 * (lane & 1), last & ~7) : min(first + (lane & 15), last);
+    return pr.place(key);
+  };
+  uint32_t here = look_up(t_begin), ahead = 0;
+  int w0 = t_begin;
+  if (w0 + kWindow < t_end) ahead = look_up(w0 + kWindow);
+
+  const int lrow = 16 * wave + lane / CH;
+  const uint32_t piece0 = (uint32_t)(lane % CH) ^ (uint32_t)swz<D>(lrow);
+  auto piece_of = [&](int j) { return D == 128 ? piece0 ^ (uint32_t)j : piece0; };
+  uint32_t voff[NI];
+#pragma unroll
+  for (int j = 0; j < NI; ++j) voff[j] = 16u * (piece_of(j) + __umul24((uint32_t)(RPI * j + lane / CH) & 7u, a.token16));
+  const uint32_t lds_k0 = (uint32_t)(uintptr_t)(INFLLM_LDS bf16_t*)sm.k[0];
+  const uint32_t lds_v0 = (uint32_t)(uintptr_t)(INFLLM_LDS bf16_t*)sm.v[0];
+  const uint32_t lds_k = lds_k0 + NI * wave * 1024, lds_v = lds_v0 + NI * wave * 1024;
+  // which of the tile's keys are there: a bit for each of the wave's 16
+  auto there_of = [&](uint32_t window, int t) -> uint32_t {
+    const uint64_t ok = __ballot(window != kNoRow) >> (kPer * (t - w0));
+    if constexpr (GROUPS) return ((ok & 1) ? 0xFFu : 0u) | ((ok & 2) ? 0xFF00u : 0u);
+    return (uint32_t)ok & 0xFFFFu;
+  };
+  // Requests the wave's rows of tile t, which the window holds.
+  auto issue = [&](int t) {
+    const uint32_t buf = (uint32_t)((t - t_begin) & 1) * kTileBytes;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the buffer has been read)
+    if constexpr (GROUPS) {
+      uint64_t base[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t p = (uint32_t)__builtin_amdgcn_readlane((int)here, 2 * (t - w0) + i);
+        base[i] = (uint64_t)(p == kNoRow ? 0u : p) << 4;
+      }
+#pragma unroll
+      for (int j = 0; j < NI; ++j) lds_load(lds_k + buf + j * 1024, kbase + base[RPI * j / 8], voff[j]);
+#pragma unroll
+      for (int j = 0; j < NI; ++j) lds_load(lds_v + buf + j * 1024, vbase + base[RPI * j / 8], voff[j]);
+    } else {
+      uint64_t off[NI];
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        const uint32_t p = __shfl(here, 16 * (t - w0) + RPI * j + lane / CH);
+        off[j] = (uint64_t)((p == kNoRow ? 0u : p) + piece_of(j)) * 16;
+      }
+#pragma unroll
+      for (int j = 0; j < NI; ++j) lds_load_lane(lds_k + buf + j * 1024, kbase + off[j]);
+#pragma unroll
+      for (int j = 0; j < NI; ++j) lds_load_lane(lds_v + buf + j * 1024, vbase + off[j]);
+    }
+  };
+  issue(t_begin);
+  uint32_t ok0 = there_of(here, t_begin), ok1 = 0xFFFFu;
+  if (t_begin + 1 < t_end) {
+    issue(t_begin + 1);
+    ok1 = there_of(here, t_begin + 1);
+  }
+
+  bf16x8 qreg[RB][KSTEPS];
+  int pos[RB];
+  float slope[RB], m[RB], neg_m[RB], l[RB];
+  f32x4 o[RB][DBLK];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int row = min(16 * rb + c, R - 1), qi = div_by(row, a.d_group), qh = g * G + row - qi * G;
+    const bf16_t* qp = (const bf16_t*)a.q + (int64_t)(w.start + qi) * a.q_tok + (int64_t)qh * a.q_head + 8 * q4;
+#pragma unroll
+    for (int s = 0; s < KSTEPS; ++s) qreg[rb][s] = *(const bf16x8*)(qp + 32 * s);
+    pos[rb] = w.past + qi;
+    slope[rb] = 0.f;
+    if constexpr (MOD & kSlopes) slope[rb] = a.slopes[qh] * 1.4426950408889634f;
+    m[rb] = -__builtin_inff();
+    neg_m[rb] = l[rb] = 0.f;
+#pragma unroll
+    for (int db = 0; db < DBLK; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const Scores<MOD> score(a);
+  // LDS offsets of the fragments, XOR-related under the swizzle: K, k-step s: ^ 64 s; V^T,
+  // block db: ^ 32 db
+  const int kr = 16 * wave + c, vr = 16 * wave + 4 * q4 + (c >> 2);
+  const uint32_t koff = 2u * D * kr + 16u * (q4 ^ swz<D>(kr));
+  const uint32_t voff0 = 2u * D * vr + 16u * (((lane & 3) >> 1) ^ swz<D>(vr)) + 8u * (lane & 1);
+  int plain0 = a.window > 0 ? (max(0, w.past + i1 - a.window + 1) + KB - 1) / KB : 0;
+  int plain1 = (w.past + i0 + 1) / KB;
+  keys.range(&plain0, &plain1);
+
+  for (int t = t_begin; t < t_end; ++t) {
+    const uint32_t buf = (uint32_t)((t - t_begin) & 1) * kTileBytes;
+    const bool more = t + 1 < t_end;
+    if (more) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * NI) : "memory");  // this tile's keys have landed
+    else asm volatile("s_waitcnt vmcnt(%0)" : : "n"(NI) : "memory");
+    f32x4 s[RB];
+    const uint32_t ka = lds_k0 + buf + koff;
+#pragma unroll
+    for (int k = 0; k < KSTEPS; ++k) {
+      const bf16x8 kf = *(const INFLLM_LDS bf16x8*)(uintptr_t)(ka ^ (64u * k));
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+        s[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qreg[rb][k], k == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb], 0, 0, 0);
+    }
+    const int k0 = keys.key_of(t) + 16 * wave;
+    const bool plain = t >= plain0 && t < plain1 && ok0 == 0xFFFFu;
+    i16x4 p[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      if constexpr (MOD & kCap) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[rb][j] = score.capped(s[rb][j]);
+      }
+      if (!plain) {
+        const uint32_t see = ((uint32_t)seen_keys(pos[rb], k0, a.window, a.n_init) & ok0) >> (4 * q4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[rb][j] = (see >> j) & 1u ? s[rb][j] : -__builtin_inff();
+      }
+      const float bias = MOD & kSlopes ? slope[rb] * (float)(k0 + 4 * q4 - pos[rb]) : 0.f;
+      float e[4], sum;
+      auto weights = [&]() {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) e[j] = fast_exp2(score.exponent(s[rb][j], MOD & kSlopes ? __builtin_fmaf(slope[rb], (float)j, bias) + neg_m[rb] : neg_m[rb]));
+        sum = (e[0] + e[1]) + (e[2] + e[3]);
+      };
+      weights();
+      // the running maximum, raised only where a sum passes 2^16 or nothing has been seen yet
+      if (__ballot(m[rb] == -__builtin_inff() || sum > 65536.f) != 0) {
+        float mx = -__builtin_inff();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) mx = fmaxf(mx, score.exponent(s[rb][j], MOD & kSlopes ? __builtin_fmaf(slope[rb], (float)j, bias) : 0.f));
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(m[rb], fmaxf(mx, __shfl_xor(mx, 32)));
+        const float alpha = mx == -__builtin_inff() ? 1.f : fast_exp2(m[rb] - mx);
+        l[rb] *= alpha;
+#pragma unroll
+        for (int db = 0; db < DBLK; ++db) o[rb][db] *= alpha;
+        m[rb] = mx;
+        neg_m[rb] = mx == -__builtin_inff() ? 0.f : -mx;
+        weights();
+      }
+      l[rb] += sum;
+      bf16x4 pb;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) pb[j] = (__bf16)e[j];  // (by at most 2^-8 of each; the sums take them unrounded)
+      p[rb] = __builtin_bit_cast(i16x4, pb);
+    }
+    if (more) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * NI) : "memory");  // its values
+    else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    const uint32_t va = lds_v0 + buf + voff0;
+    if (GROUPS && k0 + 15 > last) {
+      // rows behind the sequence's end: whatever the page holds meets weights of 0
+      for (int i = max(0, last - k0 + 1) * CH + lane; i < 16 * CH; i += 64)
+        *(INFLLM_LDS u32x4*)(uintptr_t)(lds_v0 + buf + 16 * wave * 2 * D + 16u * i) = u32x4{0, 0, 0, 0};
+      wave_lds_order();
+    }
+#pragma unroll
+    for (int db = 0; db < DBLK; ++db) {
+      const i16x4 vf = __builtin_amdgcn_ds_read_tr16_b64_v4i16((INFLLM_LDS i16x4*)(uintptr_t)(va ^ (32u * db)));
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, p[rb], o[rb][db], 0, 0, 0);
+    }
+    ok0 = ok1;
+    if (t + 2 < t_end) {
+      if (t + 2 >= w0 + kWindow) {
+        here = ahead;
+        w0 += kWindow;
+        if (w0 + kWindow < t_end) ahead = look_up(w0 + kWindow);
+      }
+      issue(t + 2);
+      ok1 = there_of(here, t + 2);
+    }
+  }
+
+  // The waves' shares through LDS: [wave][row] of D values (padded), then maxima and sums.
+  constexpr int kRow = D * 4 + 16, kRows = 16 * RB;
+  static_assert(4 * kRows * (kRow + 8) <= (int)sizeof(sm), "the shares fit");
+  INFLLM_LDS char* share = (INFLLM_LDS char*)(INFLLM_LDS PagedSmem<D>*)&sm;
+  INFLLM_LDS float* stats = (INFLLM_LDS float*)(share + 4 * kRows * kRow);  // [wave][row]{m, l}
+  lds_barrier();  // every wave is done with its tiles (its loads have landed)
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+    for (int db = 0; db < DBLK; ++db)
+      *(INFLLM_LDS f32x4*)(share + (wave * kRows + 16 * rb + c) * kRow + 4 * (16 * db + 4 * q4)) = o[rb][db];
+    float sum = l[rb];
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (q4 == 0) {
+      stats[2 * (wave * kRows + 16 * rb + c)] = m[rb];
+      stats[2 * (wave * kRows + 16 * rb + c) + 1] = sum;
+    }
+  }
+  lds_barrier();
+  constexpr int TPR = D / 8, RPP = 256 / TPR;  // threads of a row, rows at a time
+  const int64_t prow0 = (int64_t)blockIdx.x * a.item_rows;
+#pragma unroll
+  for (int r0 = 0; r0 < kRows; r0 += RPP) {
+    const int r = r0 + tid / TPR, d = 8 * (tid % TPR);
+    if (r0 + (tid & ~63) / TPR >= R) continue;  // (whole waves)
+    const int rc = min(r, kRows - 1);
+    float M = -__builtin_inff(), L = 0.f, acc[8] = {};
+#pragma unroll
+    for (int v = 0; v < 4; ++v) M = fmaxf(M, stats[2 * (v * kRows + rc)]);
+    const float base = M == -__builtin_inff() ? 0.f : M;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const float mv = stats[2 * (v * kRows + rc)], lv = stats[2 * (v * kRows + rc) + 1];
+      const float f = mv == -__builtin_inff() ? 0.f : fast_exp2(mv - base);
+      const bool live = mv != -__builtin_inff() || lv != lv;
+      L += live ? lv * (lv != lv ? 1.f : f) : 0.f;
+      const INFLLM_LDS f32x4* x = (const INFLLM_LDS f32x4*)(share + (v * kRows + rc) * kRow + 4 * d);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += live ? f * x[e >> 2][e & 3] : 0.f;
+    }
+    const bool row_ok = r < R && r < kRows;
+    const int i = div_by(min(r, R - 1), a.d_group), h = g * G + min(r, R - 1) - i * G;
+    float inv = L > 0.f ? 1.f / L : 0.f;
+    float lse_v = L > 0.f ? (M + __log2f(L)) * 0.6931471805599453f : -__builtin_inff();
+    if (L != L) {  // a NaN among the row's scores is the row's, through the merge as well
+      inv = L;
+      lse_v = one_part ? L : __builtin_inff();
+    }
+    float z = 0.f, amax = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      z = __builtin_fmaf(acc[e], 0.f, z);
+      acc[e] *= inv;
+      amax = fmaxf(amax, fabsf(acc[e]));
+    }
+#pragma unroll
+    for (int x = 1; x < TPR; x <<= 1) {
+      z += __shfl_xor(z, x);
+      amax = fmaxf(amax, __shfl_xor(amax, x));
+    }
+    // A row that a masked value which is not finite has reached (0 times it) is formed again
+    // by the wave from the keys that it sees.
+    const bool apart = row_ok && !(z == 0.f) && L == L;
+    uint64_t odd = __ballot(apart && tid % TPR == 0);
+    const int ex = one_part ? 0 : partial_row_exponent(amax);
+    if (row_ok && !apart) {
+      const float sc = exp2_int(-ex);
+      u32x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        x[e] = one_part ? (uint32_t)f32_to_bf16(acc[2 * e]) | ((uint32_t)f32_to_bf16(acc[2 * e + 1]) << 16)
+                        : pack_f16x2(acc[2 * e] * sc, acc[2 * e + 1] * sc);
+      if (!one_part) *(u32x4*)((char*)a.part_o + (prow0 + r) * (D * 2) + 2 * d) = x;
+      else *(u32x4*)((bf16_t*)a.out + (int64_t)(w.start + i) * a.out_tok + (int64_t)h * a.out_head + d) = x;
+      if (d == 0 && !one_part) a.part_exp[prow0 + r] = ex;
+    }
+    if (row_ok && d == 0) {
+      if (!one_part) a.part_lse[prow0 + r] = lse_v;
+      else if (a.lse != nullptr) a.lse[h * a.lse_stride + w.start + i] = lse_v;
+    }
+    for (; odd != 0; odd &= odd - 1) {
+      const int src = __builtin_ctzll(odd), rr = __shfl(r, src), p_r = w.past + __shfl(i, src);
+      const float nm = -__shfl(base, src), inv_r = __shfl(inv, src);
+      const int hr = __shfl(h, src);
+      const bf16_t* qp = (const bf16_t*)a.q + (int64_t)(p_r - w.past + w.start) * a.q_tok + (int64_t)hr * a.q_head;
+      float slope_r = 0.f;
+      if constexpr (MOD & kSlopes) slope_r = a.slopes[hr] * 1.4426950408889634f;
+      constexpr int DPL = D / 64;
+      float again[DPL], top = 0.f;
+      form_row<bf16_t, D>(keys, kbase, vbase, qp, p_r, a.window, a.n_init, [&](float x, int key) {
+        return fast_exp2(score.exponent(MOD & kCap ? score.capped(x) : x, slope_r * (float)(key - p_r) + nm));
+      }, again);
+#pragma unroll
+      for (int e = 0; e < DPL; ++e) {
+        again[e] *= inv_r;
+        const float x = fabsf(again[e]);
+        top = x < __builtin_inff() ? fmaxf(top, x) : top;  // (of the finite ones, which keep their precision)
+      }
+      const int ex_r = one_part ? 0 : partial_row_exponent(wave_max(top));
+      uint16_t* to = one_part ? (uint16_t*)a.out + (int64_t)(p_r - w.past + w.start) * a.out_tok + (int64_t)hr * a.out_head
+                              : (uint16_t*)a.part_o + (prow0 + rr) * D;
+#pragma unroll
+      for (int e = 0; e < DPL; ++e)
+        to[DPL * lane + e] = one_part ? f32_to_bf16(again[e]) : (uint16_t)(pack_f16x2(again[e] * exp2_int(-ex_r), 0.f) & 0xFFFFu);
+      if (!one_part && lane == 0) a.part_exp[prow0 + rr] = ex_r;
+    }
+  }
+}
+
 // GROUPS: pages of a multiple of 8 tokens.  The rows of a load instruction then lie in one
 // group of 8 keys, whose place is uniform: its base goes through scalar registers, and a
 // lane's offset from it is the same for every tile.  (With an address formed by every lane
@@ -208,6 +545,14 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   const PagedRange range = paged_range(a, w.past, i0, i1);
   const int t_begin = w.part * w.part_tiles, t_end = min(t_begin + w.part_tiles, range.n);
   if (t_begin >= t_end) return;  // (the parts of a sequence are as many for each of its row tiles)
+  if (R <= 16) {
+    few_rows<D, MOD, GROUPS, 1>(a, sm, w, range, g, i0, i1);
+    return;
+  }
+  if (R <= 32) {
+    few_rows<D, MOD, GROUPS, 2>(a, sm, w, range, g, i0, i1);
+    return;
+  }
   const bool one_part = range.n <= w.part_tiles;
   const int last = w.past + w.len - 1;
   KeyTiles<KB, 256, (MOD & kSlopes) != 0> keys{range.sink, range.low - range.sink, t_begin, t_end, last, w.table_row, GROUPS ? 3 : 0, t_begin};
@@ -343,20 +688,10 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     for (int j = 0; j < 16; ++j) oacc[db][j] = 0.f;
   float m_run = -__builtin_inff(), neg_m = 0.f, l_run = 0.f;
 
-  // Scores in the base-2 domain.  The scale and the bias are part of the exponential's
-  // argument; a capped score becomes its value first.  c tanh(x / c) = c - 2 c / (1 + e^{2 x /
-  // c}): its error of some 2^-23 c is far below what rounding P to bf16 does.  With a bias
-  // the tiles are taken from the diagonal backwards, where it falls (forwards, the maximum
-  // of a steep one grew with every tile).
-  const float log2e = 1.4426950408889634f, c2 = a.sm_scale * log2e;
-  float cap_in = 0.f, cap2 = 0.f;
-  if constexpr (MOD & kCap) {
-    cap_in = 2.f * c2 / a.softcap;
-    cap2 = a.softcap * log2e;
-  }
-  auto capped = [&](float s) {
-    return __builtin_fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + fast_exp2(s * cap_in)), cap2);
-  };
+  // With a bias the tiles are taken from the diagonal backwards, where it falls (forwards,
+  // the maximum of a steep one grew with every tile).
+  const Scores<MOD> score(a);
+  const float c2 = score.c2;
   // Key place c of a tile (element e = 16 kb + j of a lane: 32 kb + 8 (j / 4) + j % 4, its
   // half's 4 gsel aside).
   auto place_of = [](int e) { return 32 * (e >> 4) + 8 * ((e & 15) >> 2) + (e & 3); };
@@ -365,7 +700,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   // The exponent of element e of a tile, b its bias_of plus what is to be added.
   auto exponent = [&](float s, int e, float b) {
     if constexpr (MOD & kSlopes) b = __builtin_fmaf(slope, (float)place_of(e), b);
-    return MOD & kCap ? s + b : __builtin_fmaf(s, c2, b);
+    return score.exponent(s, b);
   };
   // What a row sees of a tile: a bit for each key of this lane's half from its first on.
   struct Lims {
@@ -389,7 +724,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     for (int e = 8 * i; e < 8 * i + 8; ++e) {
       const int c = place_of(e);
       float z = s[e >> 4][e & 15];
-      if constexpr (MOD & kCap) z = capped(z);
+      if constexpr (MOD & kCap) z = score.capped(z);
       if (masked) {
         const uint32_t see = (uint32_t)((int32_t)(l.vis[e >> 4] << (31 - (c & 31))) >> 31);  // all ones or none
         z = __uint_as_float((__float_as_uint(z) & see) | (0xFF800000u & ~see));
@@ -689,11 +1024,6 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
       *(INFLLM_LDS u32x2*)(stage + n_e * kStageRow + (32 * db + 8 * jq + 4 * (lane_e >> 5)) * 2) = x;
     }
   }
-  auto lds_order = []() {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
-  };
   // Values that are not finite must not reach rows that do not see their key: in a masked
   // tile such a value meets P = 0 and leaves a NaN.  A row that came out so is formed again
   // by the wave from the keys it sees, 64 at a time, against its maximum.
@@ -707,7 +1037,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     const uint64_t odd = __ballot(row_ok && !(z == 0.f) && l_tot == l_tot);
     uint32_t rows = (uint32_t)odd | (uint32_t)(odd >> 32);
     if (__builtin_expect(rows != 0, 0)) {
-      lds_order();
+      wave_lds_order();
       constexpr int DPL = D / 64;
       for (; rows != 0; rows &= rows - 1) {
         const int r = __builtin_ctz(rows);
@@ -716,7 +1046,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
         float acc[DPL];
         form_row<bf16_t, D>(keys, kbase, vbase, (const bf16_t*)late.q + (int64_t)(w.start + i) * late.q_tok + (int64_t)h * late.q_head,
                             p_r, a.window, a.n_init,
-                            [&](float s, int key) { return fast_exp2((MOD & kCap ? capped(s) : s * c2) + slope_r * (float)(key - p_r) + nm); }, acc);
+                            [&](float s, int key) { return fast_exp2(score.exponent(MOD & kCap ? score.capped(s) : s, slope_r * (float)(key - p_r) + nm)); }, acc);
         float amax = 0.f;  // (of the finite ones, which keep their precision)
 #pragma unroll
         for (int e = 0; e < DPL; ++e) {
@@ -745,7 +1075,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
       late.lse[h * late.lse_stride + w.start + i] = lse_v;
     }
   }
-  lds_order();
+  wave_lds_order();
   {
     constexpr int NS = 32 * CH / 64;  // pieces of a lane
     const int r0 = lane_e / CH, ch = lane_e % CH;
