@@ -7,6 +7,8 @@
 // keeps to one token: each lane forms the sine and cosine of one pair (in float64, reduced
 // to half a revolution there; the function's own cost is one lane's), which all rows of
 // the token then share.  In float32, rounded once.
+#include <type_traits>
+
 #include "paged.h"
 
 namespace infllm {
@@ -51,6 +53,29 @@ __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
+// Sum over the LPR lanes of a row: rotations within 16 lanes, by the lane crossbar beyond.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float x) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), CTRL, 0xF, 0xF, false));
+}
+constexpr int kRor8 = 0x128, kRor4 = 0x124, kRor2 = 0x122, kRor1 = 0x121;     // within 16 lanes
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141;                // within 4, within 8
+template <int LPR>
+__device__ __forceinline__ float row_sum(float x) {
+  if constexpr (LPR == 8) {
+    x += dpp<kXor1>(x);
+    x += dpp<kXor2>(x);
+    x += dpp<kHalfMirror>(x);
+  } else {
+    x += dpp<kRor8>(x);
+    x += dpp<kRor4>(x);
+    x += dpp<kRor2>(x);
+    x += dpp<kRor1>(x);
+    if constexpr (LPR == 32) x += __shfl_xor(x, 16);
+  }
+  return x;
 }
 
 template <typename T, int D, bool PAGED>
@@ -103,81 +128,92 @@ __global__ void __launch_bounds__(64 * kRotWaves) rotate_kernel(RotateArgs a) {
     s[e] = first ? -cs.y : cs.y;
     mate[e] = first ? d + half : d - half;
   }
-  const bool whole = a.rotary_dim == D;              // every dim turns
-  const bool by_piece = half % N == 0;               // a piece's partners are a piece
+  const bool whole = a.rotary_dim == D;                  // every dim turns
+  const bool by_lane = LPR == 16 && whole;               // partners 8 lanes apart
+  const bool by_piece = half % N == 0;                   // a piece's partners are a piece
   const bool exchange = a.rotary_dim > 0 && !a.interleaved;
-  float* const my_row = rows[wave][lane / LPR];
+  const int sub = lane / LPR;                            // this lane's row of a group
+  float* const my_row = rows[wave][sub];
 
-  for (int r0 = r_begin; r0 < r_end; r0 += kRotAhead * RPP) {
-    u32x4 raw[kRotAhead];
+  // Rows [first, end) of one kind: their values as they are (TURN false), or normed and
+  // turned.  A lane's addresses are stepped by uniform strides.
+  auto phase = [&](auto turn, int first, int end, const T* src, int64_t head, T* dst, int64_t out_head, const void* weight) {
+    constexpr bool TURN = decltype(turn)::value;
+    if (first >= end) return;
+    float wf[N];
+    if constexpr (TURN) {
 #pragma unroll
-    for (int j = 0; j < kRotAhead; ++j) {
-      const int r = r0 + j * RPP + lane / LPR;
-      if (r >= r_end) continue;
-      const T* from = r < a.n_q             ? (const T*)a.q + t * a.q_tok + r * a.q_head
-                      : r < a.n_q + a.n_k ? (const T*)a.k + t * a.kv_tok + (r - a.n_q) * a.kv_head
-                                          : (const T*)a.v + t * a.kv_tok + (r - a.n_q - a.n_k) * a.kv_head;
-      raw[j] = *(const u32x4*)(from + d0);
+      for (int e = 0; e < N; ++e) wf[e] = 1.f;
+      if (a.norm && weight != nullptr) Piece<T>::unpack(*(const u32x4*)((const T*)weight + d0), wf);
     }
+    const T* from = src + (first + sub) * head + d0;
+    T* to = dst + (first + sub) * out_head + d0;
+    const int64_t step = RPP * head, out_step = RPP * out_head;
+    for (int r0 = first; r0 < end; r0 += kRotAhead * RPP) {
+      u32x4 raw[kRotAhead];
 #pragma unroll
-    for (int j = 0; j < kRotAhead; ++j) {
-      if (r0 + j * RPP >= r_end) break;  // (uniform)
-      const int r = r0 + j * RPP + lane / LPR;
-      const bool is_q = r < a.n_q, is_v = r >= a.n_q + a.n_k;
-      float x[N];
-      Piece<T>::unpack(raw[j], x);
-      if (a.norm) {
-        float ss = 0.f;
+      for (int j = 0; j < kRotAhead; ++j) {
+        if (r0 + j * RPP + sub < end) raw[j] = *(const u32x4*)from;
+        from += step;
+      }
 #pragma unroll
-        for (int e = 0; e < N; ++e) ss = __builtin_fmaf(x[e], x[e], ss);
+      for (int j = 0; j < kRotAhead; ++j) {
+        if (r0 + j * RPP >= end) break;  // (uniform)
+        u32x4 w = raw[j];
+        if constexpr (TURN) {
+          float x[N], y[N];
+          Piece<T>::unpack(raw[j], x);
+          if (a.norm) {
+            float ss = 0.f;
 #pragma unroll
-        for (int o = 1; o < LPR; o <<= 1) ss += __shfl_xor(ss, o);
-        const float scale = 1.f / sqrtf(ss * (1.f / D) + a.eps);
-        const T* w = (const T*)(is_q ? a.q_weight : a.k_weight);
-        float wf[N];
-        if (w != nullptr) {
-          Piece<T>::unpack(*(const u32x4*)(w + d0), wf);
+            for (int e = 0; e < N; ++e) ss = __builtin_fmaf(x[e], x[e], ss);
+            const float scale = rsqrtf(__builtin_fmaf(row_sum<LPR>(ss), 1.f / D, a.eps));
 #pragma unroll
-          for (int e = 0; e < N; ++e) x[e] = x[e] * scale * wf[e];
-        } else {
+            for (int e = 0; e < N; ++e) x[e] = x[e] * scale * wf[e];
+          }
+          if (exchange && by_lane) {
 #pragma unroll
-          for (int e = 0; e < N; ++e) x[e] *= scale;
+            for (int e = 0; e < N; ++e) y[e] = x[e] * c[e] + dpp<kRor8>(x[e]) * s[e];
+          } else if (exchange) {
+            wave_lds_order();  // (the group before has been read)
+#pragma unroll
+            for (int e = 0; e < N; e += 4) *(f32x4*)(my_row + d0 + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+            wave_lds_order();
+            float m[N];
+            if (by_piece) {
+              const int at = d0 < a.rotary_dim ? mate[0] : d0;
+#pragma unroll
+              for (int e = 0; e < N; e += 4) *(f32x4*)(m + e) = *(const f32x4*)(my_row + at + e);
+            } else {
+#pragma unroll
+              for (int e = 0; e < N; ++e) m[e] = my_row[d0 + e < a.rotary_dim ? mate[e] : d0 + e];
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] = x[e] * c[e] + m[e] * s[e];
+          } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] = x[e] * c[e] + x[e ^ 1] * s[e];
+          }
+          if (!whole) {  // (an infinity times 0 is not the value as it was)
+#pragma unroll
+            for (int e = 0; e < N; ++e) y[e] = d0 + e < a.rotary_dim ? y[e] : x[e];
+          }
+          w = Piece<T>::pack(y);
         }
+        if (r0 + j * RPP + sub < end) *(u32x4*)to = w;
+        to += out_step;
       }
-      float y[N];
-      if (exchange) {
-        wave_lds_order();  // (the group before has been read)
-#pragma unroll
-        for (int e = 0; e < N; e += 4) *(f32x4*)(my_row + d0 + e) = f32x4{x[e], x[e + 1], x[e + 2], x[e + 3]};
-        wave_lds_order();
-        float m[N];
-        if (by_piece) {
-          const int at = d0 < a.rotary_dim ? mate[0] : d0;
-#pragma unroll
-          for (int e = 0; e < N; e += 4) *(f32x4*)(m + e) = *(const f32x4*)(my_row + at + e);
-        } else {
-#pragma unroll
-          for (int e = 0; e < N; ++e) m[e] = my_row[d0 + e < a.rotary_dim ? mate[e] : d0 + e];
-        }
-#pragma unroll
-        for (int e = 0; e < N; ++e) y[e] = x[e] * c[e] + m[e] * s[e];
-      } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) y[e] = x[e] * c[e] + x[e ^ 1] * s[e];
-      }
-      if (!whole) {  // (an infinity times 0 is not the value as it was)
-#pragma unroll
-        for (int e = 0; e < N; ++e) y[e] = d0 + e < a.rotary_dim ? y[e] : x[e];
-      }
-      if (r >= r_end || (!is_q && !there)) continue;
-      T* to;
-      if (is_q) to = (T*)a.q_out + t * a.qo_tok + r * a.qo_head;
-      else if constexpr (PAGED)
-        to = (T*)(is_v ? a.v_out : a.k_out) + page * a.page_stride + slot * a.ko_tok + (r - a.n_q - (is_v ? a.n_k : 0)) * a.ko_head;
-      else to = (T*)a.k_out + t * a.ko_tok + (r - a.n_q) * a.ko_head;
-      *(u32x4*)(to + d0) = is_v ? raw[j] : Piece<T>::pack(y);
     }
-  }
+  };
+  phase(std::true_type{}, r_begin, min(r_end, a.n_q), (const T*)a.q + t * a.q_tok, a.q_head, (T*)a.q_out + t * a.qo_tok, a.qo_head,
+        a.q_weight);
+  if (!there) return;
+  const int64_t out = PAGED ? page * a.page_stride + slot * a.ko_tok : t * a.ko_tok;
+  phase(std::true_type{}, max(0, r_begin - a.n_q), min(r_end - a.n_q, a.n_k), (const T*)a.k + t * a.kv_tok, a.kv_head, (T*)a.k_out + out,
+        a.ko_head, a.k_weight);
+  if constexpr (PAGED)
+    phase(std::false_type{}, max(0, r_begin - a.n_q - a.n_k), r_end - a.n_q - a.n_k, (const T*)a.v + t * a.kv_tok, a.kv_head,
+          (T*)a.v_out + out, a.ko_head, nullptr);
 }
 
 template <typename T, int D>
