@@ -550,8 +550,8 @@ infllm_status infllm_paged_append(const infllm_params* p, const infllm_rotary* r
  *   softcap > 0:  z <- softcap * tanh(z / softcap)
  *   slopes:       z <- z - slopes[h] * (p - t)   (DEVICE float32 [Hq], any finite values)
  *   window > 0:   seen only where t > p - window or t < n_init
- * (with a window of l_L and n_init = l_I this is the step's attention without looked-up
- * units).  NULL in place of the struct, or zeros, change nothing. */
+ * (for one token, window = l_L + 1 and n_init = l_I: what a step sees over units of one
+ * token of which none is looked up).  NULL in place of the struct, or zeros, change nothing. */
 typedef struct {
   float softcap;
   int32_t window;

@@ -87,6 +87,11 @@ CASES = [
     ("bf16", 7, 7, 64, 8, "heads", *STEPS),
     ("bf16", 4, 1, 128, 64, "heads", (700,), (333,)),
     ("bf16", 2, 1, 64, 128, "tokens", (300, 300), (0, 4000)),
+    ("bf16", 8, 2, 128, 16, "heads", (8,) * 4, (0, 57, 900, 2011)),   # 32 rows of a kv head
+    ("bf16", 9, 1, 64, 50, "tokens", (3, 2, 1, 4), (61, 640, 0, 1500)),
+    ("bf16", 4, 1, 128, 1, "heads", (7, 4, 1), (1, 333, 4000)),
+    ("bf16", 17, 1, 128, 32, "heads", (1, 1, 2), (5, 1029, 700)),
+    ("bf16", 33, 1, 64, 8, "apart", (1, 1), (63, 470)),
     ("f32", 4, 1, 128, 16, "heads", (1,), (0,)),
     ("f32", 4, 2, 64, 24, "tokens", *MIXED),
     ("f32", 8, 2, 128, 64, "apart", *STEPS),
@@ -125,6 +130,13 @@ FORMS = [
 def test_score_forms(form, dtype, Hq, Hkv, D, page, order):
     news, pasts = (1, 70, 1, 0, 129, 1), (900, 333, 0, 9, 1100, 64)
     r = Run(news, pasts, Hq, Hkv, D, page, dtype, order, form=form, q_scale=2.0)
+    r.verify(*r.call())
+
+
+@pytest.mark.parametrize("form", FORMS, ids=lambda f: " ".join(f"{k}={v}" for k, v in f.items()))
+def test_score_forms_of_few_rows(form):
+    """Rows that share the keys between the waves: 4 to 32 of a kv head."""
+    r = Run((1, 8, 5, 1), (1300, 700, 131, 0), 8, 2, 128, 16, "bf16", form=form, q_scale=2.0)
     r.verify(*r.call())
 
 
@@ -192,6 +204,28 @@ def test_values_that_are_not_finite_stay_with_the_rows_that_see_them(dtype, D, f
     for j in range(40):
         if clean.visible(0)[j, 91]:
             assert torch.isnan(out[j, 2:]).all() and torch.isnan(lse[2:, j]).all()
+
+
+@pytest.mark.parametrize("form", [None, dict(window=70, n_init=3), dict(softcap=4.0, slopes=True)], ids=str)
+@pytest.mark.parametrize("page", [16, 50])
+def test_values_that_are_not_finite_with_few_rows(form, page):
+    """Two current tokens of four heads: an infinite value and a NaN key that only the second sees, and values that the
+    window hides from both; split and whole."""
+    for past in (100, 6000):
+        clean, odd = (Run((2, 1), (past, 40), 4, 1, 128, page, "bf16", form=form) for _ in range(2))
+        at = [(past + 1, "values", math.inf), (past - 80, "values", math.nan)] if form and "window" in form else [(past + 1, "values", math.inf)]
+        for t, what, x in at:
+            odd.c.v[int(odd.c.host_table[0, t // page]), 0, t % page, 3] = x
+        out, lse = odd.call()
+        want, want_lse = clean.call()
+        assert torch.equal(lse, want_lse)
+        assert torch.isfinite(out[0]).all() and (out[0].double() - want[0].double()).abs().max() <= 2e-2
+        assert torch.all(out[1, :, 3] == math.inf) and torch.isfinite(out[1, :, :3]).all() and torch.isfinite(out[1, :, 4:]).all()
+        assert torch.equal(out[2], want[2])
+        odd.c.k[int(odd.c.host_table[0, (past + 1) // page]), 0, (past + 1) % page, 5] = math.nan
+        out, lse = odd.call()
+        assert torch.isfinite(out[0]).all() and torch.isnan(out[1]).all() and torch.isnan(lse[:, 1]).all()
+        assert torch.equal(out[2], want[2]) and torch.equal(lse[:, 0], want_lse[:, 0])
 
 
 def test_low_and_high_scores():
