@@ -504,7 +504,8 @@ infllm_status infllm_rope_frequencies(int32_t rotary_dim, double base, int32_t s
  * head h starts at t * token_stride + h * head_stride elements, as in
  * infllm_prompt_attend; outputs may be the inputs (same pointer and strides) and must not
  * overlap them otherwise.  positions: DEVICE int64 [n_tokens] (any sign), or NULL for
- * first_position + t.  q and q_out may both be NULL, and so may k and k_out. */
+ * first_position + t.  q and q_out may both be NULL, and so may k and k_out.
+ * E_UNSUPPORTED for 2^26 - 8192 tokens and more (here and in infllm_paged_append). */
 infllm_status infllm_rotate(const infllm_params* p, const infllm_rotary* rot, int32_t n_tokens,
                             const int64_t* positions, int64_t first_position, const void* q, int64_t q_token_stride,
                             int64_t q_head_stride, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
@@ -569,7 +570,7 @@ size_t infllm_paged_workspace_bytes(const infllm_params* p, const infllm_pages* 
  * at position past_lens[i] + j, and head h (kv head h / G) takes one softmax over the
  * tokens t <= past_lens[i] + j that `score` lets it see.  Single tokens (a decoding
  * batch), chunks of prompts and both together are one call: one launch and, where keys
- * are split, a merge (more than 256 sequences: for every 256).
+ * are split, a merge (more than 192 sequences: for every 192).
  *  q, out: packed rows with token and head strides as in infllm_prompt_attend; lse:
  *     optional [Hq][total] float32, total the sum of seq_lens.
  * A query that sees nothing (its pages not followed) gets zeros and lse -inf.

@@ -120,8 +120,9 @@ void set_rotary(const infllm_params* p, const infllm_rotary* r, RotateArgs* a) {
   a->k_weight = r->k_weight;
 }
 
-// Whether a rotation's launch, at most a wave per row of a token, stays within 2^31 waves.
-bool rotate_fits(int64_t tokens, int64_t rows) { return (__int128)tokens * rows < INT32_MAX / 64; }
+// Whether a rotation's launch (a wave per token, more only where tokens are few) stays within
+// 2^32 threads.
+bool rotate_fits(int64_t tokens) { return tokens < (1 << 26) - 8192; }
 
 // Microseconds of a workgroup of the attention, for each tile of keys and beside them: with
 // the whole chip at work, and of one that runs nearly alone.  Row tiles of few rows read
@@ -135,8 +136,8 @@ struct ItemCost {
 ItemCost item_cost(const PagedArgs& a, bool thin) {
   const bool wide = a.head_dim == 128;
   if (a.bf16) {
-    if (thin) return wide ? ItemCost{2.5f, 3.6f, 0.89f, 4.f} : ItemCost{1.f, 3.6f, 0.59f, 4.f};
-    return wide ? ItemCost{1.16f, 7.f, 0.92f, 7.f} : ItemCost{0.53f, 7.f, 0.4f, 7.f};
+    if (thin) return wide ? ItemCost{2.25f, 2.7f, 0.79f, 3.5f} : ItemCost{1.2f, 2.7f, 0.7f, 3.5f};
+    return wide ? ItemCost{1.5f, 4.8f, 0.9f, 8.8f} : ItemCost{0.62f, 4.8f, 0.49f, 8.8f};
   }
   if (thin) return wide ? ItemCost{6.f, 5.f, 5.3f, 4.3f} : ItemCost{5.5f, 5.f, 2.7f, 4.3f};
   return wide ? ItemCost{5.5f, 6.4f, 5.2f, 3.7f} : ItemCost{7.5f, 6.4f, 2.5f, 3.7f};
@@ -146,7 +147,7 @@ ItemCost item_cost(const PagedArgs& a, bool thin) {
 struct MergeCost {
   float launch, item, byte, part;
 };
-MergeCost merge_cost(const PagedArgs& a) { return a.bf16 ? MergeCost{5.3f, 2.5e-3f, 4e-7f, 0.115f} : MergeCost{3.4f, 0.f, 4.2e-7f, 0.1f}; }
+MergeCost merge_cost(const PagedArgs& a) { return a.bf16 ? MergeCost{4.7f, 3.1e-3f, 2.9e-7f, 0.18f} : MergeCost{3.4f, 0.f, 4.2e-7f, 0.1f}; }
 // Workgroups that run at a time: by their LDS (bf16 two to a compute unit), float32 by
 // their registers too.
 int resident_wgs(const PagedArgs& a) {
@@ -208,7 +209,9 @@ bool plan(const infllm_params* p, int32_t n_seqs, const int32_t* lens, const int
   constexpr int kBins = 32;  // of item lengths
   float best = -1.f;
   int best_T = most;
-  for (int T = most, c = 1; c <= kMostParts; c = std::max(c + 1, c * 4 / 3)) {
+  // (fewer lengths are looked at for many sequences, whose parts balance anyway: 192 of them
+  // took the host 41 us)
+  for (int T = most, c = 1; c <= kMostParts; c = std::max(c + 1, n > 48 ? c * 7 / 4 : c * 4 / 3)) {
     if (c > 1) {
       const int next = (most + c - 1) / c;
       if (next == T) {
@@ -221,13 +224,13 @@ bool plan(const infllm_params* p, int32_t n_seqs, const int32_t* lens, const int
       int64_t n;
       float time, work, lone;  // sums
     } bins[kBins] = {};
-    float alone = 0.f, bytes = 0.f;
+    float longest = 0.f, longest_alone = 0.f, bytes = 0.f;
     int turns = 0;
-    const float top = (float)T * std::max(thin.tile, thick.tile) + std::max(thin.item, thick.item);
+    const float per_T = 1.f / (float)T, top = (float)T * std::max(thin.tile, thick.tile) + std::max(thin.item, thick.item);
     int64_t items = 0;
     for (int j = 0; j < n; ++j) {
       const ItemCost& cost = rows[j] <= 32 ? thin : thick;
-      const int parts = (keys[j] + T - 1) / T, length = (keys[j] + parts - 1) / parts;
+      const int parts = (int)((float)keys[j] * per_T + 0.9985f), length = (int)((float)keys[j] / (float)parts + 0.9985f);
       const float time = (float)length * cost.tile + cost.item, lone = (float)length * cost.lone_tile + cost.lone_item;
       const int64_t count = (int64_t)tiles[j] * parts * Hkv;
       if (parts > 1) {
@@ -239,7 +242,10 @@ bool plan(const infllm_params* p, int32_t n_seqs, const int32_t* lens, const int
       b.time += (float)count * time;
       b.work += (float)count * ((float)length * cost.tile * seen[j] + cost.item);
       b.lone += (float)count * lone / time;
-      alone = std::max(alone, lone);
+      if (time > longest) {
+        longest = time;
+        longest_alone = lone;
+      }
       items += count;
     }
     float t = 0.f;
@@ -257,6 +263,7 @@ bool plan(const infllm_params* p, int32_t n_seqs, const int32_t* lens, const int
       whole -= take;
       if (b.n > 0) break;
     }
+    const float full = t;  // for as long the chip is full
     int64_t left = items - items / slots * slots;
     float done = 0.f;
     for (int y = 0; y < kBins && left > 0; ++y) {
@@ -267,7 +274,8 @@ bool plan(const infllm_params* p, int32_t n_seqs, const int32_t* lens, const int
       done = std::max(done, time);
       left -= b.n;
     }
-    t = std::max(t, alone);
+    // (the longest runs alone from where the others leave off)
+    t = std::max(t, longest_alone + std::min(full, longest) * (1.f - longest_alone / longest));
     if (bytes > 0.f)
       t += merge.launch + (float)items * merge.item + bytes * (float)(a->head_dim * (a->bf16 ? 2 : 4) + 8) * merge.byte +
            (float)turns * merge.part;
@@ -335,9 +343,10 @@ void set_shape(const infllm_params* p, const infllm_pages* pages, const infllm_s
   a->d_page = fast_div(pages->page_size);
 }
 
-infllm_status check_score(const infllm_score_form* s) {
+infllm_status check_score(const infllm_params* p, const infllm_score_form* s) {
   if (s == nullptr) return INFLLM_OK;
   if (!std::isfinite(s->softcap) || s->softcap < 0.f || s->window < 0 || s->n_init < 0) return INFLLM_E_SHAPE;
+  if (s->softcap > 0.f && !std::isfinite(4.f * p->sm_scale / s->softcap)) return INFLLM_E_SHAPE;  // (the kernels form it)
   return (reinterpret_cast<uintptr_t>(s->slopes) & 3u) == 0 ? INFLLM_OK : INFLLM_E_SHAPE;
 }
 
@@ -397,7 +406,7 @@ infllm_status infllm_rotate(const infllm_params* p, const infllm_rotary* rot, in
       return INFLLM_E_UNSUPPORTED;
   }
   const int n_q = q != nullptr ? p->n_q_heads : 0, n_k = k != nullptr ? p->n_kv_heads : 0;
-  if (!rotate_fits(n_tokens, (int64_t)n_q + n_k)) return INFLLM_E_UNSUPPORTED;
+  if (!rotate_fits(n_tokens)) return INFLLM_E_UNSUPPORTED;
   if ((st = check_device()) != INFLLM_OK) return st;
   RotateArgs a;
   std::memset(&a, 0, sizeof(a));
@@ -450,7 +459,7 @@ infllm_status infllm_paged_append(const infllm_params* p, const infllm_rotary* r
       return INFLLM_E_UNSUPPORTED;
   }
   const int n_q = q != nullptr ? p->n_q_heads : 0;
-  if (!rotate_fits(total, (int64_t)n_q + 2 * (int64_t)p->n_kv_heads)) return INFLLM_E_UNSUPPORTED;
+  if (!rotate_fits(total)) return INFLLM_E_UNSUPPORTED;
   if ((st = check_device()) != INFLLM_OK) return st;
   RotateArgs a;
   std::memset(&a, 0, sizeof(a));
@@ -487,7 +496,7 @@ infllm_status infllm_paged_append(const infllm_params* p, const infllm_rotary* r
 size_t infllm_paged_workspace_bytes(const infllm_params* p, const infllm_pages* pages, int32_t n_seqs,
                                     const int32_t* seq_lens, const int64_t* past_lens, const infllm_score_form* score) {
   int64_t total;
-  if (check_params(p) != INFLLM_OK || check_pages(p, pages) != INFLLM_OK || check_score(score) != INFLLM_OK ||
+  if (check_params(p) != INFLLM_OK || check_pages(p, pages) != INFLLM_OK || check_score(p, score) != INFLLM_OK ||
       check_seqs(pages, n_seqs, seq_lens, past_lens, INT32_MAX, &total) != INFLLM_OK || !numbers_fit(p, total))
     return 0;
   PagedArgs a;
@@ -512,7 +521,7 @@ infllm_status infllm_paged_attend(const infllm_params* p, const infllm_pages* pa
   if ((st = check_params(p)) != INFLLM_OK) return st;
   if (remap(p)) return INFLLM_E_UNSUPPORTED;
   if ((st = check_pages(p, pages)) != INFLLM_OK) return st;
-  if ((st = check_score(score)) != INFLLM_OK) return st;
+  if ((st = check_score(p, score)) != INFLLM_OK) return st;
   int64_t total;
   if ((st = check_seqs(pages, n_seqs, seq_lens, past_lens, table_stride, &total)) != INFLLM_OK) return st;
   if (total == 0) return INFLLM_OK;

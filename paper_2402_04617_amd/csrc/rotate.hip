@@ -15,7 +15,7 @@ namespace infllm {
 namespace {
 
 constexpr int kRotWaves = 4;
-constexpr int kRotAhead = 4;  // row groups whose loads are in flight
+constexpr int kRotAhead = 8;  // row groups whose loads are in flight
 
 template <typename T> struct Piece;
 template <> struct Piece<bf16_t> {

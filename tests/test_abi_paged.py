@@ -72,7 +72,7 @@ def test_rotate_refusals(L):  # noqa: F811
     assert call(qot=D) == SHAPE and call(koh=0) == SHAPE                    # output rows that overlap
     assert call(qot=D, qoh=4 * D) == SHAPE
     assert call(qt=1 << 61) == UNSUPPORTED and call(kot=1 << 61) == UNSUPPORTED
-    assert call(n=1 << 30) == UNSUPPORTED
+    assert call(n=1 << 30) == UNSUPPORTED and call(n=(1 << 26) - 8192) == UNSUPPORTED
     pr = P(rope_inv_freq=F.rope_frequencies(128))
     assert call(p=ctypes.byref(pr)) == UNSUPPORTED
 
@@ -149,7 +149,7 @@ def test_attend_refusals(L):  # noqa: F811
     for status, g in bad_pages():
         assert call(pages=g) == status
     seq_refusals(call)
-    for kw in (dict(softcap=-1.0), dict(softcap=math.nan), dict(softcap=math.inf), dict(window=-1), dict(n_init=-1), dict(slopes=FAKE + 2)):
+    for kw in (dict(softcap=-1.0), dict(softcap=1e-39), dict(softcap=math.nan), dict(softcap=math.inf), dict(window=-1), dict(n_init=-1), dict(slopes=FAKE + 2)):
         f = F.ScoreForm(**kw)
         assert call(score=ctypes.byref(f)) == SHAPE, kw
         assert L.infllm_paged_workspace_bytes(ctypes.byref(p), pages(), 3, SEQS["lens"], SEQS["pasts"], ctypes.byref(f)) == 0
