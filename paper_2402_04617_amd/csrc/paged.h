@@ -145,41 +145,51 @@ struct PagedWork {
   int part_tiles;  // key tiles of a part
 };
 __device__ __forceinline__ PagedWork paged_work(const PagedArgs& a, int item) {
-  constexpr int CH = kMaxAttend / kWave;
-  static_assert(CH * kWave == kMaxAttend, "whole waves");
-  const int lane = threadIdx.x & 63;
-  int first[CH], start[CH], len[CH], past[CH], more[CH], n = 0;
-#pragma unroll
-  for (int j = 0; j < CH; ++j) {
-    if (j * kWave >= a.n_seqs) break;
-    const int i = j * kWave + lane;
-    first[j] = a.first[i];
-    start[j] = a.start[i];
-    len[j] = a.len[i];
-    past[j] = a.past[i];
-    more[j] = a.parts[i] | a.table_row[i] << 8;
-  }
-#pragma unroll
-  for (int j = 0; j < CH; ++j) {
-    if (j * kWave >= a.n_seqs) break;
-    n += __popcll(__ballot(j * kWave + lane < a.n_seqs && first[j] <= item));
-  }
-  const int s = __builtin_amdgcn_readfirstlane(n) - 1;
-  auto pick = [&](const int (&x)[CH]) {
-    int v = __builtin_amdgcn_readlane(x[0], s & 63);
-#pragma unroll
-    for (int j = 1; j < CH; ++j)
-      if (s >> 6 == j) v = __builtin_amdgcn_readlane(x[j], s & 63);
-    return v;
-  };
   PagedWork w;
-  w.start = pick(start);
-  w.len = pick(len);
-  w.past = pick(past);
-  const int m = pick(more);
+  int first0, m;
+  if (a.n_seqs == 1) {  // (no trip to memory beside the other arguments')
+    first0 = 0;
+    w.start = a.start[0];
+    w.len = a.len[0];
+    w.past = a.past[0];
+    m = a.parts[0] | a.table_row[0] << 8;
+  } else {
+    constexpr int CH = kMaxAttend / kWave;
+    static_assert(CH * kWave == kMaxAttend, "whole waves");
+    const int lane = threadIdx.x & 63;
+    int first[CH], start[CH], len[CH], past[CH], more[CH], n = 0;
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      if (j * kWave >= a.n_seqs) break;
+      const int i = j * kWave + lane;
+      first[j] = a.first[i];
+      start[j] = a.start[i];
+      len[j] = a.len[i];
+      past[j] = a.past[i];
+      more[j] = a.parts[i] | a.table_row[i] << 8;
+    }
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      if (j * kWave >= a.n_seqs) break;
+      n += __popcll(__ballot(j * kWave + lane < a.n_seqs && first[j] <= item));
+    }
+    const int s = __builtin_amdgcn_readfirstlane(n) - 1;
+    auto pick = [&](const int (&x)[CH]) {
+      int v = __builtin_amdgcn_readlane(x[0], s & 63);
+#pragma unroll
+      for (int j = 1; j < CH; ++j)
+        if (s >> 6 == j) v = __builtin_amdgcn_readlane(x[j], s & 63);
+      return v;
+    };
+    w.start = pick(start);
+    w.len = pick(len);
+    w.past = pick(past);
+    m = pick(more);
+    first0 = pick(first);
+  }
   w.table_row = m >> 8;
   const int parts = (m & 255) + 1;
-  const int tiles = paged_row_tiles(a, (int)a.d_group.d, w.len), u = item - pick(first);
+  const int tiles = paged_row_tiles(a, (int)a.d_group.d, w.len), u = item - first0;
   const int down = parts == 1 ? u : tiles == 1 ? 0 : u / parts;
   w.part = u - down * parts;
   w.rt = tiles - 1 - down;

@@ -180,23 +180,27 @@ __device__ __forceinline__ void form_row(const KeyTiles<KT, THREADS, BACK>& keys
   }
 }
 
-// Scores in the base-2 domain.  The scale and the bias are part of the exponential's
-// argument; a capped score becomes its value first.  c tanh(x / c) = c - 2 c / (1 + e^{2 x /
-// c}): its error of some 2^-23 c is far below what rounding P to bf16 does.
+// Scores in the base-2 domain.  The scale, the cap and the bias are part of the
+// exponential's argument: c tanh(x / c) = c - 2 c r with r = 1 / (1 + e^{2 x / c}), and a score
+// to be capped becomes its r first.  The error of some 2^-23 c is far below what rounding P
+// to bf16 does.
 template <int MOD>
 struct Scores {
-  float c2, cap_in, cap2;
-  __device__ __forceinline__ explicit Scores(const PagedArgs& a) : c2(a.sm_scale * 1.4426950408889634f), cap_in(0.f), cap2(0.f) {
+  float scale, cap_in, cap2;
+  static constexpr float kHidden = MOD & kCap ? __builtin_inff() : -__builtin_inff();  // what a hidden key's score becomes
+  __device__ __forceinline__ explicit Scores(const PagedArgs& a) : scale(a.sm_scale * 1.4426950408889634f), cap_in(0.f), cap2(0.f) {
     if constexpr (MOD & kCap) {
-      cap_in = 2.f * c2 / a.softcap;
+      cap_in = 2.f * scale / a.softcap;
       cap2 = a.softcap * 1.4426950408889634f;
+      scale = -2.f * cap2;
     }
   }
-  __device__ __forceinline__ float capped(float s) const {
-    return __builtin_fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(1.f + fast_exp2(s * cap_in)), cap2);
+  __device__ __forceinline__ float form(float s) const {
+    return MOD & kCap ? __builtin_amdgcn_rcpf(1.f + fast_exp2(s * cap_in)) : s;
   }
-  // The exponent of a score (capped already, if it is to be), b what is to be added.
-  __device__ __forceinline__ float exponent(float s, float b) const { return MOD & kCap ? s + b : __builtin_fmaf(s, c2, b); }
+  // What is added to every score: b, and the cap's own part.
+  __device__ __forceinline__ float base(float b) const { return MOD & kCap ? b + cap2 : b; }
+  __device__ __forceinline__ float exponent(float formed, float base) const { return __builtin_fmaf(formed, scale, base); }
 };
 
 // This wave's LDS accesses before it come before those after it.
@@ -344,18 +348,18 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, PagedSmem<D>& sm, c
     for (int rb = 0; rb < RB; ++rb) {
       if constexpr (MOD & kCap) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[rb][j] = score.capped(s[rb][j]);
+        for (int j = 0; j < 4; ++j) s[rb][j] = score.form(s[rb][j]);
       }
       if (!plain) {
         const uint32_t see = ((uint32_t)seen_keys(pos[rb], k0, a.window, a.n_init) & ok0) >> (4 * q4);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[rb][j] = (see >> j) & 1u ? s[rb][j] : -__builtin_inff();
+        for (int j = 0; j < 4; ++j) s[rb][j] = (see >> j) & 1u ? s[rb][j] : Scores<MOD>::kHidden;
       }
-      const float bias = MOD & kSlopes ? slope[rb] * (float)(k0 + 4 * q4 - pos[rb]) : 0.f;
+      const float bias = score.base(MOD & kSlopes ? slope[rb] * (float)(k0 + 4 * q4 - pos[rb]) : 0.f);
       float e[4], sum;
       auto weights = [&]() {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) e[j] = fast_exp2(score.exponent(s[rb][j], MOD & kSlopes ? __builtin_fmaf(slope[rb], (float)j, bias) + neg_m[rb] : neg_m[rb]));
+        for (int j = 0; j < 4; ++j) e[j] = fast_exp2(score.exponent(s[rb][j], (MOD & kSlopes ? __builtin_fmaf(slope[rb], (float)j, bias) : bias) + neg_m[rb]));
         sum = (e[0] + e[1]) + (e[2] + e[3]);
       };
       weights();
@@ -363,7 +367,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, PagedSmem<D>& sm, c
       if (__ballot(m[rb] == -__builtin_inff() || sum > 65536.f) != 0) {
         float mx = -__builtin_inff();
 #pragma unroll
-        for (int j = 0; j < 4; ++j) mx = fmaxf(mx, score.exponent(s[rb][j], MOD & kSlopes ? __builtin_fmaf(slope[rb], (float)j, bias) : 0.f));
+        for (int j = 0; j < 4; ++j) mx = fmaxf(mx, score.exponent(s[rb][j], MOD & kSlopes ? __builtin_fmaf(slope[rb], (float)j, bias) : bias));
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(m[rb], fmaxf(mx, __shfl_xor(mx, 32)));
         const float alpha = mx == -__builtin_inff() ? 1.f : fast_exp2(m[rb] - mx);
@@ -498,7 +502,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, PagedSmem<D>& sm, c
       constexpr int DPL = D / 64;
       float again[DPL], top = 0.f;
       form_row<bf16_t, D>(keys, kbase, vbase, qp, p_r, a.window, a.n_init, [&](float x, int key) {
-        return fast_exp2(score.exponent(MOD & kCap ? score.capped(x) : x, slope_r * (float)(key - p_r) + nm));
+        return fast_exp2(score.exponent(score.form(x), score.base(slope_r * (float)(key - p_r)) + nm));
       }, again);
 #pragma unroll
       for (int e = 0; e < DPL; ++e) {
@@ -691,12 +695,11 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   // With a bias the tiles are taken from the diagonal backwards, where it falls (forwards,
   // the maximum of a steep one grew with every tile).
   const Scores<MOD> score(a);
-  const float c2 = score.c2;
   // Key place c of a tile (element e = 16 kb + j of a lane: 32 kb + 8 (j / 4) + j % 4, its
   // half's 4 gsel aside).
   auto place_of = [](int e) { return 32 * (e >> 4) + 8 * ((e & 15) >> 2) + (e & 3); };
   // The bias of this half's first key of a tile.
-  auto bias_of = [&](int t) { return MOD & kSlopes ? slope * (float)(key_of(t) + 4 * gsel - pos) : 0.f; };
+  auto bias_of = [&](int t) { return score.base(MOD & kSlopes ? slope * (float)(key_of(t) + 4 * gsel - pos) : 0.f); };
   // The exponent of element e of a tile, b its bias_of plus what is to be added.
   auto exponent = [&](float s, int e, float b) {
     if constexpr (MOD & kSlopes) b = __builtin_fmaf(slope, (float)place_of(e), b);
@@ -718,28 +721,34 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     }
     return l;
   };
-  // Elements [8i, 8i + 8) of a tile's scores: capped, and -inf where the row does not see the key.
+  // Elements [8i, 8i + 8) of a tile's scores: formed, and hidden where the row does not see the key.
   auto form8 = [&](f32x16 (&s)[2], int i, const Lims& l, bool masked) {
 #pragma unroll
     for (int e = 8 * i; e < 8 * i + 8; ++e) {
       const int c = place_of(e);
       float z = s[e >> 4][e & 15];
-      if constexpr (MOD & kCap) z = score.capped(z);
+      if constexpr (MOD & kCap) z = score.form(z);
       if (masked) {
         const uint32_t see = (uint32_t)((int32_t)(l.vis[e >> 4] << (31 - (c & 31))) >> 31);  // all ones or none
-        z = __uint_as_float((__float_as_uint(z) & see) | (0xFF800000u & ~see));
+        z = __uint_as_float((__float_as_uint(z) & see) | (__builtin_bit_cast(uint32_t, Scores<MOD>::kHidden) & ~see));
       }
       s[e >> 4][e & 15] = z;
     }
   };
   auto tile_max = [&](const f32x16 (&s)[2], int t) {
-    float mx = -__builtin_inff();
+    float mx = Scores<MOD>::kHidden;
     const float b = bias_of(t);
+    if constexpr (MOD & kSlopes) {
+      mx = -__builtin_inff();
 #pragma unroll
-    for (int e = 0; e < 32; ++e) mx = fmaxf(mx, MOD & kSlopes ? exponent(s[e >> 4][e & 15], e, b) : s[e >> 4][e & 15]);
+      for (int e = 0; e < 32; ++e) mx = fmaxf(mx, exponent(s[e >> 4][e & 15], e, b));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 32; ++e) mx = MOD & kCap ? fminf(mx, s[e >> 4][e & 15]) : fmaxf(mx, s[e >> 4][e & 15]);
+      mx = score.exponent(mx, b);
+    }
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-    mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-    return MOD ? mx : mx * c2;
+    return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
   };
   // Lazy running maximum, as in the step's attention: a tile's P is formed against the
   // maximum so far, and only where a row's sum of P passes 2^16 (or it has met no visible
@@ -1046,7 +1055,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
         float acc[DPL];
         form_row<bf16_t, D>(keys, kbase, vbase, (const bf16_t*)late.q + (int64_t)(w.start + i) * late.q_tok + (int64_t)h * late.q_head,
                             p_r, a.window, a.n_init,
-                            [&](float s, int key) { return fast_exp2(score.exponent(MOD & kCap ? score.capped(s) : s, slope_r * (float)(key - p_r) + nm)); }, acc);
+                            [&](float s, int key) { return fast_exp2(score.exponent(score.form(s), score.base(slope_r * (float)(key - p_r)) + nm)); }, acc);
         float amax = 0.f;  // (of the finite ones, which keep their precision)
 #pragma unroll
         for (int e = 0; e < DPL; ++e) {
