@@ -136,8 +136,8 @@ struct ItemCost {
 ItemCost item_cost(const PagedArgs& a, bool thin) {
   const bool wide = a.head_dim == 128;
   if (a.bf16) {
-    if (thin) return wide ? ItemCost{2.25f, 2.7f, 0.79f, 3.5f} : ItemCost{1.2f, 2.7f, 0.7f, 3.5f};
-    return wide ? ItemCost{1.5f, 4.8f, 0.9f, 8.8f} : ItemCost{0.62f, 4.8f, 0.49f, 8.8f};
+    if (thin) return wide ? ItemCost{2.25f, 2.8f, 0.785f, 3.5f} : ItemCost{0.875f, 2.8f, 0.64f, 3.5f};
+    return wide ? ItemCost{1.49f, 4.8f, 0.9f, 8.8f} : ItemCost{0.675f, 4.8f, 0.5f, 8.8f};
   }
   if (thin) return wide ? ItemCost{6.f, 5.f, 5.3f, 4.3f} : ItemCost{5.5f, 5.f, 2.7f, 4.3f};
   return wide ? ItemCost{5.5f, 6.4f, 5.2f, 3.7f} : ItemCost{7.5f, 6.4f, 2.5f, 3.7f};
@@ -147,7 +147,7 @@ ItemCost item_cost(const PagedArgs& a, bool thin) {
 struct MergeCost {
   float launch, item, byte, part;
 };
-MergeCost merge_cost(const PagedArgs& a) { return a.bf16 ? MergeCost{4.7f, 3.1e-3f, 2.9e-7f, 0.18f} : MergeCost{3.4f, 0.f, 4.2e-7f, 0.1f}; }
+MergeCost merge_cost(const PagedArgs& a) { return a.bf16 ? MergeCost{4.7f, 3.4e-3f, 2.6e-7f, 0.187f} : MergeCost{3.4f, 0.f, 4.2e-7f, 0.1f}; }
 // Workgroups that run at a time: by their LDS (bf16 two to a compute unit), float32 by
 // their registers too.
 int resident_wgs(const PagedArgs& a) {
