@@ -230,7 +230,9 @@ bool plan(const infllm_params* p, int32_t n_seqs, const int32_t* lens, const int
     int64_t items = 0;
     for (int j = 0; j < n; ++j) {
       const ItemCost& cost = rows[j] <= 32 ? thin : thick;
-      const int parts = (int)((float)keys[j] * per_T + 0.9985f), length = (int)((float)keys[j] / (float)parts + 0.9985f);
+      // (a row tile of far fewer keys than T has its one part all the same)
+      const int parts = std::max(1, (int)((float)keys[j] * per_T + 0.9985f));
+      const int length = (int)((float)keys[j] / (float)parts + 0.9985f);
       const float time = (float)length * cost.tile + cost.item, lone = (float)length * cost.lone_tile + cost.lone_item;
       const int64_t count = (int64_t)tiles[j] * parts * Hkv;
       if (parts > 1) {

@@ -174,6 +174,21 @@ def test_attend_refusals(L):  # noqa: F811
     assert call(p=ctypes.byref(pr)) == UNSUPPORTED
 
 
+def test_workspace_of_uneven_batches(L):  # noqa: F811
+    # one token beside sequences whose keys are tens of thousands of tiles, of every type and head layout
+    seqs = [(1, 0), (1, 1), (3, 60000), (700, 0), (1, 100000), (5000, 1 << 20), (1, 10 ** 7), (40, (1 << 31) - 300)]
+    forms = [None, F.ScoreForm(window=4096, n_init=128), F.ScoreForm(window=1), F.ScoreForm(n_init=(1 << 31) - 1, window=(1 << 31) - 1)]
+    for dtype, size in (("bf16", 2), ("f32", 4)):
+        for d, hq, hkv in ((128, 32, 8), (64, 8, 8), (128, 5, 1)):
+            p = P(n_q_heads=hq, n_kv_heads=hkv, head_dim=d, dtype=dtype)
+            for some in (seqs[:2], seqs[:5], seqs, seqs[::-1], [(1, 0)] * 191 + [(1, 10 ** 7)], [(1, 0), (1, 1 << 30)] * 96):
+                for form in forms:
+                    n = F.infllm_paged_workspace_bytes(p, F.Pages(100, 16, FAKE, FAKE, 16 * hkv * d, d, 16 * d),
+                                                       [x for x, _ in some], [y for _, y in some], form)
+                    parts = 256 * hkv * sum(-(-x * hq // hkv // 32) for x, _ in some)  # of row tiles of 32 rows and more
+                    assert 0 <= n <= parts * 128 * (d * size + 8) + 255
+
+
 def test_frequencies():
     turns = lambda t, n: n * t / (2 * math.pi)  # noqa: E731
     plain = F.infllm_rope_frequencies(64, 10000.0)
