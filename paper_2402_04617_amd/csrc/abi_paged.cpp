@@ -556,12 +556,13 @@ infllm_status infllm_paged_attend(const infllm_params* p, const infllm_pages* pa
   size_t need = 0;
   int64_t at = 0;
   int launches = 0;
-  bool ok;
+  bool ok, planned = false;  // whether `a` holds the call's only launch
   a.table = page_table;
   for (int i = 0; plan(p, n_seqs, seq_lens, past_lens, &i, &at, &a, &ok); ++launches) {
     if (!ok) return INFLLM_E_UNSUPPORTED;
     need = std::max(need, (size_t)partial_rows(a) * part_row_bytes(p));
-    if (i == n_seqs && launches == 0) {  // (a call's only launch is kept)
+    if (i == n_seqs && launches == 0) {
+      planned = true;
       ++launches;
       break;
     }
@@ -574,7 +575,7 @@ infllm_status infllm_paged_attend(const infllm_params* p, const infllm_pages* pa
   if ((st = check_device()) != INFLLM_OK) return st;
   at = 0;
   for (int i = 0, l = 0; l < launches; ++l) {
-    if (launches > 1) {
+    if (!planned) {
       a.table = page_table;
       plan(p, n_seqs, seq_lens, past_lens, &i, &at, &a, &ok);
     }

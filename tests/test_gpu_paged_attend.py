@@ -251,6 +251,17 @@ def test_more_sequences_than_a_launch_takes():
     r.verify(*r.call())
 
 
+@pytest.mark.parametrize("before,between,behind", [(0, 0, 9), (0, 0, 400), (193, 0, 0), (5, 300, 200), (192, 192, 192)])
+def test_batches_padded_with_empty_sequences(before, between, behind):
+    """192 sequences and more of which the first, some between and the last have no new token."""
+    some = [(1, 5), (3, 40), (1, 700), (2, 0)]
+    seqs = [(0, 0)] * before + some * 24 + [(0, 3)] * between + some * 24 + [(0, 0)] * behind
+    r = Run([a for a, _ in seqs], [b for _, b in seqs], 2, 1, 64, 16, "bf16")
+    out, lse = r.call()
+    r.verify(out, lse, heads=[1])
+    assert torch.isfinite(lse).all() and not (lse[0] == 7).any()
+
+
 def test_shared_pages():
     """Sequences that share a prompt's pages see the same keys as with copies of their own."""
     r = Run((1, 1, 5), (160, 160, 156), 4, 2, 128, 16, "bf16")
