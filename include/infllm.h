@@ -536,9 +536,9 @@ typedef struct {
  * past_lens[i] + j on the way (rot; NULL: taken as it is), v copied, and q normed and
  * rotated into q_out (which may be q) in the same launch; q and q_out both NULL leave the
  * queries alone.  Slots that no new token takes are left as they are, as are q_out's
- * rows past the last token.  Two new tokens must not share a slot.  E_RANGE where
- * past_lens[i] + seq_lens[i] tokens need more than table_stride pages; E_UNSUPPORTED
- * where they pass 2^31 - 1. */
+ * rows past the last token.  Two new tokens must not share a slot, and the inputs must
+ * not lie in the pages.  E_RANGE where past_lens[i] + seq_lens[i] tokens need more than
+ * table_stride pages; E_UNSUPPORTED where they pass 2^31 - 256. */
 infllm_status infllm_paged_append(const infllm_params* p, const infllm_rotary* rot, const infllm_pages* pages,
                                   int32_t n_seqs, const int32_t* seq_lens, const int64_t* past_lens,
                                   const int32_t* page_table, int64_t table_stride, const void* q,
@@ -575,8 +575,8 @@ size_t infllm_paged_workspace_bytes(const infllm_params* p, const infllm_pages* 
  *     optional [Hq][total] float32, total the sum of seq_lens.
  * A query that sees nothing (its pages not followed) gets zeros and lse -inf.
  * E_RANGE as in infllm_paged_append.  E_UNSUPPORTED where the rows of k span more than
- * 64 GiB or a page's tokens lie 256 MiB apart, or the work exceeds 32-bit numbers (total * G past 2^31 - 1, positions past
- * 2^31 - 256, or some 2^32 / 256 workgroups). */
+ * 64 GiB or a page's tokens lie 256 MiB apart, or the work exceeds 32-bit numbers
+ * (total * Hq past 2^31 - 1, positions past 2^31 - 256, or 2^24 workgroups). */
 infllm_status infllm_paged_attend(const infllm_params* p, const infllm_pages* pages, int32_t n_seqs,
                                   const int32_t* seq_lens, const int64_t* past_lens, const int32_t* page_table,
                                   int64_t table_stride, const infllm_score_form* score, const void* q,

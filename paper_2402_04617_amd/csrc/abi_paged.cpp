@@ -498,7 +498,7 @@ infllm_status infllm_paged_append(const infllm_params* p, const infllm_rotary* r
 size_t infllm_paged_workspace_bytes(const infllm_params* p, const infllm_pages* pages, int32_t n_seqs,
                                     const int32_t* seq_lens, const int64_t* past_lens, const infllm_score_form* score) {
   int64_t total;
-  if (check_params(p) != INFLLM_OK || check_pages(p, pages) != INFLLM_OK || check_score(p, score) != INFLLM_OK ||
+  if (check_params(p) != INFLLM_OK || remap(p) || check_pages(p, pages) != INFLLM_OK || check_score(p, score) != INFLLM_OK ||
       check_seqs(pages, n_seqs, seq_lens, past_lens, INT32_MAX, &total) != INFLLM_OK || !numbers_fit(p, total))
     return 0;
   PagedArgs a;

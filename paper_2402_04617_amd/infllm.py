@@ -377,7 +377,7 @@ def infllm_rotate(p, rot, n_tokens, positions, q, q_strides, q_out, q_out_stride
         qot, qoh, _ptr(k), kt, kh, _ptr(k_out), kot, koh, _stream(stream)))
 
 
-def _seqs(seq_lens, past_lens, page_table, table_stride):
+def _seqs(seq_lens, past_lens, page_table, table_stride, page_size=0):
     """Host lengths as arrays, and the table's row stride (of a tensor [n_seqs][width], its own)."""
     lens, pasts = _i32s(seq_lens), _i64s(past_lens)
     if len(lens) != len(pasts):
@@ -387,7 +387,15 @@ def _seqs(seq_lens, past_lens, page_table, table_stride):
             return lens, pasts, 0
         if page_table.size(0) < len(lens):
             raise ValueError(f"page_table needs {len(lens)} rows, got {page_table.size(0)}")
-        table_stride = page_table.stride(0)
+        width, table_stride = page_table.size(1), page_table.stride(0)
+        if page_table.element_size() != 4 or (width > 1 and page_table.stride(1) != 1):
+            raise ValueError("page_table is int32, a row's entries next to one another")
+        if len(lens) < 2:
+            table_stride = width
+        elif table_stride > width and page_size:  # (rows of a wider table: the library knows their stride alone)
+            need = max(((past + new - 1) // page_size + 1 for past, new in zip(pasts, lens) if new > 0), default=0)
+            if need > width:
+                raise ValueError(f"page_table needs {need} pages of a sequence, got {width}")
     return lens, pasts, table_stride
 
 
@@ -395,7 +403,7 @@ def infllm_paged_append(p, rot, pages, seq_lens, past_lens, page_table, q, q_str
                         kv_strides, table_stride=None, stream=None):
     """seq_lens, past_lens: host ints, one of each per sequence; page_table: int32 tensor [n_seqs][pages of a sequence];
     rot, and q with q_out, may be None."""
-    lens, pasts, stride = _seqs(seq_lens, past_lens, page_table, table_stride)
+    lens, pasts, stride = _seqs(seq_lens, past_lens, page_table, table_stride, pages.page_size)
     qs, qos = q_strides or (0, 0), q_out_strides or (0, 0)
     _check("infllm_paged_append", lib().infllm_paged_append(
         ctypes.byref(p), None if rot is None else ctypes.byref(rot), ctypes.byref(pages), len(lens), _at(lens),
@@ -412,7 +420,7 @@ def infllm_paged_workspace_bytes(p, pages, seq_lens, past_lens, score=None) -> i
 def infllm_paged_attend(p, pages, seq_lens, past_lens, page_table, score, q, q_strides, out, out_strides, lse=None,
                         workspace=None, workspace_bytes=None, table_stride=None, stream=None):
     """As infllm_paged_append; score: a ScoreForm, or None."""
-    lens, pasts, stride = _seqs(seq_lens, past_lens, page_table, table_stride)
+    lens, pasts, stride = _seqs(seq_lens, past_lens, page_table, table_stride, pages.page_size)
     _check("infllm_paged_attend", lib().infllm_paged_attend(
         ctypes.byref(p), ctypes.byref(pages), len(lens), _at(lens), _at(pasts), _ptr(page_table), stride,
         None if score is None else ctypes.byref(score), _ptr(q), q_strides[0], q_strides[1], _ptr(out), out_strides[0],

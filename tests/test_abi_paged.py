@@ -172,6 +172,27 @@ def test_attend_refusals(L):  # noqa: F811
     assert call(lens=i32(1 << 29, 0, 1), pasts=i64(0, 0, 0), width=1 << 30) == UNSUPPORTED
     pr = P(rope_inv_freq=F.rope_frequencies(128))
     assert call(p=ctypes.byref(pr)) == UNSUPPORTED
+    uneven = (pages(), 2, i32(1, 1), i64(30000, 100), None)
+    assert L.infllm_paged_workspace_bytes(ctypes.byref(p), *uneven) > 0
+    assert L.infllm_paged_workspace_bytes(ctypes.byref(pr), *uneven) == 0
+
+
+def test_page_tables_that_the_wrappers_refuse(L):  # noqa: F811
+    import torch
+    p, g = P(), F.Pages(100, 16, FAKE, FAKE, 16 * HKV * D, D, 16 * D)
+    wide = torch.zeros((3, 8), dtype=torch.int32)
+    for table, lens, pasts in ((wide[:1], (1, 1), (0, 0)), (wide.long(), (1,), (0,)), (wide.T, (1,), (0,)), (wide.T, (1, 1), (0, 0)),
+                               (wide[:, 4:], (1, 0, 40), (63, 1 << 40, 25)), (wide[:, 7:], (1, 1), (0, 16))):
+        with pytest.raises(ValueError):
+            F.infllm_paged_append(p, None, g, lens, pasts, table, None, None, None, None, FAKE, FAKE, (HKV * D, D))
+        with pytest.raises(ValueError):
+            F.infllm_paged_attend(p, g, lens, pasts, table, None, FAKE, (HQ * D, D), FAKE, (HQ * D, D))
+    for table in (wide[1:2, 4:], wide[:, 4:][:2]):         # a single row, and rows of a wider table: too many tokens for their pages
+        with pytest.raises((ValueError, F.InfllmError)):
+            F.infllm_paged_attend(p, g, (1,) * len(table), (64,) * len(table), table, None, FAKE, (HQ * D, D), FAKE, (HQ * D, D),
+                                  stream=FAKE)
+    with pytest.raises(ValueError):
+        F.infllm_paged_append(p, None, g, (1, 1), (0,), wide, None, None, None, None, FAKE, FAKE, (HKV * D, D))
 
 
 def test_workspace_of_uneven_batches(L):  # noqa: F811
