@@ -46,8 +46,8 @@ KERNEL_TRAFFIC = {
     # infllm_score_units: its two kernels), from `rocprofv3 --pmc FETCH_SIZE` and `--pmc WRITE_SIZE`
     # runs of `bench.py --legs 1m,decode --no-cpu-baseline --steps 1 --warmup 0`, averaged over the
     # replayed launches the bench line times
-    "attend_mfma_llama3-8b-128k": {"src": {"attend_mfma.hip": "30d23f3b234c96834cf7ca0eb4e3bb2f1ffd5b6449b35e156c6d1e49244949ed", "launch.h": "c84efff6ce119de53c6f3069382c05bae80fbc2fe80d6542be7f1e705e4441e6"},
-                                   "fetch_kib": 20584.5, "write_kib": 16896.0},
+    "attend_mfma_llama3-8b-128k": {"src": {"attend_mfma.hip": "9c986b06560e7aa04cef06f66443122825013685bd3af830d4d893eb0f3c4e40", "mfma_tile.h": "19fde6ca9dfc9047c53d0cec0d3d19f8c0c0cc14949be8130d6ba59eae604ebd", "launch.h": "c84efff6ce119de53c6f3069382c05bae80fbc2fe80d6542be7f1e705e4441e6"},
+                                   "fetch_kib": 20527.4, "write_kib": 16896.0},
     "score_llama3-8b-128k": {"src": {"score.hip": "b863ba9bf6e01b4901383469e615c02c7ae9b482693bef88e3f29735e4666a13", "launch.h": "c84efff6ce119de53c6f3069382c05bae80fbc2fe80d6542be7f1e705e4441e6"},
                              "fetch_kib": 2086.6 + 2281.5, "write_kib": 64.0 + 34.3},
     "append_llama3-8b-128k": {"src": {"append.hip": "0837574dfd5863477c3058538a7d7226d7cbcb94eced149826ff5f829db011cc", "launch.h": "c84efff6ce119de53c6f3069382c05bae80fbc2fe80d6542be7f1e705e4441e6"},
