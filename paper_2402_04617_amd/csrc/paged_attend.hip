@@ -210,15 +210,19 @@ __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
 }
 
-// A part of a row tile of at most 16 RB rows (single tokens, a few guessed ones): the waves
+// A part of a row tile of at most 16 rows (single tokens, a few guessed ones): the waves
 // share the keys instead of the rows.  Wave w takes the 16 keys of every tile that it loads
 // itself, so that the waves run without a barrier, each with its next two tiles' keys and
 // values in flight, and join their shares in LDS at the end.  S^T = K Q^T with
 // v_mfma_f32_16x16x32_bf16: a lane has keys 4 (lane / 16) .. + 3 of row lane % 16, which is
 // the B operand of v_mfma_f32_16x16x16_bf16 as it stands; V^T read transposed.  Bound by
-// memory: one wave of four with all rows of the tile (of 32, four used) took 348 us for 48
-// sequences of up to 20,000 tokens.
-template <int D, int MOD, bool GROUPS, int RB>
+// memory: 48 sequences of up to 20,000 tokens (1.98 GB) take 338 us, 5.85 TB/s, and 346 with
+// the merge.  One wave of four with all rows of the tile (of 32, four used) takes 351.5 there,
+// 99.2 instead of 93.6 with a cap and a window of 4,096 keys, 13.8 instead of 13.2 for one
+// sequence of 2,000.  Up to 32 rows this way (two blocks of them) were slower than the row
+// tile's one wave: 32 sequences of 8 tokens after 4,000 100 and 97 us, 64 of one token with 32
+// heads to a kv head 120 and 112, 4 of 5 tokens 23.8 and 20.6.
+template <int D, int MOD, bool GROUPS>
 __device__ __forceinline__ void few_rows(const PagedArgs& a, PagedSmem<D>& sm, const PagedWork& w, const PagedRange& range, int g, int i0,
                                          int i1) {
   constexpr int CH = D / 8, KSTEPS = D / 32, DBLK = D / 16;
@@ -299,24 +303,18 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, PagedSmem<D>& sm, c
     ok1 = there_of(here, t_begin + 1);
   }
 
-  bf16x8 qreg[RB][KSTEPS];
-  int pos[RB];
-  float slope[RB], m[RB], neg_m[RB], l[RB];
-  f32x4 o[RB][DBLK];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int row = min(16 * rb + c, R - 1), qi = div_by(row, a.d_group), qh = g * G + row - qi * G;
+  const int row = min(c, R - 1), qi = div_by(row, a.d_group), qh = g * G + row - qi * G, pos = w.past + qi;
+  bf16x8 qreg[KSTEPS];
+  {
     const bf16_t* qp = (const bf16_t*)a.q + (int64_t)(w.start + qi) * a.q_tok + (int64_t)qh * a.q_head + 8 * q4;
 #pragma unroll
-    for (int s = 0; s < KSTEPS; ++s) qreg[rb][s] = *(const bf16x8*)(qp + 32 * s);
-    pos[rb] = w.past + qi;
-    slope[rb] = 0.f;
-    if constexpr (MOD & kSlopes) slope[rb] = a.slopes[qh] * 1.4426950408889634f;
-    m[rb] = -__builtin_inff();
-    neg_m[rb] = l[rb] = 0.f;
-#pragma unroll
-    for (int db = 0; db < DBLK; ++db) o[rb][db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < KSTEPS; ++s) qreg[s] = *(const bf16x8*)(qp + 32 * s);
   }
+  float slope = 0.f, m = -__builtin_inff(), neg_m = 0.f, l = 0.f;
+  if constexpr (MOD & kSlopes) slope = a.slopes[qh] * 1.4426950408889634f;
+  f32x4 o[DBLK];
+#pragma unroll
+  for (int db = 0; db < DBLK; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
   const Scores<MOD> score(a);
   // LDS offsets of the fragments, XOR-related under the swizzle: K, k-step s: ^ 64 s; V^T,
   // block db: ^ 32 db
@@ -332,58 +330,55 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, PagedSmem<D>& sm, c
     const bool more = t + 1 < t_end;
     if (more) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(3 * NI) : "memory");  // this tile's keys have landed
     else asm volatile("s_waitcnt vmcnt(%0)" : : "n"(NI) : "memory");
-    f32x4 s[RB];
+    f32x4 s;
     const uint32_t ka = lds_k0 + buf + koff;
 #pragma unroll
     for (int k = 0; k < KSTEPS; ++k) {
       const bf16x8 kf = *(const INFLLM_LDS bf16x8*)(uintptr_t)(ka ^ (64u * k));
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
-        s[rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qreg[rb][k], k == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[rb], 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qreg[k], k == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s, 0, 0, 0);
     }
     const int k0 = keys.key_of(t) + 16 * wave;
     const bool plain = t >= plain0 && t < plain1 && ok0 == 0xFFFFu;
-    i16x4 p[RB];
+    if constexpr (MOD & kCap) {
 #pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      if constexpr (MOD & kCap) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s[rb][j] = score.form(s[rb][j]);
-      }
-      if (!plain) {
-        const uint32_t see = ((uint32_t)seen_keys(pos[rb], k0, a.window, a.n_init) & ok0) >> (4 * q4);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) s[rb][j] = (see >> j) & 1u ? s[rb][j] : Scores<MOD>::kHidden;
-      }
-      const float bias = score.base(MOD & kSlopes ? slope[rb] * (float)(k0 + 4 * q4 - pos[rb]) : 0.f);
-      float e[4], sum;
-      auto weights = [&]() {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) e[j] = fast_exp2(score.exponent(s[rb][j], (MOD & kSlopes ? __builtin_fmaf(slope[rb], (float)j, bias) : bias) + neg_m[rb]));
-        sum = (e[0] + e[1]) + (e[2] + e[3]);
-      };
-      weights();
-      // the running maximum, raised only where a sum passes 2^16 or nothing has been seen yet
-      if (__ballot(m[rb] == -__builtin_inff() || sum > 65536.f) != 0) {
-        float mx = -__builtin_inff();
-#pragma unroll
-        for (int j = 0; j < 4; ++j) mx = fmaxf(mx, score.exponent(s[rb][j], MOD & kSlopes ? __builtin_fmaf(slope[rb], (float)j, bias) : bias));
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(m[rb], fmaxf(mx, __shfl_xor(mx, 32)));
-        const float alpha = mx == -__builtin_inff() ? 1.f : fast_exp2(m[rb] - mx);
-        l[rb] *= alpha;
-#pragma unroll
-        for (int db = 0; db < DBLK; ++db) o[rb][db] *= alpha;
-        m[rb] = mx;
-        neg_m[rb] = mx == -__builtin_inff() ? 0.f : -mx;
-        weights();
-      }
-      l[rb] += sum;
-      bf16x4 pb;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) pb[j] = (__bf16)e[j];  // (by at most 2^-8 of each; the sums take them unrounded)
-      p[rb] = __builtin_bit_cast(i16x4, pb);
+      for (int j = 0; j < 4; ++j) s[j] = score.form(s[j]);
     }
+    if (!plain) {
+      const uint32_t see = ((uint32_t)seen_keys(pos, k0, a.window, a.n_init) & ok0) >> (4 * q4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[j] = (see >> j) & 1u ? s[j] : Scores<MOD>::kHidden;
+    }
+    const float bias = score.base(MOD & kSlopes ? slope * (float)(k0 + 4 * q4 - pos) : 0.f);
+    float e[4], sum;
+    auto exponent = [&](int j, float more) {
+      return score.exponent(s[j], (MOD & kSlopes ? __builtin_fmaf(slope, (float)j, bias) : bias) + more);
+    };
+    auto weights = [&]() {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) e[j] = fast_exp2(exponent(j, neg_m));
+      sum = (e[0] + e[1]) + (e[2] + e[3]);
+    };
+    weights();
+    // the running maximum, raised only where a sum passes 2^16 or nothing has been seen yet
+    if (__ballot(m == -__builtin_inff() || sum > 65536.f) != 0) {
+      float mx = -__builtin_inff();
+#pragma unroll
+      for (int j = 0; j < 4; ++j) mx = fmaxf(mx, exponent(j, 0.f));
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32)));
+      const float alpha = mx == -__builtin_inff() ? 1.f : fast_exp2(m - mx);
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < DBLK; ++db) o[db] *= alpha;
+      m = mx;
+      neg_m = mx == -__builtin_inff() ? 0.f : -mx;
+      weights();
+    }
+    l += sum;
+    bf16x4 pb;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) pb[j] = (__bf16)e[j];  // (by at most 2^-8 of each; the sums take them unrounded)
+    const i16x4 p = __builtin_bit_cast(i16x4, pb);
     if (more) asm volatile("s_waitcnt vmcnt(%0)" : : "n"(2 * NI) : "memory");  // its values
     else asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
     const uint32_t va = lds_v0 + buf + voff0;
@@ -396,8 +391,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, PagedSmem<D>& sm, c
 #pragma unroll
     for (int db = 0; db < DBLK; ++db) {
       const i16x4 vf = __builtin_amdgcn_ds_read_tr16_b64_v4i16((INFLLM_LDS i16x4*)(uintptr_t)(va ^ (32u * db)));
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, p[rb], o[rb][db], 0, 0, 0);
+      o[db] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, p, o[db], 0, 0, 0);
     }
     ok0 = ok1;
     if (t + 2 < t_end) {
@@ -412,112 +406,109 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, PagedSmem<D>& sm, c
   }
 
   // The waves' shares through LDS: [wave][row] of D values (padded), then maxima and sums.
-  constexpr int kRow = D * 4 + 16, kRows = 16 * RB;
+  constexpr int kRow = D * 4 + 16, kRows = 16;
   static_assert(4 * kRows * (kRow + 8) <= (int)sizeof(sm), "the shares fit");
   INFLLM_LDS char* share = (INFLLM_LDS char*)(INFLLM_LDS PagedSmem<D>*)&sm;
   INFLLM_LDS float* stats = (INFLLM_LDS float*)(share + 4 * kRows * kRow);  // [wave][row]{m, l}
   lds_barrier();  // every wave is done with its tiles (its loads have landed)
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-#pragma unroll
-    for (int db = 0; db < DBLK; ++db)
-      *(INFLLM_LDS f32x4*)(share + (wave * kRows + 16 * rb + c) * kRow + 4 * (16 * db + 4 * q4)) = o[rb][db];
-    float sum = l[rb];
+  for (int db = 0; db < DBLK; ++db)
+    *(INFLLM_LDS f32x4*)(share + (wave * kRows + c) * kRow + 4 * (16 * db + 4 * q4)) = o[db];
+  {
+    float sum = l;
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     if (q4 == 0) {
-      stats[2 * (wave * kRows + 16 * rb + c)] = m[rb];
-      stats[2 * (wave * kRows + 16 * rb + c) + 1] = sum;
+      stats[2 * (wave * kRows + c)] = m;
+      stats[2 * (wave * kRows + c) + 1] = sum;
     }
   }
   lds_barrier();
-  constexpr int TPR = D / 8, RPP = 256 / TPR;  // threads of a row, rows at a time
+  constexpr int TPR = D / 8;  // threads of a row
+  static_assert(256 / TPR >= kRows, "all rows at once");
   const int64_t prow0 = (int64_t)blockIdx.x * a.item_rows;
+  const int r = tid / TPR, d = 8 * (tid % TPR);
+  if ((tid & ~63) / TPR >= R) return;  // (whole waves)
+  const int rc = min(r, kRows - 1);
+  float M = -__builtin_inff(), L = 0.f, acc[8] = {};
 #pragma unroll
-  for (int r0 = 0; r0 < kRows; r0 += RPP) {
-    const int r = r0 + tid / TPR, d = 8 * (tid % TPR);
-    if (r0 + (tid & ~63) / TPR >= R) continue;  // (whole waves)
-    const int rc = min(r, kRows - 1);
-    float M = -__builtin_inff(), L = 0.f, acc[8] = {};
+  for (int v = 0; v < 4; ++v) M = fmaxf(M, stats[2 * (v * kRows + rc)]);
+  const float base = M == -__builtin_inff() ? 0.f : M;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) M = fmaxf(M, stats[2 * (v * kRows + rc)]);
-    const float base = M == -__builtin_inff() ? 0.f : M;
+  for (int v = 0; v < 4; ++v) {
+    const float mv = stats[2 * (v * kRows + rc)], lv = stats[2 * (v * kRows + rc) + 1];
+    const float f = mv == -__builtin_inff() ? 0.f : fast_exp2(mv - base);
+    const bool live = mv != -__builtin_inff() || lv != lv;
+    L += live ? lv * (lv != lv ? 1.f : f) : 0.f;
+    const INFLLM_LDS f32x4* x = (const INFLLM_LDS f32x4*)(share + (v * kRows + rc) * kRow + 4 * d);
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-      const float mv = stats[2 * (v * kRows + rc)], lv = stats[2 * (v * kRows + rc) + 1];
-      const float f = mv == -__builtin_inff() ? 0.f : fast_exp2(mv - base);
-      const bool live = mv != -__builtin_inff() || lv != lv;
-      L += live ? lv * (lv != lv ? 1.f : f) : 0.f;
-      const INFLLM_LDS f32x4* x = (const INFLLM_LDS f32x4*)(share + (v * kRows + rc) * kRow + 4 * d);
+    for (int e = 0; e < 8; ++e) acc[e] += live ? f * x[e >> 2][e & 3] : 0.f;
+  }
+  const bool row_ok = r < R && r < kRows;
+  const int i = div_by(min(r, R - 1), a.d_group), h = g * G + min(r, R - 1) - i * G;
+  float inv = L > 0.f ? 1.f / L : 0.f;
+  float lse_v = L > 0.f ? (M + __log2f(L)) * 0.6931471805599453f : -__builtin_inff();
+  if (L != L) {  // a NaN among the row's scores is the row's, through the merge as well
+    inv = L;
+    lse_v = one_part ? L : __builtin_inff();
+  }
+  float z = 0.f, amax = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += live ? f * x[e >> 2][e & 3] : 0.f;
+  for (int e = 0; e < 8; ++e) {
+    z = __builtin_fmaf(acc[e], 0.f, z);
+    acc[e] *= inv;
+    amax = fmaxf(amax, fabsf(acc[e]));
+  }
+#pragma unroll
+  for (int x = 1; x < TPR; x <<= 1) {
+    z += __shfl_xor(z, x);
+    amax = fmaxf(amax, __shfl_xor(amax, x));
+  }
+  // A row that a masked value which is not finite has reached (0 times it) is formed again
+  // by the wave from the keys that it sees.
+  const bool apart = row_ok && !(z == 0.f) && L == L;
+  uint64_t odd = __ballot(apart && tid % TPR == 0);
+  const int ex = one_part ? 0 : partial_row_exponent(amax);
+  if (row_ok && !apart) {
+    const float sc = exp2_int(-ex);
+    u32x4 x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      x[e] = one_part ? (uint32_t)f32_to_bf16(acc[2 * e]) | ((uint32_t)f32_to_bf16(acc[2 * e + 1]) << 16)
+                      : pack_f16x2(acc[2 * e] * sc, acc[2 * e + 1] * sc);
+    if (!one_part) *(u32x4*)((char*)a.part_o + (prow0 + r) * (D * 2) + 2 * d) = x;
+    else *(u32x4*)((bf16_t*)a.out + (int64_t)(w.start + i) * a.out_tok + (int64_t)h * a.out_head + d) = x;
+    if (d == 0 && !one_part) a.part_exp[prow0 + r] = ex;
+  }
+  if (row_ok && d == 0) {
+    if (!one_part) a.part_lse[prow0 + r] = lse_v;
+    else if (a.lse != nullptr) a.lse[h * a.lse_stride + w.start + i] = lse_v;
+  }
+  for (; odd != 0; odd &= odd - 1) {
+    const int src = __builtin_ctzll(odd), rr = __shfl(r, src), p_r = w.past + __shfl(i, src);
+    const float nm = -__shfl(base, src), inv_r = __shfl(inv, src);
+    const int hr = __shfl(h, src);
+    const bf16_t* qp = (const bf16_t*)a.q + (int64_t)(p_r - w.past + w.start) * a.q_tok + (int64_t)hr * a.q_head;
+    float slope_r = 0.f;
+    if constexpr (MOD & kSlopes) slope_r = a.slopes[hr] * 1.4426950408889634f;
+    constexpr int DPL = D / 64;
+    float again[DPL], top = 0.f;
+    form_row<bf16_t, D>(keys, kbase, vbase, qp, p_r, a.window, a.n_init, [&](float x, int key) {
+      return fast_exp2(score.exponent(score.form(x), score.base(slope_r * (float)(key - p_r)) + nm));
+    }, again);
+#pragma unroll
+    for (int e = 0; e < DPL; ++e) {
+      again[e] *= inv_r;
+      const float x = fabsf(again[e]);
+      top = x < __builtin_inff() ? fmaxf(top, x) : top;  // (of the finite ones, which keep their precision)
     }
-    const bool row_ok = r < R && r < kRows;
-    const int i = div_by(min(r, R - 1), a.d_group), h = g * G + min(r, R - 1) - i * G;
-    float inv = L > 0.f ? 1.f / L : 0.f;
-    float lse_v = L > 0.f ? (M + __log2f(L)) * 0.6931471805599453f : -__builtin_inff();
-    if (L != L) {  // a NaN among the row's scores is the row's, through the merge as well
-      inv = L;
-      lse_v = one_part ? L : __builtin_inff();
-    }
-    float z = 0.f, amax = 0.f;
+    const int ex_r = one_part ? 0 : partial_row_exponent(wave_max(top));
+    uint16_t* to = one_part ? (uint16_t*)a.out + (int64_t)(p_r - w.past + w.start) * a.out_tok + (int64_t)hr * a.out_head
+                            : (uint16_t*)a.part_o + (prow0 + rr) * D;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      z = __builtin_fmaf(acc[e], 0.f, z);
-      acc[e] *= inv;
-      amax = fmaxf(amax, fabsf(acc[e]));
-    }
-#pragma unroll
-    for (int x = 1; x < TPR; x <<= 1) {
-      z += __shfl_xor(z, x);
-      amax = fmaxf(amax, __shfl_xor(amax, x));
-    }
-    // A row that a masked value which is not finite has reached (0 times it) is formed again
-    // by the wave from the keys that it sees.
-    const bool apart = row_ok && !(z == 0.f) && L == L;
-    uint64_t odd = __ballot(apart && tid % TPR == 0);
-    const int ex = one_part ? 0 : partial_row_exponent(amax);
-    if (row_ok && !apart) {
-      const float sc = exp2_int(-ex);
-      u32x4 x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        x[e] = one_part ? (uint32_t)f32_to_bf16(acc[2 * e]) | ((uint32_t)f32_to_bf16(acc[2 * e + 1]) << 16)
-                        : pack_f16x2(acc[2 * e] * sc, acc[2 * e + 1] * sc);
-      if (!one_part) *(u32x4*)((char*)a.part_o + (prow0 + r) * (D * 2) + 2 * d) = x;
-      else *(u32x4*)((bf16_t*)a.out + (int64_t)(w.start + i) * a.out_tok + (int64_t)h * a.out_head + d) = x;
-      if (d == 0 && !one_part) a.part_exp[prow0 + r] = ex;
-    }
-    if (row_ok && d == 0) {
-      if (!one_part) a.part_lse[prow0 + r] = lse_v;
-      else if (a.lse != nullptr) a.lse[h * a.lse_stride + w.start + i] = lse_v;
-    }
-    for (; odd != 0; odd &= odd - 1) {
-      const int src = __builtin_ctzll(odd), rr = __shfl(r, src), p_r = w.past + __shfl(i, src);
-      const float nm = -__shfl(base, src), inv_r = __shfl(inv, src);
-      const int hr = __shfl(h, src);
-      const bf16_t* qp = (const bf16_t*)a.q + (int64_t)(p_r - w.past + w.start) * a.q_tok + (int64_t)hr * a.q_head;
-      float slope_r = 0.f;
-      if constexpr (MOD & kSlopes) slope_r = a.slopes[hr] * 1.4426950408889634f;
-      constexpr int DPL = D / 64;
-      float again[DPL], top = 0.f;
-      form_row<bf16_t, D>(keys, kbase, vbase, qp, p_r, a.window, a.n_init, [&](float x, int key) {
-        return fast_exp2(score.exponent(score.form(x), score.base(slope_r * (float)(key - p_r)) + nm));
-      }, again);
-#pragma unroll
-      for (int e = 0; e < DPL; ++e) {
-        again[e] *= inv_r;
-        const float x = fabsf(again[e]);
-        top = x < __builtin_inff() ? fmaxf(top, x) : top;  // (of the finite ones, which keep their precision)
-      }
-      const int ex_r = one_part ? 0 : partial_row_exponent(wave_max(top));
-      uint16_t* to = one_part ? (uint16_t*)a.out + (int64_t)(p_r - w.past + w.start) * a.out_tok + (int64_t)hr * a.out_head
-                              : (uint16_t*)a.part_o + (prow0 + rr) * D;
-#pragma unroll
-      for (int e = 0; e < DPL; ++e)
-        to[DPL * lane + e] = one_part ? f32_to_bf16(again[e]) : (uint16_t)(pack_f16x2(again[e] * exp2_int(-ex_r), 0.f) & 0xFFFFu);
-      if (!one_part && lane == 0) a.part_exp[prow0 + rr] = ex_r;
-    }
+    for (int e = 0; e < DPL; ++e)
+      to[DPL * lane + e] = one_part ? f32_to_bf16(again[e]) : (uint16_t)(pack_f16x2(again[e] * exp2_int(-ex_r), 0.f) & 0xFFFFu);
+    if (!one_part && lane == 0) a.part_exp[prow0 + rr] = ex_r;
   }
 }
 
@@ -550,11 +541,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   const int t_begin = w.part * w.part_tiles, t_end = min(t_begin + w.part_tiles, range.n);
   if (t_begin >= t_end) return;  // (the parts of a sequence are as many for each of its row tiles)
   if (R <= 16) {
-    few_rows<D, MOD, GROUPS, 1>(a, sm, w, range, g, i0, i1);
-    return;
-  }
-  if (R <= 32) {
-    few_rows<D, MOD, GROUPS, 2>(a, sm, w, range, g, i0, i1);
+    few_rows<D, MOD, GROUPS>(a, sm, w, range, g, i0, i1);
     return;
   }
   const bool one_part = range.n <= w.part_tiles;
