@@ -15,6 +15,16 @@
 // the query rows in registers, so that a lane has 16 scores of one row for each of two key
 // blocks; P^T = exp2(z - m) is the B operand of O^T += V^T P^T as it stands, V^T read
 // transposed.  Products of one tile run beside the exponentials of another.
+//
+// What bounds it: a long chunk the matrix cores at the clock that the power limit leaves
+// (2,048 tokens after 64,000, 32 query heads of 128, 8 kv heads: 1.86 to 2.02 ms by card, 1.08
+// to 1.17 PFLOP/s, 85 to 92 % of a library product of 8,192^3 on the same card; the matrix
+// cores busy 68 % of the cycles, 5.2 vector instructions for each of theirs).  The cap adds
+// an exponential and a reciprocal to a score and makes the vector ALU the bound (10.8 vector
+// instructions for one matrix instruction; 700, 1,500 and 64 tokens with a window of 4,096:
+// 107 us, 0.65 PFLOP/s), the bias two multiply-adds (7.2; 125 us, 0.80).  Single tokens beside
+// chunks read their keys from memory while chunks have theirs in the caches: 512 and 300 new
+// tokens and 30 single ones (613 MB) 165 us and 13 for the merge.  A few rows: see few_rows.
 #include <type_traits>
 
 #include "mfma_tile.h"
@@ -1096,7 +1106,12 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
 // order that lets one 16-byte read feed four products; sums of 16 products are joined by
 // additions.  O^T += V^T P^T with P^T as it stands; output block db holds dims DBLK*m + db,
 // so that one read feeds all blocks.  Rows of an LDS tile are XOR-swizzled by piece, which
-// leaves both reads without conflicts.
+// leaves both reads without conflicts.  Bound by the float32 matrix cores where a workgroup
+// has its keys (64 dims: a tile's products 1.8 us, its softmax 0.7), and in small batches by
+// what stands around them: 637 tokens of five sequences after up to 2,600, 8 query heads of
+// 64, 20.9 us and 6.5 for the merge, of which 3.4 are the wait for arguments, table and first
+// tile.  Rows of a tile (128, 64, 32) by the longest sequence's: waves without rows would
+// only load.
 constexpr int kF32Tile = 32;
 
 // e^x for x <= 0 (and NaN): 2^t, t = x log2(e) rounded, which moves e^x by at most 2^-25 of

@@ -7,6 +7,11 @@
 // keeps to one token: each lane forms the sine and cosine of one pair (in float64, reduced
 // to half a revolution there; the function's own cost is one lane's), which all rows of
 // the token then share.  In float32, rounded once.
+//
+// Bound by memory: 16,000 tokens of 32 + 8 heads of 128 with norms (328 MB) take 66 us, 5.0
+// TB/s, 92 % of a large copy's rate; 20 prompts into pages with queries and values (435 MB) 89
+// us, 4.9.  A few tokens (16: 4 us, 32 into pages: 5) are one launch's latency, their rows
+// over several waves.
 #include <type_traits>
 
 #include "paged.h"
@@ -15,7 +20,7 @@ namespace infllm {
 namespace {
 
 constexpr int kRotWaves = 4;
-constexpr int kRotAhead = 8;  // row groups whose loads are in flight
+constexpr int kRotAhead = 8;  // row groups whose loads are in flight (of 4: the prompts 91 us, not 89)
 
 template <typename T> struct Piece;
 template <> struct Piece<bf16_t> {
