@@ -465,10 +465,9 @@ infllm_status infllm_paged_append(const infllm_params* p, const infllm_rotary* r
   const int n_q = q != nullptr ? p->n_q_heads : 0;
   if (!rotate_fits(total)) return INFLLM_E_UNSUPPORTED;
   if ((st = check_device()) != INFLLM_OK) return st;
-  RotateArgs a;
+  AppendPagesArgs a;
   std::memset(&a, 0, sizeof(a));
   set_rotary(p, rot, &a);
-  a.paged = true;
   a.n_q = n_q;
   a.n_k = a.n_v = p->n_kv_heads;
   a.q = q;

@@ -34,8 +34,8 @@ __device__ __forceinline__ int paged_seq_of(const PagedSeqs& a, int t) {
   return __builtin_amdgcn_readfirstlane(n) - 1;
 }
 
-// Norms and rotation (and, with pages, the append).  A token has n_q query rows, n_k key
-// rows and n_v value rows, in this order; a wave has `rows_wave` of them.
+// Norms and rotation.  A token has n_q query rows, n_k key rows and n_v value rows, in this
+// order; a wave has `rows_wave` of them.
 struct RotateArgs {
   int first_token, n_tokens;  // of this launch
   int n_q, n_k, n_v;
@@ -56,11 +56,15 @@ struct RotateArgs {
   const void* q_weight;
   const void* k_weight;
   int head_dim;
-  bool bf16, paged;
+  bool bf16;
   double rev[kMaxPairs];  // revolutions per position of pair i
+};
+// And the append to pages.  (Apart, for the 2 KB of sequences cost a launch 0.4 us on the host.)
+struct AppendPagesArgs : RotateArgs {
   PagedSeqs seqs;
 };
 hipError_t launch_rotate(const RotateArgs& a, hipStream_t s);
+hipError_t launch_rotate(const AppendPagesArgs& a, hipStream_t s);
 
 // Attention over pages.  A row tile is a run of rows (query-major, the group's heads
 // packed) of one sequence.  The key tiles that a row tile sees, in order, are those of the

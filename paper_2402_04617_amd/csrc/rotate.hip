@@ -83,8 +83,9 @@ __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-template <typename T, int D, bool PAGED>
-__global__ void __launch_bounds__(64 * kRotWaves) rotate_kernel(RotateArgs a) {
+template <typename T, int D, typename Args>
+__global__ void __launch_bounds__(64 * kRotWaves) rotate_kernel(Args a) {
+  constexpr bool PAGED = std::is_same<Args, AppendPagesArgs>::value;
   constexpr int N = Piece<T>::N, LPR = D / N, RPP = 64 / LPR;
   __shared__ __attribute__((aligned(16))) float2 trig[kRotWaves][D / 2];
   __shared__ __attribute__((aligned(16))) float rows[kRotWaves][RPP][D];
@@ -97,17 +98,18 @@ __global__ void __launch_bounds__(64 * kRotWaves) rotate_kernel(RotateArgs a) {
   const int r_end = min(a.n_q + a.n_k + a.n_v, r_begin + a.rows_wave);
   int64_t pos;
   int page = 0, slot = 0;
+  bool there = true;
   if constexpr (PAGED) {
     const int s = paged_seq_of(a.seqs, (int)t);
     const int at = a.seqs.past[s] + ((int)t - a.seqs.start[s]);
     const int x = div_by(at, a.seqs.d_page);
     slot = at - x * a.seqs.page_size;
     page = a.seqs.table[s * a.seqs.table_stride + x];
+    there = page >= 0 && page < a.seqs.n_pages;
     pos = at;
   } else {
     pos = a.positions != nullptr ? a.positions[t] : (int64_t)((uint64_t)a.first_position + (uint64_t)t);
   }
-  const bool there = !PAGED || (page >= 0 && page < a.seqs.n_pages);
 
   const int half = a.rotary_dim >> 1;
   if (lane < half) {
@@ -221,16 +223,12 @@ __global__ void __launch_bounds__(64 * kRotWaves) rotate_kernel(RotateArgs a) {
           (T*)a.v_out + out, a.ko_head, nullptr);
 }
 
-template <typename T, int D>
-void launch_d(const RotateArgs& a, int wgs, hipStream_t s) {
-  if (a.paged) hipLaunchKernelGGL((rotate_kernel<T, D, true>), dim3(wgs), dim3(64 * kRotWaves), 0, s, a);
-  else hipLaunchKernelGGL((rotate_kernel<T, D, false>), dim3(wgs), dim3(64 * kRotWaves), 0, s, a);
+template <typename T, int D, typename Args>
+void launch_d(const Args& a, int wgs, hipStream_t s) {
+  hipLaunchKernelGGL((rotate_kernel<T, D, Args>), dim3(wgs), dim3(64 * kRotWaves), 0, s, a);
 }
-
-}  // namespace
-
-hipError_t launch_rotate(const RotateArgs& args, hipStream_t s) {
-  RotateArgs a = args;
+template <typename Args>
+hipError_t launch(Args a, hipStream_t s) {
   const int rows = a.n_q + a.n_k + a.n_v, rpp = 64 / (a.head_dim / (a.bf16 ? 8 : 4));
   const int groups = (rows + rpp - 1) / rpp;
   // few tokens: their rows over several waves, until the chip has some 2,048
@@ -244,5 +242,10 @@ hipError_t launch_rotate(const RotateArgs& args, hipStream_t s) {
   else a.head_dim == 128 ? launch_d<float, 128>(a, wgs, s) : launch_d<float, 64>(a, wgs, s);
   return hipGetLastError();
 }
+
+}  // namespace
+
+hipError_t launch_rotate(const RotateArgs& a, hipStream_t s) { return launch(a, s); }
+hipError_t launch_rotate(const AppendPagesArgs& a, hipStream_t s) { return launch(a, s); }
 
 }  // namespace infllm
