@@ -289,10 +289,14 @@ __global__ void __launch_bounds__(256) prefix_merge_kernel(PrefixArgs a) {
 // workgroups of each part's item join a P-th of the rows, so that none is idle.  SPLIT: few
 // rows to an item (decoding), a wave per row whose lane groups take every GR-th part; else
 // a group of lanes per row.  Bound by its chain of loads (arguments, the parts' rows): 4.5
-// to 5 us for one token's parts, 6.5 for 48 sequences', 12.5 where two chunks of 512 and 300
+// to 5 us for one token's parts, 6.5 for 48 sequences', 10.5 where two chunks of 512 and 300
 // tokens join some 50,000 partial rows (13.6 MB read, 4.4 written).
-template <typename T, bool HALF, int D, bool SPLIT>
-__global__ void __launch_bounds__(256) paged_merge_kernel(PagedArgs a) {
+//
+// TURNS: a workgroup takes its rows in turns of `at_once`.  Where the workgroups do not all fit
+// the chip (2,048 of them), half as many are quicker: that batch 10.5 us, not 12.8; where
+// they do, a loop costs 0.4 of 6.6.
+template <typename T, bool HALF, int D, bool SPLIT, bool TURNS>
+__global__ void __launch_bounds__(256) paged_merge_kernel(PagedArgs a, int at_once) {
   constexpr int DPT = HALF ? 8 : 4, TPR = D / DPT, GR = SPLIT ? 64 / TPR : 1;
   const int item = div_by(blockIdx.x, a.d_kv), g = (int)blockIdx.x - item * (int)a.d_kv.d;
   const PagedWork w = paged_work(a, item);
@@ -303,50 +307,63 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(PagedArgs a) {
   if (parts == 1 || w.part >= parts) return;
   const int rows = min(rows_wg, R - tile0), share = (rows + parts - 1) / parts;
   const int r_end = min(rows, (w.part + 1) * share);
-  const int r = w.part * share + blockIdx.y * (256 / (TPR * GR)) + threadIdx.x / (TPR * GR);
-  if (r >= r_end) return;
+  const int r0 = w.part * share + blockIdx.y * (256 / (TPR * GR)) + threadIdx.x / (TPR * GR);
+  if (r0 >= r_end) return;
   const int grp = SPLIT ? (threadIdx.x / TPR) % GR : 0, c = threadIdx.x % TPR;
-  const int64_t row0 = ((int64_t)(item - w.part) * a.n_kv_heads + g) * a.item_rows + r, step = (int64_t)a.n_kv_heads * a.item_rows;
-  float M = -__builtin_inff(), tot = 0.f, acc[DPT] = {};
-  auto join = [&](auto chunk) {
-    constexpr int CH = decltype(chunk)::value;
-    for (int p0 = grp; p0 < parts; p0 += CH * GR) {
-      float l[CH], o[CH][DPT];
+  const int64_t tile_row0 = ((int64_t)(item - w.part) * a.n_kv_heads + g) * a.item_rows, step = (int64_t)a.n_kv_heads * a.item_rows;
+  auto row = [&](int r) {
+    float M = -__builtin_inff(), tot = 0.f, acc[DPT] = {};
+    auto join = [&](auto chunk) {
+      constexpr int CH = decltype(chunk)::value;
+      for (int p0 = grp; p0 < parts; p0 += CH * GR) {
+        float l[CH], o[CH][DPT];
 #pragma unroll
-      for (int j = 0; j < CH; ++j) load_piece<HALF>(a, row0 + min(p0 + j * GR, parts - 1) * step, c, o[j], l[j]);
-      add_parts<DPT, CH, true>(l, o, (parts - p0 + GR - 1) / GR, p0 > grp, M, tot, acc);
-    }
-  };
-  if (parts <= 2 * GR) join(std::integral_constant<int, 2>{});
-  else if (parts <= 4 * GR) join(std::integral_constant<int, 4>{});
-  else join(std::integral_constant<int, 8>{});
-  if constexpr (SPLIT) {
-#pragma unroll
-    for (int o = TPR; o < 64; o <<= 1) {
-      const float M2 = __shfl_xor(M, o), tot2 = __shfl_xor(tot, o), m_new = fmaxf(M, M2);
-      const float w1 = M == -__builtin_inff() ? 0.f : expf(M - m_new), w2 = M2 == -__builtin_inff() ? 0.f : expf(M2 - m_new);
-      tot = tot * w1 + tot2 * w2;
-#pragma unroll
-      for (int e = 0; e < DPT; ++e) {
-        const float x2 = __shfl_xor(acc[e], o);
-        acc[e] = (M == -__builtin_inff() ? 0.f : acc[e] * w1) + (M2 == -__builtin_inff() ? 0.f : x2 * w2);
+        for (int j = 0; j < CH; ++j) load_piece<HALF>(a, tile_row0 + r + min(p0 + j * GR, parts - 1) * step, c, o[j], l[j]);
+        add_parts<DPT, CH, true>(l, o, (parts - p0 + GR - 1) / GR, p0 > grp, M, tot, acc);
       }
-      M = m_new;
+    };
+    if (parts <= 2 * GR) join(std::integral_constant<int, 2>{});
+    else if (parts <= 4 * GR) join(std::integral_constant<int, 4>{});
+    else join(std::integral_constant<int, 8>{});
+    if constexpr (SPLIT) {
+#pragma unroll
+      for (int o = TPR; o < 64; o <<= 1) {
+        const float M2 = __shfl_xor(M, o), tot2 = __shfl_xor(tot, o), m_new = fmaxf(M, M2);
+        const float w1 = M == -__builtin_inff() ? 0.f : expf(M - m_new), w2 = M2 == -__builtin_inff() ? 0.f : expf(M2 - m_new);
+        tot = tot * w1 + tot2 * w2;
+#pragma unroll
+        for (int e = 0; e < DPT; ++e) {
+          const float x2 = __shfl_xor(acc[e], o);
+          acc[e] = (M == -__builtin_inff() ? 0.f : acc[e] * w1) + (M2 == -__builtin_inff() ? 0.f : x2 * w2);
+        }
+        M = m_new;
+      }
+      if (grp != 0) return;
     }
-    if (grp != 0) return;
+    const int i = div_by(tile0 + r, a.d_group), h = g * G + tile0 + r - i * G;
+    store_row_piece<T, DPT>((T*)a.out + (int64_t)(w.start + i) * a.out_tok + (int64_t)h * a.out_head + DPT * c,
+                            a.lse != nullptr && c == 0 ? a.lse + h * a.lse_stride + w.start + i : nullptr, M, tot, acc);
+  };
+  if constexpr (TURNS) {
+    for (int r = r0; r < r_end; r += at_once) row(r);
+  } else {
+    row(r0);
   }
-  const int i = div_by(tile0 + r, a.d_group), h = g * G + tile0 + r - i * G;
-  store_row_piece<T, DPT>((T*)a.out + (int64_t)(w.start + i) * a.out_tok + (int64_t)h * a.out_head + DPT * c,
-                          a.lse != nullptr && c == 0 ? a.lse + h * a.lse_stride + w.start + i : nullptr, M, tot, acc);
 }
 template <typename T, bool HALF, int D>
 void launch_paged_merge_t(const PagedArgs& a, hipStream_t s) {
   constexpr int groups = 256 / (D / (HALF ? 8 : 4));  // of a workgroup
   const bool split = a.item_rows <= 16;
   const int per_wg = split ? 4 : groups, share = (a.item_rows + 1) / 2;  // (of two parts, the most)
-  const dim3 grid(a.items * a.n_kv_heads, (share + per_wg - 1) / per_wg), block(256);
-  if (split) hipLaunchKernelGGL((paged_merge_kernel<T, HALF, D, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((paged_merge_kernel<T, HALF, D, false>), grid, block, 0, s, a);
+  const int wgs = a.items * a.n_kv_heads, turns = (share + per_wg - 1) / per_wg;
+  const dim3 block(256);
+  if (split) {
+    hipLaunchKernelGGL((paged_merge_kernel<T, HALF, D, true, false>), dim3(wgs, turns), block, 0, s, a, 0);
+  } else if ((int64_t)wgs * turns <= 2048 || turns < 4) {
+    hipLaunchKernelGGL((paged_merge_kernel<T, HALF, D, false, false>), dim3(wgs, turns), block, 0, s, a, 0);
+  } else {
+    hipLaunchKernelGGL((paged_merge_kernel<T, HALF, D, false, true>), dim3(wgs, turns / 2), block, 0, s, a, turns / 2 * per_wg);
+  }
 }
 
 constexpr int kManyRows = 1024;  // most rows whose many parts are split over threads

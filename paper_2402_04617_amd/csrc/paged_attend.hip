@@ -22,9 +22,9 @@
 // cores busy 68 % of the cycles, 5.2 vector instructions for each of theirs).  The cap adds
 // an exponential and a reciprocal to a score and makes the vector ALU the bound (10.8 vector
 // instructions for one matrix instruction; 700, 1,500 and 64 tokens with a window of 4,096:
-// 107 us, 0.65 PFLOP/s), the bias two multiply-adds (7.2; 125 us, 0.80).  Single tokens beside
+// 107 us, 0.65 PFLOP/s), the bias two multiply-adds (7.2; 122 us with the merge, 0.82).  Single tokens beside
 // chunks read their keys from memory while chunks have theirs in the caches: 512 and 300 new
-// tokens and 30 single ones (613 MB) 165 us and 13 for the merge.  A few rows: see few_rows.
+// tokens and 30 single ones (613 MB) 165 us and 10.5 for the merge.  A few rows: see few_rows.
 #include <type_traits>
 
 #include "mfma_tile.h"

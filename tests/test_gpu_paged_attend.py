@@ -262,6 +262,20 @@ def test_batches_padded_with_empty_sequences(before, between, behind):
     assert torch.isfinite(lse).all() and not (lse[0] == 7).any()
 
 
+@pytest.mark.parametrize("dtype,Hq,new,past,step", [("bf16", 32, 300, 6000, 150), ("f32", 8, 150, 1500, 60)])
+def test_more_partial_rows_than_workgroups_at_once(dtype, Hq, new, past, step):
+    """A chunk and single tokens in more parts than the chip has places for the merge's workgroups."""
+    singles = 24
+    r = Run((1,) * 11 + (new,) + (1,) * (singles - 11), tuple(range(50, 50 + 11 * step, step)) + (past,) + tuple(range(50 + 11 * step, 50 + singles * step, step)),
+            Hq, 8, 128, 16, dtype)
+    rows = r.ws_bytes() // (128 * 2 + 8 if dtype == "bf16" else 128 * 4 + 4)
+    log(f"[paged] {dtype}: {rows} partial rows")
+    out, lse = r.call()
+    r.verify(out, lse, heads=[0, 13 % Hq, Hq - 1])
+    again = r.call()
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+
+
 def test_shared_pages():
     """Sequences that share a prompt's pages see the same keys as with copies of their own."""
     r = Run((1, 1, 5), (160, 160, 156), 4, 2, 128, 16, "bf16")
