@@ -34,7 +34,7 @@ namespace infllm {
 
 namespace {
 
-constexpr int kCap = 1, kSlopes = 2;  // what scores become
+constexpr int kCap = 1, kSlopes = 2, kWideCap = 4;  // what scores become (see Scores; a cap is either kind)
 constexpr int kTable = 1024;          // key groups whose places are in LDS
 constexpr int kAhead = 3;             // a step looks up the tile that many ahead
 
@@ -192,21 +192,63 @@ __device__ __forceinline__ void form_row(const KeyTiles<KT, THREADS, BACK>& keys
 
 // Scores in the base-2 domain.  The scale, the cap and the bias are part of the
 // exponential's argument: c tanh(x / c) = c - 2 c r with r = 1 / (1 + e^{2 x / c}), and a score
-// to be capped becomes its r first.  The error of some 2^-23 c is far below what rounding P
-// to bf16 does.
+// to be capped becomes its r first (kCap).  That is off by some 2^-23 of c, 2^-20 at most, however
+// small the score is, so it is for caps up to kMostFolded alone: 6e-5 there, thirty times less
+// than rounding P to bf16 does.  Above (kWideCap) a score is capped by itself, off by its own
+// roundings: x (1 - u^2 / 3 + 2 u^4 / 15 - 17 u^6 / 315), u = x / c, where |u| < 3 / 16 (the series'
+// next term is 2^-25 there), else c (1 - 2 r).
+constexpr float kMostFolded = 64.f;
 template <int MOD>
 struct Scores {
-  float scale, cap_in, cap2;
+  float scale, cap_in, cap2, u_in, cap_s;
   static constexpr float kHidden = MOD & kCap ? __builtin_inff() : -__builtin_inff();  // what a hidden key's score becomes
-  __device__ __forceinline__ explicit Scores(const PagedArgs& a) : scale(a.sm_scale * 1.4426950408889634f), cap_in(0.f), cap2(0.f) {
-    if constexpr (MOD & kCap) {
+  __device__ __forceinline__ explicit Scores(const PagedArgs& a)
+      : scale(a.sm_scale * 1.4426950408889634f), cap_in(0.f), cap2(0.f), u_in(0.f), cap_s(0.f) {
+    if constexpr (MOD & (kCap | kWideCap)) {
       cap_in = 2.f * scale / a.softcap;
       cap2 = a.softcap * 1.4426950408889634f;
-      scale = -2.f * cap2;
+    }
+    if constexpr (MOD & kCap) scale = -2.f * cap2;
+    if constexpr (MOD & kWideCap) {
+      u_in = a.sm_scale / a.softcap;
+      cap_s = a.softcap / a.sm_scale;
     }
   }
+  static constexpr float kSeries = 0.1875f;
+  __device__ __forceinline__ float series(float s) const {
+    const float u = s * u_in, u2 = u * u;
+    return s * __builtin_fmaf(__builtin_fmaf(__builtin_fmaf(-17.f / 315.f, u2, 2.f / 15.f), u2, -1.f / 3.f), u2, 1.f);
+  }
+  __device__ __forceinline__ float saturated(float s) const {
+    return __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + fast_exp2(s * cap_in)), 1.f) * cap_s;
+  }
   __device__ __forceinline__ float form(float s) const {
-    return MOD & kCap ? __builtin_amdgcn_rcpf(1.f + fast_exp2(s * cap_in)) : s;
+    if constexpr (MOD & kCap) return __builtin_amdgcn_rcpf(1.f + fast_exp2(s * cap_in));
+    if constexpr (MOD & kWideCap) return fabsf(s * u_in) < kSeries ? series(s) : saturated(s);
+    return s;
+  }
+  // N scores: where the series does for all of the wave's, nothing else is formed (chunks of
+  // 700, 1,500 and 64 tokens under a cap of 65: 107 to 110 us, folded 103 to 106; with scores up
+  // to the cap 156, and 151 with both for every score).
+  template <int N>
+  __device__ __forceinline__ void form_all(float (&s)[N]) const {
+    if constexpr (MOD & kWideCap) {
+      float most = 0.f, x[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        most = fmaxf(most, fabsf(s[i]));
+        x[i] = series(s[i]);
+      }
+      if (__builtin_expect(__ballot(most * u_in >= kSeries) != 0, 0)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = form(s[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] = x[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) s[i] = form(s[i]);
+    }
   }
   // What is added to every score: b, and the cap's own part.
   __device__ __forceinline__ float base(float b) const { return MOD & kCap ? b + cap2 : b; }
@@ -349,9 +391,10 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, PagedSmem<D>& sm, c
     }
     const int k0 = keys.key_of(t) + 16 * wave;
     const bool plain = t >= plain0 && t < plain1 && ok0 == 0xFFFFu;
-    if constexpr (MOD & kCap) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) s[j] = score.form(s[j]);
+    if constexpr (MOD & (kCap | kWideCap)) {
+      float x[4] = {s[0], s[1], s[2], s[3]};
+      score.form_all(x);
+      s = f32x4{x[0], x[1], x[2], x[3]};
     }
     if (!plain) {
       const uint32_t see = ((uint32_t)seen_keys(pos, k0, a.window, a.n_init) & ok0) >> (4 * q4);
@@ -720,11 +763,14 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   };
   // Elements [8i, 8i + 8) of a tile's scores: formed, and hidden where the row does not see the key.
   auto form8 = [&](f32x16 (&s)[2], int i, const Lims& l, bool masked) {
+    float x[8];
+#pragma unroll
+    for (int e = 8 * i; e < 8 * i + 8; ++e) x[e - 8 * i] = s[e >> 4][e & 15];
+    score.form_all(x);
 #pragma unroll
     for (int e = 8 * i; e < 8 * i + 8; ++e) {
       const int c = place_of(e);
-      float z = s[e >> 4][e & 15];
-      if constexpr (MOD & kCap) z = score.form(z);
+      float z = x[e - 8 * i];
       if (masked) {
         const uint32_t see = (uint32_t)((int32_t)(l.vis[e >> 4] << (31 - (c & 31))) >> 31);  // all ones or none
         z = __uint_as_float((__float_as_uint(z) & see) | (__builtin_bit_cast(uint32_t, Scores<MOD>::kHidden) & ~see));
@@ -1336,19 +1382,27 @@ __global__ void __launch_bounds__(64 * NW, D == 64 && NW > 1 ? 2 : 1) paged_f32_
 template <int D, int MOD>
 void launch_form(const PagedArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)(a.items * a.n_kv_heads)), block(2 << a.rows_log2);
-  if (a.bf16 && a.page_size % 8 == 0) hipLaunchKernelGGL((paged_mfma_kernel<D, MOD, true>), grid, block, 0, s, a);
-  else if (a.bf16) hipLaunchKernelGGL((paged_mfma_kernel<D, MOD, false>), grid, block, 0, s, a);
-  else if (a.rows_log2 == 7) hipLaunchKernelGGL((paged_f32_kernel<D, 4, MOD>), grid, block, 0, s, a);
-  else if (a.rows_log2 == 6) hipLaunchKernelGGL((paged_f32_kernel<D, 2, MOD>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((paged_f32_kernel<D, 1, MOD>), grid, block, 0, s, a);
+  if constexpr ((MOD & kWideCap) == 0) {  // (float32 has one form for every cap)
+    if (!a.bf16) {
+      if (a.rows_log2 == 7) hipLaunchKernelGGL((paged_f32_kernel<D, 4, MOD>), grid, block, 0, s, a);
+      else if (a.rows_log2 == 6) hipLaunchKernelGGL((paged_f32_kernel<D, 2, MOD>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((paged_f32_kernel<D, 1, MOD>), grid, block, 0, s, a);
+      return;
+    }
+  }
+  if (a.page_size % 8 == 0) hipLaunchKernelGGL((paged_mfma_kernel<D, MOD, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((paged_mfma_kernel<D, MOD, false>), grid, block, 0, s, a);
 }
 template <int D>
 void launch_d(const PagedArgs& a, hipStream_t s) {
-  const int mod = (a.softcap > 0.f ? kCap : 0) | (a.slopes != nullptr ? kSlopes : 0);
+  const int cap = a.softcap == 0.f ? 0 : a.bf16 && a.softcap > kMostFolded ? kWideCap : kCap;
+  const int mod = cap | (a.slopes != nullptr ? kSlopes : 0);
   if (mod == 0) launch_form<D, 0>(a, s);
   else if (mod == kCap) launch_form<D, kCap>(a, s);
   else if (mod == kSlopes) launch_form<D, kSlopes>(a, s);
-  else launch_form<D, kCap | kSlopes>(a, s);
+  else if (mod == (kCap | kSlopes)) launch_form<D, kCap | kSlopes>(a, s);
+  else if (mod == kWideCap) launch_form<D, kWideCap>(a, s);
+  else launch_form<D, kWideCap | kSlopes>(a, s);
 }
 
 }  // namespace
