@@ -550,7 +550,8 @@ infllm_status infllm_paged_append(const infllm_params* p, const infllm_rotary* r
  * the key at t <= p: z = sm_scale q . k_t;
  *   softcap > 0:  z <- softcap * tanh(z / softcap)  (in float32, as all of z; with bf16 caps up
  *                 to 64 are off by as much as 2^-20 softcap beside float32's roundings of z)
- *   slopes:       z <- z - slopes[h] * (p - t)   (DEVICE float32 [Hq], any finite values)
+ *   slopes:       z <- z - slopes[h] * (p - t)   (DEVICE float32 [Hq], finite; steep ones may take
+ *                 z to -infinity, but none to +infinity for any t <= p)
  *   window > 0:   seen only where t > p - window or t < n_init
  * (for one token, window = l_L + 1 and n_init = l_I: what a step sees over units of one
  * token of which none is looked up).  NULL in place of the struct, or zeros, change nothing. */

@@ -255,6 +255,11 @@ struct Scores {
   __device__ __forceinline__ float exponent(float formed, float base) const { return __builtin_fmaf(formed, scale, base); }
 };
 
+// A head's slope in the base-2 domain, finite: times a distance of 0 it is 0.
+__device__ __forceinline__ float slope_of(float slope) {
+  return fminf(fmaxf(slope * 1.4426950408889634f, -3.402823466e38f), 3.402823466e38f);
+}
+
 // This wave's LDS accesses before it come before those after it.
 __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
@@ -363,7 +368,7 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, PagedSmem<D>& sm, c
     for (int s = 0; s < KSTEPS; ++s) qreg[s] = *(const bf16x8*)(qp + 32 * s);
   }
   float slope = 0.f, m = -__builtin_inff(), neg_m = 0.f, l = 0.f;
-  if constexpr (MOD & kSlopes) slope = a.slopes[qh] * 1.4426950408889634f;
+  if constexpr (MOD & kSlopes) slope = slope_of(a.slopes[qh]);
   f32x4 o[DBLK];
 #pragma unroll
   for (int db = 0; db < DBLK; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -401,10 +406,11 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, PagedSmem<D>& sm, c
 #pragma unroll
       for (int j = 0; j < 4; ++j) s[j] = (see >> j) & 1u ? s[j] : Scores<MOD>::kHidden;
     }
-    const float bias = score.base(MOD & kSlopes ? slope * (float)(k0 + 4 * q4 - pos) : 0.f);
+    const float distance = (float)(k0 + 4 * q4 - pos), base = score.base(0.f);
     float e[4], sum;
     auto exponent = [&](int j, float more) {
-      return score.exponent(s[j], (MOD & kSlopes ? __builtin_fmaf(slope, (float)j, bias) : bias) + more);
+      if constexpr (MOD & kSlopes) return score.exponent(s[j], __builtin_fmaf(slope, fminf(distance + (float)j, 0.f), base)) + more;
+      return score.exponent(s[j], base + more);
     };
     auto weights = [&]() {
 #pragma unroll
@@ -543,11 +549,11 @@ __device__ __forceinline__ void few_rows(const PagedArgs& a, PagedSmem<D>& sm, c
     const int hr = __shfl(h, src);
     const bf16_t* qp = (const bf16_t*)a.q + (int64_t)(p_r - w.past + w.start) * a.q_tok + (int64_t)hr * a.q_head;
     float slope_r = 0.f;
-    if constexpr (MOD & kSlopes) slope_r = a.slopes[hr] * 1.4426950408889634f;
+    if constexpr (MOD & kSlopes) slope_r = slope_of(a.slopes[hr]);
     constexpr int DPL = D / 64;
     float again[DPL], top = 0.f;
     form_row<bf16_t, D>(keys, kbase, vbase, qp, p_r, a.window, a.n_init, [&](float x, int key) {
-      return fast_exp2(score.exponent(score.form(x), score.base(slope_r * (float)(key - p_r)) + nm));
+      return fast_exp2(score.exponent(score.form(x), score.base(slope_r * (float)(key - p_r))) + nm);
     }, again);
 #pragma unroll
     for (int e = 0; e < DPL; ++e) {
@@ -659,7 +665,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     for (int s = 0; s < KSTEPS; ++s) qreg[s] = *(const bf16x8*)(qp + 16 * s);
   }
   float slope = 0.f;
-  if constexpr (MOD & kSlopes) slope = a.slopes[qh] * 1.4426950408889634f;
+  if constexpr (MOD & kSlopes) slope = slope_of(a.slopes[qh]);
 
   const bool bad = keys.fill_first(sm.table);
 #pragma unroll
@@ -738,12 +744,29 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   // Key place c of a tile (element e = 16 kb + j of a lane: 32 kb + 8 (j / 4) + j % 4, its
   // half's 4 gsel aside).
   auto place_of = [](int e) { return 32 * (e >> 4) + 8 * ((e & 15) >> 2) + (e & 3); };
-  // The bias of this half's first key of a tile.
-  auto bias_of = [&](int t) { return score.base(MOD & kSlopes ? slope * (float)(key_of(t) + 4 * gsel - pos) : 0.f); };
-  // The exponent of element e of a tile, b its bias_of plus what is to be added.
-  auto exponent = [&](float s, int e, float b) {
-    if constexpr (MOD & kSlopes) b = __builtin_fmaf(slope, (float)place_of(e), b);
-    return score.exponent(s, b);
+  // What a score is given besides its scale.  NEAR, with a bias: each key's own bias from its
+  // distance (0 for keys behind the query, whose bias must not grow), the maximum taken off the
+  // rounded score, so that a score is off by its own rounding, whatever the slope, and none
+  // passes a maximum formed alike.  Else from the bias of this half's first key, with
+  // the maximum taken off that (two instructions a score, not five): off by at most twice a score's own
+  // rounding where every key of the tile is 64 and more away.
+  struct Bias {
+    float b, distance, more;
+  };
+  auto bias_of = [&](int t, auto near, float more) {
+    Bias x{score.base(more), 0.f, more};
+    if constexpr (MOD & kSlopes) {
+      x.distance = (float)(key_of(t) + 4 * gsel - (int)opaque_v((uint32_t)pos));  // (the 32 sums of two tiles' places would not fit)
+      if constexpr (!decltype(near)::value) x.b = score.base(slope * x.distance) + more;
+    }
+    return x;
+  };
+  // The exponent of element e of a tile.
+  auto exponent = [&](float s, int e, const Bias& x, auto near) {
+    if constexpr ((MOD & kSlopes) == 0) return score.exponent(s, x.b);
+    else if constexpr (decltype(near)::value)
+      return score.exponent(s, __builtin_fmaf(slope, fminf(x.distance + (float)place_of(e), 0.f), score.base(0.f))) + x.more;
+    else return score.exponent(s, __builtin_fmaf(slope, (float)place_of(e), x.b));
   };
   // What a row sees of a tile: a bit for each key of this lane's half from its first on.
   struct Lims {
@@ -780,15 +803,16 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   };
   auto tile_max = [&](const f32x16 (&s)[2], int t) {
     float mx = Scores<MOD>::kHidden;
-    const float b = bias_of(t);
+    const std::true_type near;
+    const Bias b = bias_of(t, near, 0.f);
     if constexpr (MOD & kSlopes) {
       mx = -__builtin_inff();
 #pragma unroll
-      for (int e = 0; e < 32; ++e) mx = fmaxf(mx, exponent(s[e >> 4][e & 15], e, b));
+      for (int e = 0; e < 32; ++e) mx = fmaxf(mx, exponent(s[e >> 4][e & 15], e, b, near));
     } else {
 #pragma unroll
       for (int e = 0; e < 32; ++e) mx = MOD & kCap ? fminf(mx, s[e >> 4][e & 15]) : fmaxf(mx, s[e >> 4][e & 15]);
-      mx = score.exponent(mx, b);
+      mx = score.exponent(mx, b.b);
     }
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
     return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
@@ -820,8 +844,8 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   };
   // Two weights as a bf16 pair; the row sums add them unrounded.  (Rounded by at most 2^-8
   // of each: the instruction takes bf16 weights with bf16 values.)
-  auto p_pair = [&](float z0, float z1, int e, float b, float (&acc)[2], bool first) -> uint32_t {
-    const float e0 = fast_exp2(exponent(z0, e, b)), e1 = fast_exp2(exponent(z1, e + 1, b));
+  auto p_pair = [&](float z0, float z1, int e, const Bias& b, auto near, float (&acc)[2], bool first) -> uint32_t {
+    const float e0 = fast_exp2(exponent(z0, e, b, near)), e1 = fast_exp2(exponent(z1, e + 1, b, near));
     acc[0] = first ? e0 : acc[0] + e0;
     acc[1] = first ? e1 : acc[1] + e1;
     bf16x2 pr;
@@ -831,17 +855,26 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   };
   auto half_p = [&](const f32x16 (&s)[2], int h, int t, u32x4 (&p)[2]) {
     float ps[2];
-    const float b = bias_of(t) + neg_m;
+    const std::true_type near;
+    const Bias b = bias_of(t, near, neg_m);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) p[i >> 2][i & 3] = p_pair(s[h][2 * i], s[h][2 * i + 1], 16 * h + 2 * i, b, ps, i == 0);
+    for (int i = 0; i < 8; ++i) p[i >> 2][i & 3] = p_pair(s[h][2 * i], s[h][2 * i + 1], 16 * h + 2 * i, b, near, ps, i == 0);
     return ps[0] + ps[1];
   };
   auto as_frag = [](const u32x4& x) { return __builtin_bit_cast(bf16x8, x); };
 
-  // Tiles all of whose keys every row of the workgroup sees: [plain0, plain1).
+  // Tiles all of whose keys every row of the workgroup sees: [plain0, plain1).  With a bias those
+  // among them whose keys are 64 positions and more before every row; what comes before plain0 is
+  // near then, and so is tile plain0 as the current one of its step.
   int plain0 = a.window > 0 ? (max(0, w.past + i1 - a.window + 1) + KB - 1) / KB : 0;
-  int plain1 = has_bad ? 0 : (w.past + i0 + 1) / KB;
+  int plain1 = has_bad ? 0 : max(0, w.past + i0 + (MOD & kSlopes ? 1 - KB : 1)) / KB;
+  if constexpr (MOD & kSlopes) {
+    // (scores past 2^24, whose roundings pass 1: each is formed the near way, or the maximum could
+    // lie so far from them that their exponentials overflow)
+    if (__ballot(fabsf(slope) * (float)(pos - keys.lowest()) > 16777216.f) != 0) plain1 = 0;
+  }
   keys.range(&plain0, &plain1);
+  if constexpr (MOD & kSlopes) ++plain0;
 
   // Step of tile t: QK(t+1) beside the second half of P(t), then PV(t) beside the form, mask
   // and first half of P of tile t+1.  At its top K(t+1) and V(t) have landed; it requests
@@ -866,14 +899,14 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     }
     __builtin_amdgcn_s_setprio(1);
   };
-  auto step = [&](int t, f32x16 (&cur)[2], f32x16 (&nxt)[2], auto next_masked) {
+  auto step = [&](int t, f32x16 (&cur)[2], f32x16 (&nxt)[2], auto next_masked, auto near) {
     constexpr bool MASK = decltype(next_masked)::value;
     const int bc = (t - t_begin) & 1, bn = bc ^ 1;
     u32x4 w1[2];
     float ps1[2];
     bf16x8 va[DBLK];
     const uint32_t vaddr = vaddr_of(bc);
-    const float bc_m = bias_of(t) + neg_m;
+    const Bias bc_m = bias_of(t, near, neg_m);
     {
       const uint32_t ka = kaddr_of(bn);
       bf16x8 a0[2], a1[2];
@@ -903,7 +936,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
 #pragma unroll
         for (int i = 0; i < EPC; i += 2) {
           const int x = (EPC * s + i) >> 1;
-          w1[x >> 2][x & 3] = p_pair(cur[1][2 * x], cur[1][2 * x + 1], 16 + 2 * x, bc_m, ps1, x == 0);
+          w1[x >> 2][x & 3] = p_pair(cur[1][2 * x], cur[1][2 * x + 1], 16 + 2 * x, bc_m, near, ps1, x == 0);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -918,7 +951,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     float ps0[2];
     {
       const Lims l = lims_of(t + 1, MASK);
-      const float bn_m = bias_of(t + 1) + neg_m;
+      const Bias bn_m = bias_of(t + 1, near, neg_m);
       Entries en;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -937,7 +970,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int x = 2 * j + i;
-          q0[x >> 2][x & 3] = p_pair(nxt[0][2 * x], nxt[0][2 * x + 1], 2 * x, bn_m, ps0, x == 0);
+          q0[x >> 2][x & 3] = p_pair(nxt[0][2 * x], nxt[0][2 * x + 1], 2 * x, bn_m, near, ps0, x == 0);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -984,28 +1017,30 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     set_max(tile_max(sA, t_begin));  // the first tile's maximum
     l_pend = half_p(sA, 0, t_begin, p0);
     int t = t_begin;
-    // pairs whose next tiles need a mask, plain pairs, pairs that need one again
+    // pairs whose next tiles need a mask (with a bias: or are near), plain pairs, pairs that need one again
+    const std::true_type yes;
+    const std::false_type no;
     for (; t + 2 < t_end && t + 1 < plain0; t += 2) {
       top(t);
-      step(t, sA, sB, std::true_type{});
+      step(t, sA, sB, yes, yes);
       top(t + 1);
-      step(t + 1, sB, sA, std::true_type{});
+      step(t + 1, sB, sA, yes, yes);
     }
     for (; t + 2 < plain1; t += 2) {
       top(t);
-      step(t, sA, sB, std::false_type{});
+      step(t, sA, sB, no, no);
       top(t + 1);
-      step(t + 1, sB, sA, std::false_type{});
+      step(t + 1, sB, sA, no, no);
     }
     for (; t + 2 < t_end; t += 2) {
       top(t);
-      step(t, sA, sB, std::true_type{});
+      step(t, sA, sB, yes, no);
       top(t + 1);
-      step(t + 1, sB, sA, std::true_type{});
+      step(t + 1, sB, sA, yes, no);
     }
     if (t + 1 < t_end) {
       top(t);
-      step(t, sA, sB, std::true_type{});
+      step(t, sA, sB, yes, yes);
       sA[0] = sB[0];
       sA[1] = sB[1];
       ++t;
@@ -1098,7 +1133,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
         float acc[DPL];
         form_row<bf16_t, D>(keys, kbase, vbase, (const bf16_t*)late.q + (int64_t)(w.start + i) * late.q_tok + (int64_t)h * late.q_head,
                             p_r, a.window, a.n_init,
-                            [&](float s, int key) { return fast_exp2(score.exponent(score.form(s), score.base(slope_r * (float)(key - p_r)) + nm)); }, acc);
+                            [&](float s, int key) { return fast_exp2(score.exponent(score.form(s), score.base(slope_r * (float)(key - p_r))) + nm); }, acc);
         float amax = 0.f;  // (of the finite ones, which keep their precision)
 #pragma unroll
         for (int e = 0; e < DPL; ++e) {

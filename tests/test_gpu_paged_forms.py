@@ -116,3 +116,49 @@ def test_values_that_are_not_finite_under_a_cap(dtype, D, cap):
         count = torch.arange(past + 1, past + news[0] + 1).double().log()
         top = torch.where(q > 0, torch.full_like(q, cap), torch.full_like(q, -cap)) + count
         check("lse", lse[:, :news[0]], top, (16 * cap + past + news[0] + 16) * U32 + 4 * U32 * top.abs())
+
+
+STEEP = [[1e5, 1e3, 7.0, 0.3], [3.3e6, 0.0, -0.05, 1.0], [1e30, 1e-30, -1e-3, 12345.678], [3.4e38, 1e37, 2e35, 6e36]]
+
+
+@pytest.mark.parametrize("dtype,D,page", [("bf16", 128, 16), ("bf16", 64, 50), ("f32", 64, 16)])
+@pytest.mark.parametrize("slopes", STEEP, ids=str)
+@pytest.mark.parametrize("kw", [dict(), dict(cap=5.0), dict(cap=1e3), dict(window=90, n_init=33), dict(window=2000, n_init=3)], ids=str)
+def test_steep_biases(kw, slopes, dtype, D, page):
+    """The key at the query's own position keeps its score, however steep the bias is."""
+    for news, pasts in (((1, 200, 3, 1), (900, 30, 0, 6000)), ((130,), (1900,)), ((64, 65, 127), (64, 63, 1))):
+        r = with_form(dtype, D, news, pasts, page=page, slopes=slopes, **kw)
+        verify(r, *r.call(), cap=kw.get("cap", 0.0), slopes=slopes)
+
+
+def test_steep_biases_of_one_head_each():
+    """Row tiles of 128 queries: rows and their nearest keys in different tiles."""
+    for slopes, pasts in (([1e5, 2e3], (3000, 65)), ([77.0, 1e4], (5001, 127))):
+        r = with_form("bf16", 128, (300, 128), pasts, Hq=2, Hkv=2, slopes=slopes)
+        verify(r, *r.call(), slopes=slopes)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("bf16", 64), ("f32", 64)])
+@pytest.mark.parametrize("slopes", [[1e3, 50.0, 0.5, -0.02], [1e5, 1e9, 1e25, -10.0]], ids=str)
+def test_steep_biases_whose_nearest_keys_are_far(slopes, dtype, D):
+    """The last pages are not followed: the nearest key that a query sees is hundreds of positions before it."""
+    for news, pasts in (((1, 2), (900, 5000)), ((60, 1), (1500, 300))):
+        r = with_form(dtype, D, news, pasts, slopes=slopes)
+        bad = {}
+        for i, (new, past) in enumerate(zip(news, pasts)):
+            pages = -(-(new + past) // 16)
+            bad[i] = range(pages - 16, pages)
+            r.c.table[i, pages - 16:pages] = -1
+        out, lse = r.call()
+        r.slopes = torch.tensor(slopes, dtype=torch.float32)
+        at = 0
+        for i, (new, past) in enumerate(zip(news, pasts)):
+            seen = seen_by(past, new)
+            for x in bad[i]:
+                seen[:, x * 16:(x + 1) * 16] = False
+            distance = (torch.arange(past, past + new)[:, None] - torch.arange(past + new)[None]).double()
+            for h in range(4):
+                w = form64(r.q[at:at + new, h].double(), r.c.keys[i][:, 0].double(), r.c.values[i][:, 0].double(), r.scale, seen, distance, dtype, 0.0, float(r.slopes[h]))
+                check(f"lse, sequence {i}, head {h}", lse[h, at:at + new], w[1], w[3])
+                check(f"out, sequence {i}, head {h}", out[at:at + new, h], w[0], w[2])
+            at += new
