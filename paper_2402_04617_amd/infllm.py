@@ -364,6 +364,16 @@ def infllm_rope_frequencies(rotary_dim: int, base: float = 500000.0, scaling: st
     return list(out)[:rotary_dim // 2]
 
 
+def _entries(name, x, dtype, least):
+    """A tensor that the device reads entry by entry: of that torch dtype, one after another, `least` at least.  (Raw
+    pointers are the caller's.)"""
+    if x is None or isinstance(x, int):
+        return
+    if str(x.dtype) != dtype or not x.is_contiguous() or x.numel() < least:
+        raise ValueError(f"{name}: {least} entries of {dtype} next to one another needed, got {tuple(x.shape)} of {x.dtype} with "
+                         f"strides {tuple(x.stride())}")
+
+
 def infllm_rotate(p, rot, n_tokens, positions, q, q_strides, q_out, q_out_strides, k, k_strides, k_out, k_out_strides,
                   first_position=0, stream=None):
     """positions: int64 tensor, or None for first_position + t; strides: (token, head) in elements (of what is None
@@ -372,6 +382,7 @@ def infllm_rotate(p, rot, n_tokens, positions, q, q_strides, q_out, q_out_stride
     qot, qoh = q_out_strides or (0, 0)
     kt, kh = k_strides or (0, 0)
     kot, koh = k_out_strides or (0, 0)
+    _entries("positions", positions, "torch.int64", n_tokens)
     _check("infllm_rotate", lib().infllm_rotate(
         ctypes.byref(p), ctypes.byref(rot), n_tokens, _ptr(positions), first_position, _ptr(q), qt, qh, _ptr(q_out),
         qot, qoh, _ptr(k), kt, kh, _ptr(k_out), kot, koh, _stream(stream)))
