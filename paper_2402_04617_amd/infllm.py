@@ -374,6 +374,16 @@ def _entries(name, x, dtype, least):
                          f"strides {tuple(x.stride())}")
 
 
+_DTYPES = {"torch.float32": INFLLM_F32, "torch.bfloat16": INFLLM_BF16}
+
+
+def _layer_weights(p, rot):
+    """Norm weights given to rotary() as tensors: head_dim elements of the layer's type."""
+    for name, n, dtype in getattr(rot, "_weights", ()):
+        if n != p.head_dim or dtype != p.dtype:
+            raise ValueError(f"{name}: {p.head_dim} elements of the layer's type needed, got {n} of type {dtype} (layer: {p.dtype})")
+
+
 def infllm_rotate(p, rot, n_tokens, positions, q, q_strides, q_out, q_out_strides, k, k_strides, k_out, k_out_strides,
                   first_position=0, stream=None):
     """positions: int64 tensor, or None for first_position + t; strides: (token, head) in elements (of what is None
@@ -383,6 +393,7 @@ def infllm_rotate(p, rot, n_tokens, positions, q, q_strides, q_out, q_out_stride
     kt, kh = k_strides or (0, 0)
     kot, koh = k_out_strides or (0, 0)
     _entries("positions", positions, "torch.int64", n_tokens)
+    _layer_weights(p, rot)
     _check("infllm_rotate", lib().infllm_rotate(
         ctypes.byref(p), ctypes.byref(rot), n_tokens, _ptr(positions), first_position, _ptr(q), qt, qh, _ptr(q_out),
         qot, qoh, _ptr(k), kt, kh, _ptr(k_out), kot, koh, _stream(stream)))
@@ -416,6 +427,7 @@ def infllm_paged_append(p, rot, pages, seq_lens, past_lens, page_table, q, q_str
     rot, and q with q_out, may be None."""
     lens, pasts, stride = _seqs(seq_lens, past_lens, page_table, table_stride, pages.page_size)
     qs, qos = q_strides or (0, 0), q_out_strides or (0, 0)
+    _layer_weights(p, rot)
     _check("infllm_paged_append", lib().infllm_paged_append(
         ctypes.byref(p), None if rot is None else ctypes.byref(rot), ctypes.byref(pages), len(lens), _at(lens),
         _at(pasts), _ptr(page_table), stride, _ptr(q), qs[0], qs[1], _ptr(q_out), qos[0], qos[1], _ptr(k), _ptr(v),
@@ -504,11 +516,17 @@ def recommended_ring(p: Params, chunk: int) -> int:
 
 def rotary(inv_freq, interleaved=False, magnitude=1.0, norm=False, q_weight=None, k_weight=None, eps=1e-6) -> Rotary:
     """Rotation by the given frequencies (two dimensions each; an empty list turns nothing) and, with norm, per-head
-    norms with weights of head_dim elements (None: ones).  The struct keeps the weights alive."""
+    norms with weights of head_dim elements in the layer's type (None: ones).  The struct keeps the weights alive."""
     table = (ctypes.c_double * max(1, len(inv_freq)))(*[float(x) for x in inv_freq])
     r = Rotary(2 * len(inv_freq), int(bool(interleaved)), ctypes.cast(table, ctypes.POINTER(ctypes.c_double)), magnitude,
                int(bool(norm)), eps, _ptr(q_weight) if norm else None, _ptr(k_weight) if norm else None)
     r._held = (table, q_weight, k_weight)  # the struct holds raw pointers
+    r._weights = []                        # (name, elements, type) for the calls to check
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if norm and w is not None and not isinstance(w, int):
+            if not w.is_contiguous():
+                raise ValueError(f"{name}: elements next to one another needed, got strides {tuple(w.stride())}")
+            r._weights.append((name, w.numel(), _DTYPES.get(str(w.dtype), w.dtype)))
     return r
 
 

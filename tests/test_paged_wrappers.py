@@ -35,3 +35,34 @@ def test_positions_that_do(L):  # noqa: F811
         pytest.skip("fake pointers")
     for positions in (torch.zeros(5, dtype=torch.int64), torch.zeros(9, dtype=torch.int64)[2:], torch.zeros((1, 5), dtype=torch.int64), FAKE, None):
         past_the_wrapper(lambda: rotate(5, positions))
+
+
+def append(rot):
+    g = F.Pages(100, 16, FAKE, FAKE, 16 * HKV * D, D, 16 * D)
+    F.infllm_paged_append(P(), rot, g, (1,), (0,), FAKE, None, None, None, None, FAKE, FAKE, (HKV * D, D), table_stride=4, stream=FAKE)
+
+
+@pytest.mark.parametrize("which", ["q_weight", "k_weight"])
+@pytest.mark.parametrize("weight", [
+    torch.ones(D), torch.ones(D, dtype=torch.float16), torch.ones(D // 2, dtype=torch.bfloat16), torch.ones((HQ, D), dtype=torch.bfloat16)])
+def test_weights(L, which, weight):  # noqa: F811
+    """Of a bf16 layer: float32 weights (as checkpoints often hold them), other types, other lengths."""
+    rot = F.rotary([0.5] * (D // 2), norm=True, **{which: weight})
+    with pytest.raises(ValueError, match=which):
+        rotate(5, None, rot)
+    with pytest.raises(ValueError, match=which):
+        append(rot)
+    with pytest.raises(ValueError, match=which):
+        F.rotary([], norm=True, **{which: torch.ones(2 * D, dtype=torch.bfloat16)[::2]})
+
+
+def test_weights_that_do(L):  # noqa: F811
+    if torch.cuda.is_available():
+        pytest.skip("fake pointers")
+    one = torch.ones(D + 8, dtype=torch.bfloat16)
+    for w in (one[8:], one[:D].view(1, D), FAKE, None):
+        past_the_wrapper(lambda: rotate(5, None, F.rotary([0.5] * (D // 2), norm=True, q_weight=w, k_weight=w)))
+        past_the_wrapper(lambda: append(F.rotary([], norm=True, q_weight=w, k_weight=w)))
+    past_the_wrapper(lambda: rotate(5, None, F.rotary([], norm=True, q_weight=torch.ones(D)), P(dtype="f32")))
+    past_the_wrapper(lambda: rotate(5, None, F.rotary([], q_weight=torch.ones(D))))      # without norms they are not read
+    past_the_wrapper(lambda: append(None))
