@@ -443,6 +443,8 @@ def infllm_paged_workspace_bytes(p, pages, seq_lens, past_lens, score=None) -> i
 def infllm_paged_attend(p, pages, seq_lens, past_lens, page_table, score, q, q_strides, out, out_strides, lse=None,
                         workspace=None, workspace_bytes=None, table_stride=None, stream=None):
     """As infllm_paged_append; score: a ScoreForm, or None."""
+    if getattr(score, "_n_slopes", p.n_q_heads) != p.n_q_heads:
+        raise ValueError(f"slopes: {p.n_q_heads} needed, one per query head, got {score._n_slopes}")
     lens, pasts, stride = _seqs(seq_lens, past_lens, page_table, table_stride, pages.page_size)
     _check("infllm_paged_attend", lib().infllm_paged_attend(
         ctypes.byref(p), ctypes.byref(pages), len(lens), _at(lens), _at(pasts), _ptr(page_table), stride,
@@ -541,6 +543,9 @@ def pages(k, v, page_size, page_stride=None, token_stride=None, head_stride=None
 
 def score(softcap=0.0, window=0, n_init=0, slopes=None) -> ScoreForm:
     """slopes: float32 tensor of one per query head, or None.  The struct keeps it alive."""
+    _entries("slopes", slopes, "torch.float32", 1)
     st = ScoreForm(softcap, window, n_init, _ptr(slopes))
     st._held = slopes
+    if slopes is not None and not isinstance(slopes, int):
+        st._n_slopes = slopes.numel()      # (for the calls to check)
     return st

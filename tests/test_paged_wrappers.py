@@ -66,3 +66,27 @@ def test_weights_that_do(L):  # noqa: F811
     past_the_wrapper(lambda: rotate(5, None, F.rotary([], norm=True, q_weight=torch.ones(D)), P(dtype="f32")))
     past_the_wrapper(lambda: rotate(5, None, F.rotary([], q_weight=torch.ones(D))))      # without norms they are not read
     past_the_wrapper(lambda: append(None))
+
+
+def attend(score=None, pages=None, table=FAKE, table_stride=4, p=None, lens=(1,), pasts=(0,)):
+    g = F.Pages(100, 16, FAKE, FAKE, 16 * HKV * D, D, 16 * D) if pages is None else pages
+    F.infllm_paged_attend(P() if p is None else p, g, lens, pasts, table, score, FAKE, (HQ * D, D), FAKE, (HQ * D, D), table_stride=table_stride,
+                          stream=FAKE)
+
+
+def test_slopes(L):  # noqa: F811
+    for slopes in (torch.ones(HQ, dtype=torch.bfloat16), torch.ones(HQ, dtype=torch.float64), torch.ones(2 * HQ)[::2], torch.ones(0)):
+        with pytest.raises(ValueError, match="slopes"):
+            F.score(slopes=slopes)
+    for n in (1, HKV, HQ - 1, HQ + 1):
+        with pytest.raises(ValueError, match="slopes"):
+            attend(F.score(slopes=torch.ones(n)))
+
+
+def test_slopes_that_do(L):  # noqa: F811
+    if torch.cuda.is_available():
+        pytest.skip("fake pointers")
+    for slopes in (torch.ones(HQ), torch.ones((HKV, HQ // HKV)), torch.ones(2 * HQ)[HQ:], FAKE, None):
+        past_the_wrapper(lambda: attend(F.score(softcap=3.0, slopes=slopes)))
+    past_the_wrapper(lambda: attend(F.ScoreForm(window=5, slopes=FAKE)))
+    past_the_wrapper(lambda: attend(None))
