@@ -404,14 +404,16 @@ def _seqs(seq_lens, past_lens, page_table, table_stride, page_size=0):
     lens, pasts = _i32s(seq_lens), _i64s(past_lens)
     if len(lens) != len(pasts):
         raise ValueError("one past length per sequence")
+    if page_table is not None and not isinstance(page_table, int) and str(page_table.dtype) != "torch.int32":
+        raise ValueError(f"page_table is int32, got {page_table.dtype}")
     if table_stride is None:
         if page_table is None:
             return lens, pasts, 0
         if page_table.size(0) < len(lens):
             raise ValueError(f"page_table needs {len(lens)} rows, got {page_table.size(0)}")
         width, table_stride = page_table.size(1), page_table.stride(0)
-        if page_table.element_size() != 4 or (width > 1 and page_table.stride(1) != 1):
-            raise ValueError("page_table is int32, a row's entries next to one another")
+        if width > 1 and page_table.stride(1) != 1:
+            raise ValueError("a row's entries of page_table lie next to one another")
         if len(lens) < 2:
             table_stride = width
         elif table_stride > width and page_size:  # (rows of a wider table: the library knows their stride alone)

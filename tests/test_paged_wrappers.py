@@ -90,3 +90,22 @@ def test_slopes_that_do(L):  # noqa: F811
         past_the_wrapper(lambda: attend(F.score(softcap=3.0, slopes=slopes)))
     past_the_wrapper(lambda: attend(F.ScoreForm(window=5, slopes=FAKE)))
     past_the_wrapper(lambda: attend(None))
+
+
+def test_page_tables(L):  # noqa: F811
+    for dtype in (torch.float32, torch.int64, torch.int16):
+        for stride in (None, 4):
+            with pytest.raises(ValueError, match="page_table"):
+                attend(table=torch.zeros((2, 4), dtype=dtype), table_stride=stride)
+            with pytest.raises(ValueError, match="page_table"):
+                g = F.Pages(100, 16, FAKE, FAKE, 16 * HKV * D, D, 16 * D)
+                F.infllm_paged_append(P(), None, g, (1, 1), (0, 0), torch.zeros((2, 4), dtype=dtype), None, None, None, None, FAKE, FAKE,
+                                      (HKV * D, D), table_stride=stride, stream=FAKE)
+
+
+def test_page_tables_that_do(L):  # noqa: F811
+    if torch.cuda.is_available():
+        pytest.skip("fake pointers")
+    table = torch.zeros((2, 4), dtype=torch.int32)
+    for stride in (None, 4):
+        past_the_wrapper(lambda: attend(table=table, table_stride=stride, lens=(1, 1), pasts=(0, 63)))
