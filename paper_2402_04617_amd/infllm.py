@@ -423,6 +423,21 @@ def _seqs(seq_lens, past_lens, page_table, table_stride, page_size=0):
     return lens, pasts, table_stride
 
 
+def _layer_pages(p, g):
+    """Pages given to pages() as tensors: of the layer's type, and all of its rows within the tensors' memory."""
+    held, layer = getattr(g, "_held", None), (p.dtype, p.n_kv_heads, p.head_dim)
+    if held is None or g._fits == layer:
+        return
+    reach = (g.n_pages - 1) * g.page_stride + (g.page_size - 1) * g.token_stride + (p.n_kv_heads - 1) * g.head_stride + p.head_dim
+    for name, x in zip("kv", held):
+        if _DTYPES.get(str(x.dtype)) != p.dtype:
+            raise ValueError(f"{name}: the layer's type needed ({p.dtype}), got {x.dtype}")
+        room = x.untyped_storage().nbytes() // x.element_size() - x.storage_offset()
+        if reach > room:
+            raise ValueError(f"{name}: pages, slots and {p.n_kv_heads} heads of {p.head_dim} reach {reach} elements, the tensor's memory holds {room}")
+    g._fits = layer
+
+
 def infllm_paged_append(p, rot, pages, seq_lens, past_lens, page_table, q, q_strides, q_out, q_out_strides, k, v,
                         kv_strides, table_stride=None, stream=None):
     """seq_lens, past_lens: host ints, one of each per sequence; page_table: int32 tensor [n_seqs][pages of a sequence];
@@ -430,6 +445,7 @@ def infllm_paged_append(p, rot, pages, seq_lens, past_lens, page_table, q, q_str
     lens, pasts, stride = _seqs(seq_lens, past_lens, page_table, table_stride, pages.page_size)
     qs, qos = q_strides or (0, 0), q_out_strides or (0, 0)
     _layer_weights(p, rot)
+    _layer_pages(p, pages)
     _check("infllm_paged_append", lib().infllm_paged_append(
         ctypes.byref(p), None if rot is None else ctypes.byref(rot), ctypes.byref(pages), len(lens), _at(lens),
         _at(pasts), _ptr(page_table), stride, _ptr(q), qs[0], qs[1], _ptr(q_out), qos[0], qos[1], _ptr(k), _ptr(v),
@@ -447,6 +463,7 @@ def infllm_paged_attend(p, pages, seq_lens, past_lens, page_table, score, q, q_s
     """As infllm_paged_append; score: a ScoreForm, or None."""
     if getattr(score, "_n_slopes", p.n_q_heads) != p.n_q_heads:
         raise ValueError(f"slopes: {p.n_q_heads} needed, one per query head, got {score._n_slopes}")
+    _layer_pages(p, pages)
     lens, pasts, stride = _seqs(seq_lens, past_lens, page_table, table_stride, pages.page_size)
     _check("infllm_paged_attend", lib().infllm_paged_attend(
         ctypes.byref(p), ctypes.byref(pages), len(lens), _at(lens), _at(pasts), _ptr(page_table), stride,
@@ -535,11 +552,17 @@ def rotary(inv_freq, interleaved=False, magnitude=1.0, norm=False, q_weight=None
 
 
 def pages(k, v, page_size, page_stride=None, token_stride=None, head_stride=None) -> Pages:
-    """Pages in tensors k and v whose first dimension counts them: by default [n_pages][Hkv][page_size][D] with the
-    tensors' own strides."""
+    """Pages in tensors k and v of one type, shape and strides whose first dimension counts them: by default
+    [n_pages][Hkv][page_size][D] with the tensors' own strides."""
+    if k.dtype != v.dtype or k.shape != v.shape or any(n > 1 and a != b for n, a, b in zip(k.shape, k.stride(), v.stride())):
+        raise ValueError(f"k and v need one type, shape and strides, got {k.dtype}, {tuple(k.shape)}, {tuple(k.stride())} and "
+                         f"{v.dtype}, {tuple(v.shape)}, {tuple(v.stride())}")
+    if k.shape[-1] > 1 and k.stride(-1) != 1:
+        raise ValueError(f"the elements of a row lie next to one another, got strides {tuple(k.stride())}")
     st = Pages(k.shape[0], page_size, k.data_ptr(), v.data_ptr(), k.stride(0) if page_stride is None else page_stride,
                k.stride(2) if token_stride is None else token_stride, k.stride(1) if head_stride is None else head_stride)
     st._held = (k, v)
+    st._fits = None                        # the layer that _layer_pages has found to fit
     return st
 
 

@@ -109,3 +109,39 @@ def test_page_tables_that_do(L):  # noqa: F811
     table = torch.zeros((2, 4), dtype=torch.int32)
     for stride in (None, 4):
         past_the_wrapper(lambda: attend(table=table, table_stride=stride, lens=(1, 1), pasts=(0, 63)))
+
+
+def test_pages(L):  # noqa: F811
+    k = torch.zeros((6, HKV, 16, D), dtype=torch.bfloat16)
+    for v in (k.float(), k[:5], torch.zeros((6, 16, HKV, D), dtype=torch.bfloat16), torch.zeros((6, 16, HKV, D), dtype=torch.bfloat16).transpose(1, 2),
+              torch.zeros((6, HKV, 16, D + 8), dtype=torch.bfloat16)[..., :D]):
+        with pytest.raises(ValueError, match="k and v"):
+            F.pages(k, v, 16)
+    t = torch.zeros((6, HKV, D, 16), dtype=torch.bfloat16).transpose(2, 3)
+    with pytest.raises(ValueError, match="row"):
+        F.pages(t, t, 16)
+    # another type than the layer's, and rows behind the tensors' end
+    f = k.float()
+    for g in (F.pages(f, f, 16), F.pages(k, k, 17), F.pages(k[:, :4], k[:, 4:], 16, token_stride=2 * D), F.pages(k[:, 4:], k[:, 4:], 16),
+              F.pages(k[1:], k[1:], 16, page_stride=17 * HKV * D), F.pages(k.view(-1)[:1], k.view(-1)[:1], 1 << 20, HKV * D, HKV * D, D)):
+        with pytest.raises(ValueError, match="[kv]: "):
+            attend(pages=g)
+        with pytest.raises(ValueError, match="[kv]: "):
+            F.infllm_paged_append(P(), None, g, (1,), (0,), FAKE, None, None, None, None, FAKE, FAKE, (HKV * D, D), table_stride=4, stream=FAKE)
+
+
+def test_pages_that_do(L):  # noqa: F811
+    if torch.cuda.is_available():
+        pytest.skip("fake pointers")
+    one = torch.zeros((1, HKV, 16, D), dtype=torch.bfloat16)
+    both = torch.zeros((6, 2, 16, HKV, D + 8), dtype=torch.bfloat16)
+    k = torch.zeros((6, HKV, 16, D), dtype=torch.bfloat16)
+    for g in (F.pages(k, k.clone(), 16), F.pages(k, k, 8), F.pages(one, both.view(-1)[:16 * HKV * D].view(1, HKV, 16, D), 16),
+              F.pages(both[:, 0], both[:, 1], 16, both.stride(0), HKV * (D + 8), D + 8),
+              F.pages(both[:, 0, ..., :D], both[:, 1, ..., :D], 16, both.stride(0), HKV * (D + 8), D + 8),
+              F.pages(k.transpose(1, 2), k.transpose(1, 2), 16, k.stride(0), D, 16 * D)):
+        for _ in range(2):
+            past_the_wrapper(lambda: attend(pages=g))
+    f = k.float()
+    past_the_wrapper(lambda: attend(pages=F.pages(f, f, 16), p=P(dtype="f32")))
+    past_the_wrapper(lambda: attend(pages=F.pages(k, k, 16), p=P(n_q_heads=4, n_kv_heads=4)))
