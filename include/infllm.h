@@ -496,7 +496,8 @@ typedef enum {
 } infllm_rope_scaling;
 /* inv_freq: HOST output of rotary_dim/2.  slow < fast and original_len >= 1 are used by
  * INFLLM_ROPE_PARTS alone.  Host only.  E_SHAPE: an odd or negative rotary_dim, a base
- * or factor that is not finite and > 0, or an unknown scaling. */
+ * (scaled, too) or factor that is not finite and > 0, frequencies past float64, or an unknown
+ * scaling. */
 infllm_status infllm_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double factor,
                                       int64_t original_len, double slow, double fast, double* inv_freq);
 

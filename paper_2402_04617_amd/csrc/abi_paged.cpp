@@ -370,6 +370,10 @@ infllm_status infllm_rope_frequencies(int32_t rotary_dim, double base, int32_t s
   if (rotary_dim == 0) return INFLLM_OK;
   if (inv_freq == nullptr) return INFLLM_E_NULL;
   const double r = rotary_dim, b = scaling == INFLLM_ROPE_BASE ? base * std::pow(factor, r / (r - 2.0)) : base;
+  if (!std::isfinite(b) || !(b > 0.0)) return INFLLM_E_SHAPE;
+  // (the largest frequency is the first or the last: no output is written where one passes float64)
+  const double most = std::max(1.0, std::pow(b, -(r - 2.0) / r));
+  if (!std::isfinite(scaling == INFLLM_ROPE_LINEAR || scaling == INFLLM_ROPE_PARTS ? most / std::min(1.0, factor) : most)) return INFLLM_E_SHAPE;
   for (int i = 0; i < rotary_dim / 2; ++i) {
     double theta = std::pow(b, -2.0 * i / r);
     if (scaling == INFLLM_ROPE_LINEAR) theta /= factor;

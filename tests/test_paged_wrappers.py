@@ -145,3 +145,18 @@ def test_pages_that_do(L):  # noqa: F811
     f = k.float()
     past_the_wrapper(lambda: attend(pages=F.pages(f, f, 16), p=P(dtype="f32")))
     past_the_wrapper(lambda: attend(pages=F.pages(k, k, 16), p=P(n_q_heads=4, n_kv_heads=4)))
+
+
+@pytest.mark.parametrize("kw", [
+    dict(base=1e300, scaling="base", factor=1e9), dict(base=1e-300, scaling="base", factor=1e-30), dict(scaling="linear", factor=1e-310, base=1e-3),
+    dict(scaling="parts", factor=1e-310, original_len=4096, base=1e-10), dict(scaling="linear", factor=5e-324)])
+def test_frequencies_past_float64(L, kw):  # noqa: F811
+    """A base or a frequency that overflows, or a base of 0, is refused, and not returned as 0 or infinity."""
+    with pytest.raises(F.InfllmError):
+        F.infllm_rope_frequencies(64, **kw)
+
+
+def test_frequencies_at_the_ends(L):  # noqa: F811
+    for kw in (dict(base=1e300), dict(base=1e-300), dict(base=1e300, scaling="linear", factor=1e-5), dict(base=1e-250, scaling="base", factor=1e-20)):
+        x = F.infllm_rope_frequencies(64, **kw)
+        assert len(x) == 32 and all(0.0 < y < float("inf") for y in x), kw
