@@ -867,7 +867,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   // among them whose keys are 64 positions and more before every row; what comes before plain0 is
   // near then, and so is tile plain0 as the current one of its step.
   int plain0 = a.window > 0 ? (max(0, w.past + i1 - a.window + 1) + KB - 1) / KB : 0;
-  int plain1 = has_bad ? 0 : max(0, w.past + i0 + (MOD & kSlopes ? 1 - KB : 1)) / KB;
+  int plain1 = max(0, w.past + i0 + (MOD & kSlopes ? 1 - KB : 1)) / KB;
   if constexpr (MOD & kSlopes) {
     // (scores past 2^24, whose roundings pass 1: each is formed the near way, or the maximum could
     // lie so far from them that their exponentials overflow)
@@ -875,6 +875,7 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
   }
   keys.range(&plain0, &plain1);
   if constexpr (MOD & kSlopes) ++plain0;
+  if (has_bad) plain1 = 0;  // (none; never past t_end, where the plain pairs would not stop)
 
   // Step of tile t: QK(t+1) beside the second half of P(t), then PV(t) beside the form, mask
   // and first half of P of tile t+1.  At its top K(t+1) and V(t) have landed; it requests
