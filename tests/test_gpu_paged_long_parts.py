@@ -118,3 +118,11 @@ def test_score_forms_of_shared_keys(form, page):
     """4 to 16 rows of a kv head, all of which share the keys of a tile between the waves."""
     r = Run((1, 4, 3, 1, 2), (1300, 700, 131, 0, 5000), 8, 2, 128, page, "bf16", form=form, q_scale=2.0)
     r.verify(*r.call())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq", [130, 300])
+def test_groups_larger_than_a_row_tile(dtype, Hq):
+    """One kv head for 130 and 300 query heads: row tiles that end within a token's heads."""
+    r = Run((1, 3, 0, 2), (900, 70, 5, 0), Hq, 1, 64, 16, dtype, form=dict(window=300, n_init=9))
+    r.verify(*r.call(), heads=[0, 1, 63, 64, 127, 128, Hq - 2, Hq - 1])
