@@ -457,7 +457,8 @@ infllm_status infllm_copy_sequences(const infllm_params* p, const infllm_memory*
 /* ---- paged caches ------------------------------------------------------------
  * What a program that serves many requests uses for those whose keys and values it
  * keeps in pages rather than in a memory's dense store (questions and passages that fit
- * the window, until they need a memory): rotation of the projections to their positions,
+ * the window; no call moves pages into a memory, which is built from a request's first token):
+ * rotation of the projections to their positions,
  * with the norms of models that have them; the new tokens' keys and values into their
  * pages; and causal attention of the new tokens over them.  All take the positions of
  * infllm_rotary, not the remap (E_UNSUPPORTED with params.rope_inv_freq); of the params

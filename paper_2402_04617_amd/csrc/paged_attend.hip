@@ -20,11 +20,15 @@
 // (2,048 tokens after 64,000, 32 query heads of 128, 8 kv heads: 1.86 to 2.02 ms by card, 1.08
 // to 1.17 PFLOP/s, 85 to 92 % of a library product of 8,192^3 on the same card; the matrix
 // cores busy 68 % of the cycles, 5.2 vector instructions for each of theirs).  The cap adds
-// an exponential and a reciprocal to a score and makes the vector ALU the bound (10.8 vector
-// instructions for one matrix instruction; 700, 1,500 and 64 tokens with a window of 4,096:
-// 107 us, 0.65 PFLOP/s), the bias two multiply-adds (7.2; 122 us with the merge, 0.82).  Single tokens beside
-// chunks read their keys from memory while chunks have theirs in the caches: 512 and 300 new
-// tokens and 30 single ones (613 MB) 165 us and 10.5 for the merge.  A few rows: see few_rows.
+// an exponential and a reciprocal to a score (10.8 vector instructions for one matrix
+// instruction) and makes the vector ALU the bound where the chip is full: 2,048 tokens after
+// 30,000 take 1,165 us with it, 0.89 PFLOP/s, 919 without; with a bias (7.8) 888.  Batches of few
+// row tiles are bound by how these fill the chip, which the host's model does not foresee for
+// either form: 700, 1,500 and 64 tokens, capped, with a window of 4,096 107 to 114 us (the
+// same tiles evenly spread: 81), 300, 800, 25 and two single ones with a bias 115 and 11 to 13 for the
+// merge.  Single tokens beside chunks read their keys from memory while chunks have theirs in the
+// caches: 512 and 300 new tokens and 30 single ones (613 MB) 164 us and 10.6 for the merge.  A few
+// rows: see few_rows.
 #include <type_traits>
 
 #include "mfma_tile.h"
@@ -677,6 +681,10 @@ __global__ void __launch_bounds__(256, 2) paged_mfma_kernel(PagedArgs a) {
     if (lane == 0) sm.bad[wave] = any;
   }
   lds_barrier();
+  // (A page that is not there, seen by a row or not, has every tile of the part masked.  A window
+  // whose pages between it and the initial tokens are freed comes to that where a tile holds both
+  // kinds: 2,048 tokens after 30,000, window 4,096, 152 us with pages of 16 and 100 initial tokens, 137
+  // where all are there; 139 either way with pages of 64 and 128.)
   const bool has_bad = (sm.bad[0] | sm.bad[1] | sm.bad[2] | sm.bad[3]) != 0;
 
   // Places of the wave's rows of tile t (past the part's end: of its last tile again,
